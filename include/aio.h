@@ -424,6 +424,205 @@ int aio_spec_generate(aio_model* target, aio_model* draft, int32_t pos, int32_t 
                       float* draft_logits_dev, int32_t* argmax_dev, int32_t* draft_tokens_dev,
                       int32_t* out, aio_spec_stats* stats);
 
+/* --------------------------------------- several sequences in one pool */
+
+/* The models above serve one sequence per handle.  A router (Section 3.1)
+ * holds many requests, most of them behind shared templates (Section 3.2).
+ * The operators below keep the keys and values of several sequences in one
+ * pool of pages, attend over them, and score what a model answered.  They
+ * take no handle but the hipStream_t they enqueue on (NULL = the default
+ * stream): any layer of any model can use them, and aio_paged_forward runs a
+ * whole model on them.  Device pointers belong to the current HIP device and
+ * are 16-byte aligned unless stated otherwise; every scalar and every host
+ * array is checked before anything is enqueued.  What lies in device memory
+ * (lengths, page ids) cannot be checked on the host: the kernels bound it, so
+ * no value there makes them read or write outside the buffers described.  No
+ * call allocates, synchronises or keeps state, so all of them can be captured
+ * into a HIP graph (which keeps the pointers and host values of the capture). */
+
+/* Element types of rows and logits. */
+enum { AIO_F32 = 0, AIO_BF16 = 1 };
+
+/* Keys and values of one layer, bf16, in pages: slot s of kv head h of page p
+ * is the head_dim elements at p page_stride + h head_stride + s head_dim. */
+typedef struct aio_paged_kv {
+  void* k_dev;
+  void* v_dev;
+  int64_t page_stride; /* elements, a multiple of 8                        */
+  int64_t head_stride; /* elements, a multiple of 8                        */
+  int32_t n_pages;
+  int32_t page_size;   /* positions per page: a power of two, 8 .. 256      */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128                                         */
+} aio_paged_kv;
+
+/* Keys and values of one layer, bf16, of several sequences packed behind one
+ * another: row t of kv head h is the head_dim elements at t row_stride +
+ * h head_stride. */
+typedef struct aio_packed_kv {
+  const void* k_dev;
+  const void* v_dev;
+  int64_t row_stride;  /* elements, a multiple of 8                         */
+  int64_t head_stride; /* elements, a multiple of 8                         */
+  int32_t n_rows;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128                                         */
+} aio_packed_kv;
+
+/* The sequences of a call.  Sequence i has the rows cu_q[i] .. cu_q[i+1] - 1
+ * (cu_q_dev NULL: row i, one new token each, n_rows == n_seqs), which are the
+ * last of its keys: its keys number lens[i] in pages, cu_k[i+1] - cu_k[i]
+ * packed, and row r of its q rows sees keys 0 .. keys - q + r.  In pages,
+ * key j is slot j mod page_size of page table[i][j / page_size].  A page id
+ * outside [0, n_pages) is a hole (an evicted page): its keys are seen by no
+ * row.  Keys past max_len or past the table's width are not there either.  A row that sees no key
+ * gets zeros and the log-sum-exp -infinity; rows of no sequence are left as
+ * they are. */
+typedef struct aio_seqs {
+  int32_t n_seqs;
+  int32_t n_rows;            /* rows of q and out (of k and v rows to append) */
+  int32_t max_len;           /* no sequence has more keys                     */
+  const int32_t* cu_q_dev;   /* [n_seqs + 1], ascending from 0, or NULL       */
+  const int32_t* lens_dev;   /* pages: [n_seqs] keys, the new rows among them */
+  const int32_t* table_dev;  /* pages: [n_seqs][table_stride] page ids        */
+  int32_t table_stride;
+  const int32_t* cu_k_dev;   /* packed: [n_seqs + 1], ascending from 0        */
+} aio_seqs;
+
+/* Queries and outputs of an attention: [n_rows][n_heads][head_dim], fp32 or
+ * bf16 (both the same), rows q_stride and out_stride elements apart (whole
+ * numbers of 16 bytes).  fp32 queries keep fp32 accuracy throughout (exact
+ * splits into three bf16 terms, of the queries and of the softmax weights);
+ * with bf16 ones the softmax weights are rounded to bf16 too.  Sums and
+ * softmax statistics are fp32 in both.  Query head h reads kv head
+ * h / (n_heads / n_kv_heads). */
+typedef struct aio_attn {
+  const void* q_dev;
+  void* out_dev;
+  float* lse_dev;     /* fp32 [n_rows][n_heads], natural log, or NULL        */
+  int64_t q_stride;
+  int64_t out_stride;
+  int32_t dtype;      /* AIO_F32 or AIO_BF16                                 */
+  int32_t n_heads;    /* a multiple of n_kv_heads, at most 16 times as many  */
+  float scale;        /* of the scores, > 0 (1 / sqrt(head_dim))             */
+} aio_attn;
+
+/* Bytes of workspace that an attention over these sequences takes (0: none;
+ * its ws_dev may then be NULL): the partial results of a split over the keys.
+ * Pure host, reads only the sizes and whether cu_q_dev and cu_k_dev are
+ * NULL.  What the workspace holds does not matter, before or after; calls
+ * that may overlap need one each.  Returns 0 for bad sizes, too. */
+size_t aio_attn_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
+                                int32_t head_dim);
+
+/* Attention over paged keys and values: of one new token per sequence
+ * (cu_q_dev NULL), the decode step of several requests, or of the rows of
+ * several prompts, each behind what its pages hold already (a cached template,
+ * an earlier turn).  The rows' own keys have to be in the pages
+ * (aio_page_append).  An idle place in a padded batch has lens 0.
+ * AIO_EINVAL: a null or misaligned pointer or stride, a bad shape or type, a
+ * scale that is not positive and finite, or a workspace smaller than
+ * aio_attn_workspace_bytes says.  AIO_ERANGE: negative counts, cu_q_dev NULL with n_rows !=
+ * n_seqs, or more work than one launch covers.  AIO_EUNSUPPORTED: a page
+ * size, head dimension or number of heads per kv head not listed above. */
+int aio_paged_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_attn* a,
+                        void* ws_dev, size_t ws_bytes, void* hip_stream);
+
+/* Causal attention over the rows of several prompts whose keys and values are
+ * packed behind one another (cu_q_dev and cu_k_dev; lens and table are not
+ * read).  A sequence may have more keys than rows (its rows are the last
+ * ones); rows before its first key see nothing.  Errors as
+ * aio_paged_attention. */
+int aio_packed_attention(const aio_packed_kv* kv, const aio_seqs* s, const aio_attn* a,
+                         void* ws_dev, size_t ws_bytes, void* hip_stream);
+
+/* Writes the new rows' keys and values (fp32 or bf16, [n_rows][n_kv_heads]
+ * [head_dim], rows row_stride and heads head_stride elements apart, both whole
+ * numbers of 16 bytes) into their pages: row r of sequence i's q rows is key lens[i] - q + r.
+ * fp32 is rounded to the nearest bf16, ties to even, as everywhere in a cache.
+ * A row that falls before key 0, past max_len or the table's width, or into a hole
+ * is not written.  Two sequences of one call must not write the same slot
+ * (aio_pages_extend sees to that).  Errors as aio_paged_attention. */
+int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_rows_dev,
+                    const void* v_rows_dev, int32_t dtype, int64_t row_stride,
+                    int64_t head_stride, void* hip_stream);
+
+/* Copies pages in every plane of a pool (a plane: K or V of one layer):
+ * page_bytes bytes from page src[i] to page dst[i] of each of n_planes planes,
+ * which are plane_bytes apart, pages page_stride_bytes apart (all three whole
+ * numbers of 16, page_stride_bytes >= page_bytes).  src and dst are host
+ * arrays of n entries, read before the call returns.  AIO_ERANGE: n < 0,
+ * n_planes < 1 or a page id outside [0, n_pages).  AIO_EINVAL: a page that is
+ * the destination of two copies or both source and destination (the copies
+ * run at once, so their order would matter), or a null or misaligned
+ * argument. */
+int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t n_pages,
+                  int64_t page_stride_bytes, int64_t page_bytes, const int32_t* src,
+                  const int32_t* dst, int32_t n, void* hip_stream);
+
+/* Log probabilities of logit rows ([rows][n], fp32 or bf16, rows `stride`
+ * elements apart, 4- or 2-byte aligned): logprob[r] = x[target[r]] - log sum_j
+ * e^x[j], entropy[r] the Shannon entropy in nats of the row's softmax, and the
+ * `top` largest logits' indices and log probabilities, largest first, the
+ * lower index first among equals; NaN ranks above +Inf, as in aio_argmax.
+ * Scores the tokens of a prompt, a verify forward's drafts, or an answer.
+ * targets_dev (int32 [rows]) may be NULL with logprob_dev; a target outside
+ * [0, n) has none, and its logprob is NaN.  entropy_dev may be NULL;
+ * top_ids_dev (int32 [rows][top]) and top_logprobs_dev (fp32 [rows][top]) may
+ * be NULL where top is 0.  -Inf logits (forbidden tokens) have probability 0;
+ * a row of nothing else, or one with a NaN or +Inf, gives NaN.  ws_dev: see
+ * aio_logprobs_workspace_bytes.  AIO_ERANGE: rows < 0, n outside [1, 2^30],
+ * stride < n or top outside [0, min(n, AIO_MAX_TOP)]; AIO_EINVAL: null or
+ * misaligned pointers, a bad type or too small a workspace. */
+#define AIO_MAX_TOP 32
+int aio_logprobs(const void* logits_dev, int32_t dtype, int32_t rows, int32_t n, int64_t stride,
+                 const int32_t* targets_dev, int32_t top, float* logprob_dev, float* entropy_dev,
+                 int32_t* top_ids_dev, float* top_logprobs_dev, void* ws_dev, size_t ws_bytes,
+                 void* hip_stream);
+
+/* Bytes of workspace aio_logprobs takes (0: none), as
+ * aio_attn_workspace_bytes. */
+size_t aio_logprobs_workspace_bytes(int32_t rows, int32_t n, int32_t top);
+
+/* ----------------------------------------------- page tables (pure host) */
+
+/* Which pages of a pool each sequence holds.  Pages are counted per sequence
+ * that holds them: a fork shares its parent's, and the first to write into a
+ * shared, partly filled page gets a copy of it.  A handle is not thread-safe
+ * and makes no device call: the caller enqueues the copies that it is told
+ * (aio_page_copy), before anything that writes to the pool afterwards. */
+typedef struct aio_pages aio_pages;
+
+/* AIO_ERANGE: n_pages or max_seqs outside [1, 2^30] or a page size that
+ * aio_paged_kv does not take. */
+int aio_pages_create(int32_t n_pages, int32_t page_size, int32_t max_seqs, aio_pages** out);
+void aio_pages_destroy(aio_pages* p);
+
+/* A new, empty sequence; *seq receives its number, the lowest that is not in
+ * use.  AIO_ENOMEM: max_seqs are open. */
+int aio_pages_open(aio_pages* p, int32_t* seq);
+/* Drops the sequence; pages that no other one holds are free again. */
+int aio_pages_close(aio_pages* p, int32_t seq);
+/* A new sequence of the same contents, which holds the same pages. */
+int aio_pages_fork(aio_pages* p, int32_t seq, int32_t* child);
+/* Room for n more positions.  *n_copies (0 or 1) receives how many pages have
+ * to be copied first, *src and *dst which.  AIO_ENOMEM: too few free pages
+ * (nothing has changed then); AIO_ERANGE: n < 0 or over 2^30 positions. */
+int aio_pages_extend(aio_pages* p, int32_t seq, int32_t n, int32_t* src, int32_t* dst,
+                     int32_t* n_copies);
+/* Keeps the first len positions (after rejected drafts, say). */
+int aio_pages_truncate(aio_pages* p, int32_t seq, int32_t len);
+/* Moves the pages in use to the front of the pool: src and dst (room for
+ * `room` entries each) receive the *n copies to enqueue, at once, before any
+ * other use of the pool.  AIO_ERANGE: room is too small (nothing has changed;
+ * *n says how many are needed). */
+int aio_pages_compact(aio_pages* p, int32_t* src, int32_t* dst, int32_t room, int32_t* n);
+/* The sequence's length and its row of a page table: `width` ids, -1 behind
+ * the last.  row may be NULL.  AIO_ERANGE: width is too small. */
+int aio_pages_row(const aio_pages* p, int32_t seq, int32_t* row, int32_t width, int32_t* len);
+/* Pages that no sequence holds (AIO_EINVAL: null). */
+int aio_pages_free(const aio_pages* p);
+
 #ifdef __cplusplus
 }
 #endif

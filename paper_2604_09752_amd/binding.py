@@ -19,6 +19,8 @@ AIO_OK, AIO_EINVAL, AIO_ERANGE, AIO_EUNSUPPORTED, AIO_EHIP, AIO_ENOMEM, AIO_EDEV
     0, -1, -2, -3, -4, -5, -6
 AIO_WFMT_BF16, AIO_WFMT_INT8 = 0, 1
 AIO_MAX_VERIFY_ROWS = 10
+AIO_F32, AIO_BF16 = 0, 1
+AIO_MAX_TOP = 32
 LINEARS = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
 SCALES = ("sq", "sk", "sv", "so", "s_gate", "s_up", "s_down")
 
@@ -48,6 +50,32 @@ class aio_pld_stats(ctypes.Structure):
 class aio_spec_stats(ctypes.Structure):
     _fields_ = [("rounds", ctypes.c_int32), ("drafted", ctypes.c_int32),
                 ("accepted", ctypes.c_int32), ("draft_steps", ctypes.c_int32)]
+
+
+class aio_paged_kv(ctypes.Structure):
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim")]
+
+
+class aio_packed_kv(ctypes.Structure):
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("n_rows", "n_kv_heads", "head_dim")]
+
+
+class aio_seqs(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("cu_q_dev", ctypes.c_void_p),
+                ("lens_dev", ctypes.c_void_p), ("table_dev", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int32), ("cu_k_dev", ctypes.c_void_p)]
+
+
+class aio_attn(ctypes.Structure):
+    _fields_ = [("q_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
+                ("lse_dev", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class AioError(RuntimeError):
@@ -105,6 +133,27 @@ def lib():
                                       P(ctypes.c_float), P(i32)]
         L.aio_spec_generate.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp,
                                         P(aio_spec_stats)]
+        i64, sz = ctypes.c_int64, ctypes.c_size_t
+        L.aio_attn_workspace_bytes.argtypes = [P(aio_seqs), i32, i32, i32]
+        L.aio_attn_workspace_bytes.restype = sz
+        L.aio_paged_attention.argtypes = [P(aio_paged_kv), P(aio_seqs), P(aio_attn), vp, sz, vp]
+        L.aio_packed_attention.argtypes = [P(aio_packed_kv), P(aio_seqs), P(aio_attn), vp, sz, vp]
+        L.aio_page_append.argtypes = [P(aio_paged_kv), P(aio_seqs), vp, vp, i32, i64, i64, vp]
+        L.aio_page_copy.argtypes = [vp, i32, i64, i32, i64, i64, vp, vp, i32, vp]
+        L.aio_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.aio_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
+        L.aio_logprobs_workspace_bytes.restype = sz
+        L.aio_pages_create.argtypes = [i32, i32, i32, P(vp)]
+        L.aio_pages_destroy.argtypes = [vp]
+        L.aio_pages_destroy.restype = None
+        L.aio_pages_open.argtypes = [vp, P(i32)]
+        L.aio_pages_close.argtypes = [vp, i32]
+        L.aio_pages_fork.argtypes = [vp, i32, P(i32)]
+        L.aio_pages_extend.argtypes = [vp, i32, i32, P(i32), P(i32), P(i32)]
+        L.aio_pages_truncate.argtypes = [vp, i32, i32]
+        L.aio_pages_compact.argtypes = [vp, vp, vp, i32, P(i32)]
+        L.aio_pages_row.argtypes = [vp, i32, vp, i32, P(i32)]
+        L.aio_pages_free.argtypes = [vp]
         _lib = L
     return _lib
 
@@ -317,6 +366,301 @@ def aio_device_status(handle: int) -> int:
 
 def aio_uses_step_kernel(handle: int) -> bool:
     return bool(lib().aio_uses_step_kernel(handle))
+
+
+# ------------------------------------------------- several sequences in one pool
+#
+# The operators below run on the current stream of their tensors' device, like
+# torch's own; a tensor made or used on another stream has to be ordered with
+# it by the caller, as torch asks.
+
+_DTYPES = {torch.float32: AIO_F32, torch.bfloat16: AIO_BF16}
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(t: torch.Tensor, *others) -> None:
+    _need(t.is_cuda, "a device tensor is needed")
+    for o in others:
+        _need(o is None or o.device == t.device, "tensors on different devices")
+
+
+class _Call:
+    """The tensor's device made current for a call, and its current stream."""
+
+    def __init__(self, t: torch.Tensor):
+        self.index = t.device.index
+
+    def __enter__(self):
+        self.old = torch.cuda.current_device()
+        if self.old != self.index:
+            torch.cuda.set_device(self.index)
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.old != self.index:
+            torch.cuda.set_device(self.old)
+
+
+def _i32(t: torch.Tensor, dim: int, what: str) -> None:
+    _need(t.dtype == torch.int32 and t.dim() == dim and (t.numel() == 0 or t.stride(-1) == 1),
+          what + ": an int32 tensor with %d dimension(s) is needed" % dim)
+
+
+def _rows3(t: torch.Tensor, what: str) -> int:
+    """[rows][heads][head_dim] with the last two dimensions contiguous; its row stride."""
+    _need(t.dim() == 3 and t.dtype in _DTYPES, what + ": fp32 or bf16 [rows, heads, head_dim]")
+    n, h, d = t.shape
+    _need(t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)),
+          what + ": heads and dimensions have to be contiguous")
+    return t.stride(0) if n > 1 else h * d
+
+
+def _paged(k: torch.Tensor, v: torch.Tensor) -> aio_paged_kv:
+    _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype == torch.bfloat16,
+          "pages: two bf16 [n_pages, kv_heads, page_size, head_dim]")
+    _need(k.stride() == v.stride() and k.stride(3) == 1 and k.stride(2) == k.shape[3],
+          "pages: K and V of the same strides, slots and dimensions contiguous")
+    return aio_paged_kv(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0],
+                        k.shape[2], k.shape[1], k.shape[3])
+
+
+def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_seqs:
+    _i32(lens, 1, "lens")
+    _i32(table, 2, "table")
+    n = lens.shape[0]
+    _need(table.shape[0] == n, "lens and table are of different batches")
+    if cu_q is not None:
+        _i32(cu_q, 1, "cu_q")
+        _need(cu_q.shape[0] == n + 1, "cu_q: one more entry than sequences")
+    if max_len is None:
+        max_len = table.shape[1] * page_size
+    return aio_seqs(n, n_rows, min(int(max_len), 0x7fffffff), _ptr(cu_q), lens.data_ptr(),
+                    table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], None)
+
+
+def _attn(q, out, lse, scale) -> aio_attn:
+    sq, so = _rows3(q, "q"), _rows3(out, "out")
+    _need(q.shape == out.shape and q.dtype == out.dtype, "q and out differ in shape or type")
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous(),
+              "lse: contiguous fp32 [rows, heads]")
+    return aio_attn(q.data_ptr(), out.data_ptr(), _ptr(lse), sq, so, _DTYPES[q.dtype], q.shape[1],
+                    q.shape[2] ** -0.5 if scale is None else float(scale))
+
+
+def _workspace(nbytes: int, ws, like: torch.Tensor):
+    if nbytes == 0:
+        return None
+    if ws is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    _need(ws.is_contiguous() and ws.numel() * ws.element_size() >= nbytes,
+          "the workspace is smaller than %d bytes" % nbytes)
+    return ws
+
+
+def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: int,
+                             n_kv_heads: int, head_dim: int, prompts: bool = False) -> int:
+    """Workspace of an attention over n_seqs sequences with n_rows rows (prompts:
+    several rows per sequence, i.e. a call with cu_q)."""
+    s = aio_seqs(n_seqs, n_rows, max_len, 16 if prompts else None, None, None, 0, None)
+    return int(lib().aio_attn_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
+
+
+def _attend(name, kv, s, a, q, n_kv_heads, ws):
+    L = lib()
+    n = L.aio_attn_workspace_bytes(ctypes.byref(s), a.n_heads, n_kv_heads, q.shape[2])
+    with _Call(q) as stream:
+        w = _workspace(n, ws, q)
+        _check(getattr(L, name)(ctypes.byref(kv), ctypes.byref(s), ctypes.byref(a), _ptr(w), n,
+                                stream), name)
+
+
+def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
+                        table: torch.Tensor, out: torch.Tensor, cu_q: torch.Tensor | None = None,
+                        lse: torch.Tensor | None = None, scale: float | None = None,
+                        max_len: int | None = None, ws: torch.Tensor | None = None) -> None:
+    """Attention of q [rows, heads, head_dim] (fp32 or bf16) over the pages k, v
+    (bf16 [n_pages, kv_heads, page_size, head_dim]) of the sequences with lens
+    keys and table pages: one row per sequence, or with cu_q the rows of
+    prompts, causal.  max_len: no sequence is longer (default: the table's
+    width; a closer one gives a better split of the work)."""
+    _on_device(q, k, v, lens, table, out, cu_q, lse, ws)
+    kv, a = _paged(k, v), _attn(q, out, lse, scale)
+    _need(q.shape[2] == k.shape[3], "q and k differ in head_dim")
+    s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, k.shape[2])
+    _attend("aio_paged_attention", kv, s, a, q, k.shape[1], ws)
+
+
+def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
+                         cu_k: torch.Tensor, out: torch.Tensor, lse: torch.Tensor | None = None,
+                         scale: float | None = None, max_len: int | None = None,
+                         ws: torch.Tensor | None = None) -> None:
+    """Causal attention of the packed rows q over packed keys and values k, v
+    (bf16 [keys, kv_heads, head_dim]); cu_q and cu_k give each sequence's first
+    row and key."""
+    _on_device(q, k, v, cu_q, cu_k, out, lse, ws)
+    a = _attn(q, out, lse, scale)
+    _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype == torch.bfloat16 and
+          k.shape[2] == q.shape[2], "k, v: two bf16 [keys, kv_heads, head_dim]")
+    _need(k.stride() == v.stride() and (k.numel() == 0 or k.stride(2) == 1),
+          "k, v: the same strides, dimensions contiguous")
+    for t, what in ((cu_q, "cu_q"), (cu_k, "cu_k")):
+        _i32(t, 1, what)
+    _need(cu_q.shape == cu_k.shape and cu_q.shape[0] >= 1, "cu_q and cu_k differ in length")
+    kv = aio_packed_kv(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0],
+                       k.shape[1], k.shape[2])
+    s = aio_seqs(cu_q.shape[0] - 1, q.shape[0], k.shape[0] if max_len is None else int(max_len),
+                 cu_q.data_ptr(), None, None, 0, cu_k.data_ptr())
+    _attend("aio_packed_attention", kv, s, a, q, k.shape[1], ws)
+
+
+def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                    lens: torch.Tensor, table: torch.Tensor, cu_q: torch.Tensor | None = None,
+                    max_len: int | None = None) -> None:
+    """Write the new rows' keys and values ([rows, kv_heads, head_dim], fp32 or
+    bf16) into their pages; lens counts them already."""
+    _on_device(k_rows, v_rows, k, v, lens, table, cu_q)
+    kv = _paged(k, v)
+    _need(k_rows.dim() == 3 and k_rows.shape == v_rows.shape and k_rows.dtype == v_rows.dtype and
+          k_rows.dtype in _DTYPES and k_rows.shape[1] == k.shape[1] and
+          k_rows.shape[2] == k.shape[3], "rows: two fp32 or bf16 [rows, kv_heads, head_dim]")
+    _need(k_rows.stride() == v_rows.stride() and (k_rows.numel() == 0 or k_rows.stride(2) == 1),
+          "rows: the same strides, dimensions contiguous")
+    s = _paged_seqs(lens, table, cu_q, k_rows.shape[0], max_len, k.shape[2])
+    with _Call(k) as stream:
+        _check(lib().aio_page_append(ctypes.byref(kv), ctypes.byref(s), k_rows.data_ptr(),
+                                     v_rows.data_ptr(), _DTYPES[k_rows.dtype], k_rows.stride(0),
+                                     k_rows.stride(1), stream), "aio_page_append")
+
+
+def aio_page_copy(pool: torch.Tensor, src, dst) -> None:
+    """Copy pages src[i] to dst[i] (host int32 arrays) in every plane of the pool
+    [planes, n_pages, ...], whose pages are contiguous."""
+    _on_device(pool)
+    _need(pool.dim() >= 3 and pool[0, 0].is_contiguous(),
+          "pool: [planes, n_pages, ...] with contiguous pages")
+    a, b = np.ascontiguousarray(src, dtype=np.int32), np.ascontiguousarray(dst, dtype=np.int32)
+    _need(a.ndim == 1 and a.shape == b.shape, "src and dst differ in length")
+    size = pool.element_size()
+    page = pool.stride(1) if pool.shape[1] > 1 else pool[0, 0].numel()
+    with _Call(pool) as stream:
+        _check(lib().aio_page_copy(pool.data_ptr(), pool.shape[0], pool.stride(0) * size,
+                                   pool.shape[1], page * size, pool[0, 0].numel() * size,
+                                   a.ctypes.data, b.ctypes.data, a.size, stream),
+               "aio_page_copy")
+
+
+def aio_logprobs_workspace_bytes(rows: int, n: int, top: int) -> int:
+    return int(lib().aio_logprobs_workspace_bytes(rows, n, top))
+
+
+def aio_logprobs(logits: torch.Tensor, targets: torch.Tensor | None,
+                 logprob: torch.Tensor | None, entropy: torch.Tensor | None,
+                 top_ids: torch.Tensor | None = None, top_logprobs: torch.Tensor | None = None,
+                 ws: torch.Tensor | None = None) -> None:
+    """Log probabilities of the targets, entropies and the top alternatives of
+    logits [rows, n] (fp32 or bf16); each output may be None."""
+    _on_device(logits, targets, logprob, entropy, top_ids, top_logprobs, ws)
+    _need(logits.dim() == 2 and logits.dtype in _DTYPES and
+          (logits.numel() == 0 or logits.shape[1] == 1 or logits.stride(1) == 1),
+          "logits: fp32 or bf16 [rows, n]")
+    rows, n = logits.shape
+    if targets is not None:
+        _i32(targets, 1, "targets")
+    for t in (targets, logprob, entropy):
+        _need(t is None or (t.shape == (rows,) and t.is_contiguous()), "one value per row")
+    for t in (logprob, entropy, top_logprobs):
+        _need(t is None or t.dtype == torch.float32, "fp32 outputs")
+    _need((top_ids is None) == (top_logprobs is None), "top_ids and top_logprobs go together")
+    top = 0
+    if top_ids is not None:
+        _i32(top_ids, 2, "top_ids")
+        _need(top_ids.shape == top_logprobs.shape and top_ids.shape[0] == rows and
+              top_ids.is_contiguous() and top_logprobs.is_contiguous(),
+              "top_ids, top_logprobs: contiguous [rows, top]")
+        top = top_ids.shape[1]
+    L = lib()
+    need = L.aio_logprobs_workspace_bytes(rows, n, top)
+    with _Call(logits) as stream:
+        w = _workspace(need, ws, logits)
+        _check(L.aio_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], rows, n,
+                              logits.stride(0) if rows > 1 else n, _ptr(targets), top,
+                              _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
+                              _ptr(w), need, stream), "aio_logprobs")
+
+
+class Pages:
+    """Which pages of a pool each sequence holds (host bookkeeping: aio_pages_*).
+    ``extend`` and ``compact`` return the copies (src, dst) to enqueue."""
+
+    def __init__(self, n_pages: int, page_size: int, max_seqs: int):
+        h = ctypes.c_void_p()
+        _check(lib().aio_pages_create(n_pages, page_size, max_seqs, ctypes.byref(h)),
+               "aio_pages_create")
+        self.handle, self.n_pages, self.page_size = h.value, n_pages, page_size
+
+    def open(self) -> int:
+        s = ctypes.c_int32(-1)
+        _check(lib().aio_pages_open(self.handle, ctypes.byref(s)), "aio_pages_open")
+        return s.value
+
+    def close(self, seq: int) -> None:
+        _check(lib().aio_pages_close(self.handle, seq), "aio_pages_close")
+
+    def fork(self, seq: int) -> int:
+        s = ctypes.c_int32(-1)
+        _check(lib().aio_pages_fork(self.handle, seq, ctypes.byref(s)), "aio_pages_fork")
+        return s.value
+
+    def extend(self, seq: int, n: int):
+        a, b, c = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int32(0)
+        _check(lib().aio_pages_extend(self.handle, seq, n, ctypes.byref(a), ctypes.byref(b),
+                                      ctypes.byref(c)), "aio_pages_extend")
+        return ([a.value], [b.value]) if c.value else ([], [])
+
+    def truncate(self, seq: int, length: int) -> None:
+        _check(lib().aio_pages_truncate(self.handle, seq, length), "aio_pages_truncate")
+
+    def compact(self):
+        a, b = np.empty(self.n_pages, np.int32), np.empty(self.n_pages, np.int32)
+        n = ctypes.c_int32(0)
+        _check(lib().aio_pages_compact(self.handle, a.ctypes.data, b.ctypes.data, self.n_pages,
+                                       ctypes.byref(n)), "aio_pages_compact")
+        return a[: n.value].copy(), b[: n.value].copy()
+
+    def length(self, seq: int) -> int:
+        n = ctypes.c_int32(0)
+        _check(lib().aio_pages_row(self.handle, seq, None, 0, ctypes.byref(n)), "aio_pages_row")
+        return n.value
+
+    def rows(self, seqs, width: int):
+        """(lens [n], table [n, width]) of the sequences, host int32."""
+        lens, table = np.zeros(len(seqs), np.int32), np.full((len(seqs), width), -1, np.int32)
+        n = ctypes.c_int32(0)
+        for i, s in enumerate(seqs):
+            _check(lib().aio_pages_row(self.handle, s, table[i].ctypes.data, width,
+                                       ctypes.byref(n)), "aio_pages_row")
+            lens[i] = n.value
+        return lens, table
+
+    @property
+    def free(self) -> int:
+        return int(lib().aio_pages_free(self.handle))
+
+    def destroy(self) -> None:
+        if getattr(self, "handle", None):
+            lib().aio_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
 
 
 # ------------------------------------------------------------------ a model

@@ -72,6 +72,9 @@ constexpr int kVattnBlocksPerSplit = 8;
 
 WsLayout aio_ws_layout(const aio_config& c);
 
+// Notes the error for aio_last_hip_error; AIO_EHIP.
+int aio_hip_fail(hipError_t e);
+
 struct aio_model {
   aio_config cfg;
   std::vector<aio_layer_weights> layers;

@@ -42,10 +42,7 @@ hipError_t scratch_address(int dev, char** out) {
 
 thread_local int g_last_hip = 0;
 
-int hip_fail(hipError_t e) {
-  g_last_hip = (int)e;
-  return AIO_EHIP;
-}
+int hip_fail(hipError_t e) { return aio_hip_fail(e); }
 
 size_t align256(size_t v) { return (v + 255u) & ~(size_t)255u; }
 
@@ -78,6 +75,11 @@ int choose_splits(const aio_config& c) {
 }
 
 }  // namespace
+
+int aio_hip_fail(hipError_t e) {
+  g_last_hip = (int)e;
+  return AIO_EHIP;
+}
 
 WsLayout aio_ws_layout(const aio_config& c) {
   WsLayout L{};

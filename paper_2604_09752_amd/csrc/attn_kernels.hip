@@ -1,0 +1,694 @@
+// Attention over the keys of several sequences, in pages or packed: one new
+// token per sequence (k_attn_step) and the rows of prompts (k_attn_rows).
+//
+// For a row with scores s_j = scale q.k_j over its visible keys j, with the
+// running maximum m and sum l over the key blocks seen so far:
+//   m' = max(m, max_j s_j),  p_j = e^(s_j - m'),  c = e^(m - m'),
+//   l' = c l + sum_j p_j,    o' = c o + sum_j p_j v_j,    out = o / l.
+// Two such states join by the same rule, so the keys can be split over waves
+// and workgroups (k_attn_join).
+//
+// Both products run on MFMA with the keys (the value tile, transposed) as the
+// A operand: S^T = K Q^T, O^T += V^T P^T.  A column is a query, so a lane's
+// scores all belong to one query and the weights stay in registers: the k
+// slots of the second product are taken in the order in which the scores of the
+// first lie in a lane, and the value rows are read through transposing LDS
+// reads in that order.  fp32 queries and their softmax weights are split into
+// three bf16 terms each (truncation, exact), accumulated into one tile.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "paged.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 4;
+constexpr int kBlock = kWaves * AIO_WAVE;
+
+AIO_DEV bf16x8 as_bf16x8(u32x4 u) { return __builtin_bit_cast(bf16x8, u); }
+
+AIO_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+AIO_DEV f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Eight fp32 values as NT bf16 operands: one, rounded to nearest even, or
+// three that add up to the value exactly.
+template <int NT>
+AIO_DEV void terms(const float (&x)[8], bf16x8 (&t)[NT]) {
+  if constexpr (NT == 1) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[0][j] = (__bf16)x[j];
+  } else {
+    uint32_t w[3][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      w[0][j] = __float_as_uint(x[j]);
+      const float r1 = x[j] - __uint_as_float(w[0][j] & 0xffff0000u);
+      w[1][j] = __float_as_uint(r1);
+      w[2][j] = __float_as_uint(r1 - __uint_as_float(w[1][j] & 0xffff0000u));
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      u32x4 u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[j] = w[k][2 * j] >> 16 | (w[k][2 * j + 1] & 0xffff0000u);
+      t[k] = as_bf16x8(u);
+    }
+  }
+}
+
+// Eight elements of a query row.
+template <int NT>
+AIO_DEV void load_query(const AttnArgs& a, int row, int head, int hd, int d0, bool live,
+                        bf16x8 (&t)[NT]) {
+  const int64_t at = (int64_t)row * a.ldq + (int64_t)head * hd + d0;
+  if constexpr (NT == 1) {
+    u32x4 u = {0, 0, 0, 0};
+    if (live) u = *(const u32x4*)((const uint16_t*)a.q + at);
+    t[0] = as_bf16x8(u);
+  } else {
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (live) {
+      const float4 u = *(const float4*)((const float*)a.q + at);
+      const float4 v = *(const float4*)((const float*)a.q + at + 4);
+      x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+      x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+    }
+    terms<3>(x, t);
+  }
+}
+
+AIO_DEV void store_out(const AttnArgs& a, bool f32, int64_t at, float v) {
+  if (f32) ((float*)a.out)[at] = v;
+  else ((uint16_t*)a.out)[at] = f32_to_bf16(v);
+}
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ------------------------------------------------ one new token per sequence
+
+// Workgroup (sequence, kv head, split): the G query heads of the kv head are
+// columns of one 16-wide tile; each wave takes every fourth block of 32 keys of
+// the split, and the waves' states join in LDS.
+template <int HD>
+struct StepLds {
+  static constexpr int VROW = HD * 2 + 16;        // bytes of a value row
+  static constexpr int VBYTES = 32 * VROW;        // a wave's value tile
+  static constexpr int OROW = HD + 4;             // floats of an output row
+  static constexpr int OBYTES = kWaves * kMaxGroup * OROW * 4;
+  static constexpr int BYTES = kWaves * VBYTES > OBYTES ? kWaves * VBYTES : OBYTES;
+};
+
+template <int HD, int NT>
+__global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
+  using L = StepLds<HD>;
+  __shared__ __align__(16) char smem[L::BYTES];
+  __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
+  constexpr int NC = HD / 32;              // k chunks of a score product
+  constexpr int RPL = AIO_WAVE * 8 / HD;   // value rows per load
+  constexpr int NV = 32 / RPL;             // loads of a value tile
+  constexpr int ND = HD / 16;              // output tiles
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
+  const int col = lane & 15, grp = lane >> 4;
+  const int b = blockIdx.x, sh = udiv(b, a.by_s), split = b - sh * a.S;
+  const int seq = udiv(sh, a.by_hkv), kvh = sh - seq * a.kv.Hkv;
+  const int len = paged_len(a.kv, seq, a.max_len);
+  const int c0 = split * a.chunk, c1 = min(len, c0 + a.chunk);
+  const int h0 = kvh * a.G;
+  if (split > 0 && c0 >= len) {  // a split without keys
+    if (tid < a.G) a.part_ml[(((int64_t)split * a.n_rows + seq) * a.H + h0 + tid) * 2] = -INFINITY;
+    return;
+  }
+  bf16x8 q[NC][NT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    load_query<NT>(a, seq, h0 + col, HD, c * 32 + 8 * grp, col < a.G, q[c]);
+
+  const int32_t* table = a.kv.table + (int64_t)seq * a.kv.tstride;
+  const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
+  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride;
+  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride;
+  // Lane l holds the page of key l mod 32 of a block (-1: not visible).
+  auto load_page = [&](int t) {
+    const int key = c0 + t * 32 + (lane & 31);
+    int p = -1;
+    if (key < c1) p = table[key >> a.kv.shift];
+    return (unsigned)p < (unsigned)a.kv.limit ? p : -1;
+  };
+  // Keys as the A operand (key row col of 16, dims 32 c + 8 grp ..), values row
+  // by row.  The 8 keys of an aligned group share a page, so pages are wave
+  // uniform: a value load covers 4 or 8 keys, a key load two groups.  Keys that
+  // are not visible read page 0.
+  u32x4 kr[2][NC], vr[NV];
+  auto load_block = [&](int t, int page) {
+    const int j0 = c0 + t * 32;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const int64_t lo = max(__builtin_amdgcn_readlane(page, kt * 16), 0) * a.kv.stride;
+      const int64_t hi = max(__builtin_amdgcn_readlane(page, kt * 16 + 8), 0) * a.kv.stride;
+      const uint16_t* p =
+          kb + (col < 8 ? lo : hi) + (((j0 + kt * 16 + col) & pm) * HD + 8 * grp);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) kr[kt][c] = *(const u32x4*)(p + c * 32);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t pg = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride;
+      const int kk = i * RPL + lane / (HD / 8);
+      vr[i] = *(const u32x4*)(vb + pg + (((j0 + kk) & pm) * HD + lane % (HD / 8) * 8));
+    }
+  };
+  f32x4 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  char* vt = smem + wid * L::VBYTES;
+  const char* vtr = vt + (4 * grp + col / 4) * L::VROW + (col & 3) * 8;
+
+  int page = load_page(wid), next = load_page(wid + kWaves);
+  if (wid < nt) load_block(wid, page);
+  for (int t = wid; t < nt; t += kWaves) {
+    const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
+    // value rows -> LDS; what no row may see is zero there (0 x NaN is not)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int kk = i * RPL + lane / (HD / 8);
+      u32x4 w = vr[i];
+      if (vis != 0xffffffffu && !(vis >> kk & 1)) w = u32x4{0, 0, 0, 0};
+      *(u32x4*)(vt + kk * L::VROW + lane % (HD / 8) * 16) = w;
+    }
+    float p[8];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s = mfma16(as_bf16x8(kr[kt][c]), q[c][n], s);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) p[4 * kt + v] = s[v];
+    }
+    // the wave's next block (its last one is read again: no branch)
+    const bool more = t + kWaves < nt;
+    load_block(more ? t + kWaves : t, more ? next : page);
+    page = next;
+    next = load_page(t + 2 * kWaves);
+    if (vis != 0xffffffffu) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v)
+        if (!(vis >> (v / 4 * 16 + 4 * grp + v % 4) & 1)) p[v] = -INFINITY;
+    }
+    float mx = p[0];
+#pragma unroll
+    for (int v = 1; v < 8; ++v) mx = fmaxf(mx, p[v]);
+    float other = mx;
+    swap32(mx, other);
+    mx = fmaxf(mx, other);
+    other = mx;
+    swap16(mx, other);
+    mx = fmaxf(mx, other);
+    const float mnew = fmaxf(m, mx);
+    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+    if (__any(mnew > m)) {
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+      l *= c;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= c;
+    }
+    m = mnew;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+      p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], a.scale_log2, -mref));
+      l += p[v];
+    }
+    bf16x8 pt[NT];
+    terms<NT>(p, pt);
+    wave_lds_sync();  // the value tile is in LDS
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const uint2 v0 = lds_read_tr16(vtr + d * 32);
+      const uint2 v1 = lds_read_tr16(vtr + 16 * L::VROW + d * 32);
+      const bf16x8 av = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[d] = mfma16(av, pt[n], o[d]);
+    }
+    wave_lds_sync();  // every read of the tile is done before the next writes
+  }
+  l += __shfl_xor(l, 16, AIO_WAVE);
+  l += __shfl_xor(l, 32, AIO_WAVE);
+  if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
+
+  // join the waves
+  __syncthreads();
+  float* om = (float*)smem;  // [wave][column][OROW]
+  if (col < a.G) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+      *(f32x4*)(om + (wid * kMaxGroup + col) * L::OROW + d * 16 + 4 * grp) = o[d];
+    if (grp == 0) {
+      wm[wid][col] = m * a.scale_log2;
+      wl[wid][col] = l;
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < a.G * HD; e += kBlock) {
+    const int g = e / HD, d = e % HD;
+    float M = wm[0][g];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wm[w][g]);
+    float ls = 0.f, os = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float x = wm[w][g];
+      const float c = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M);
+      ls += c * wl[w][g];
+      os += c * om[(w * kMaxGroup + g) * L::OROW + d];
+    }
+    const int64_t rh = (int64_t)seq * a.H + h0 + g;
+    if (a.S == 1) {
+      const bool none = ls == 0.f;  // no visible key
+      store_out(a, NT == 3, (int64_t)seq * a.ldo + (int64_t)(h0 + g) * HD + d, none ? 0.f : os / ls);
+      if (d == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
+    } else {
+      const int64_t at = (int64_t)split * a.n_rows * a.H + rh;
+      a.part_o[at * HD + d] = os;
+      if (d == 0) {
+        a.part_ml[at * 2] = ls != ls ? ls : M;
+        a.part_ml[at * 2 + 1] = ls;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------- the rows of prompts
+
+// A sequence's rows and the G heads of a kv head form one list of q G packed
+// rows (row-major: packed row r G + g is row r of head h0 + g), cut into tiles of
+// kRows; workgroup (tile, kv head, split).  Each wave owns 32 packed rows (the columns of
+// 32-wide tiles) and all of them share the key and value tiles in LDS, kKeys keys
+// at a time, the next ones in flight in registers.
+constexpr int kRows = kWaves * 32;
+constexpr int kKeys = 64;
+
+template <int HD>
+struct RowsLds {
+  static constexpr int ROW = HD * 2 + 16;  // bytes of a key or value row
+  static constexpr int TILE = kKeys * ROW;
+};
+
+// Tile `t` of the launch: its sequence, the tile within it and how many the
+// sequence has; false behind the last.
+AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile, int& tiles) {
+  const int lane = threadIdx.x & (AIO_WAVE - 1);
+  for (int base = 0; base < a.n_seqs; base += AIO_WAVE) {
+    const int i = base + lane;
+    int n = 0;
+    if (i < a.n_seqs) {
+      int first, count;
+      seq_rows(a.cu_q, a.n_rows, i, first, count);
+      n = (int)(((int64_t)count * a.G + kRows - 1) / kRows);
+    }
+    int incl = n;
+#pragma unroll
+    for (int off = 1; off < AIO_WAVE; off <<= 1) {
+      const int o = __shfl_up(incl, off, AIO_WAVE);
+      if (lane >= off) incl += o;
+    }
+    const uint64_t past = __ballot(incl > t);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      seq = base + at;
+      tiles = __shfl(n, at, AIO_WAVE);
+      tile = t - (__shfl(incl, at, AIO_WAVE) - tiles);
+      return true;
+    }
+    t -= __shfl(incl, AIO_WAVE - 1, AIO_WAVE);
+  }
+  return false;
+}
+
+AIO_DEV bool not_finite(u32x4 w) {  // of eight bf16
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+
+template <int HD, int NT, bool PAGED>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
+  using L = RowsLds<HD>;
+  __shared__ __align__(16) char kt_s[L::TILE];
+  __shared__ __align__(16) char vt_s[L::TILE];
+  __shared__ uint8_t seen[kKeys];
+  __shared__ int flags[2];
+  constexpr int NC = HD / 16;                      // k chunks of a score product
+  constexpr int NHB = HD / 32;                     // output tiles
+  constexpr int TPR = HD / 8;                      // threads of a row
+  constexpr int RPP = kBlock / TPR;                // rows per pass
+  constexpr int NP = kKeys / RPP;                  // passes of a tile
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
+  const int rl = lane & 31, kh = lane >> 5;
+  // Tiles from the sequence's end (a causal tile's work grows with its position,
+  // and workgroups start in index order: the longest start first).
+  const int split = udiv(blockIdx.x, a.by_s);  // by_s: workgroups per split
+  const int lin = blockIdx.x - split * a.by_s.d;
+  const int tg = udiv(lin, a.by_hkv), kvh = lin - tg * a.kv.Hkv;
+  int seq, tile, tiles;
+  if (!find_tile(a, tg, seq, tile, tiles)) return;
+  tile = tiles - 1 - tile;
+  int first, count;
+  seq_rows(a.cu_q, a.n_rows, seq, first, count);
+  int len, key0 = 0;
+  if constexpr (PAGED) {
+    len = paged_len(a.kv, seq, a.max_len);
+  } else {
+    key0 = min(max(a.kv.cu_k[seq], 0), a.kv.limit);
+    len = min(max(min(a.kv.cu_k[seq + 1], a.kv.limit) - key0, 0), a.max_len);
+  }
+  const int packed = count * a.G, p0 = tile * kRows;
+  const int h0 = kvh * a.G;
+  // this lane's query
+  const int pr = p0 + wid * 32 + rl;
+  const bool live = pr < packed;
+  const int row = udiv(min(pr, packed - 1), a.by_g), g = min(pr, packed - 1) - row * a.G;
+  const int lim = len - count + row;  // its last visible key
+  // the last key that any row of the wave, of the workgroup sees, and the last
+  // that all rows of the workgroup see
+  const int wave_lim = len - count + udiv(min(p0 + wid * 32 + 31, packed - 1), a.by_g);
+  const int wg_lim = len - count + udiv(min(p0 + kRows, packed) - 1, a.by_g);
+  const int all_lim = len - count + udiv(p0, a.by_g);
+  const int nkt = wg_lim < 0 ? 0 : wg_lim / kKeys + 1;
+  // this split's key tiles
+  const int each = nkt / a.S, rest = nkt - each * a.S;
+  const int t0 = split * each + min(split, rest), t1 = t0 + each + (split < rest ? 1 : 0);
+
+  bf16x8 q[NC][NT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    load_query<NT>(a, first + row, h0 + g, HD, c * 16 + 8 * kh, live, q[c]);
+
+  // staging: pass p of this thread is row p RPP + tid / TPR, 8 dims
+  const int sr = tid / TPR, sd = tid % TPR * 8;
+  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride + sd;
+  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride + sd;
+  const int32_t* table = PAGED ? a.kv.table + (int64_t)seq * a.kv.tstride : nullptr;
+  int page[NP];
+  u32x4 kr[NP], vr[NP];
+  uint32_t ok = 0;  // bit p: the row of pass p is there
+  auto load_pages = [&](int t) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int key = t * kKeys + p * RPP + sr;
+        page[p] = key < len && t < t1 ? table[key >> a.kv.shift] : -1;
+      }
+    }
+  };
+  auto load_tile = [&](int t) {
+    ok = 0;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int key = t * kKeys + p * RPP + sr;
+      bool there = key < len;
+      int64_t at;
+      if constexpr (PAGED) {
+        there = (unsigned)page[p] < (unsigned)a.kv.limit;
+        at = page[p] * a.kv.stride + (int64_t)(key & ((1 << a.kv.shift) - 1)) * HD;
+      } else {
+        at = (int64_t)(key0 + key) * a.kv.stride;
+      }
+      kr[p] = vr[p] = u32x4{0, 0, 0, 0};
+      if (there) {
+        kr[p] = *(const u32x4*)(kb + at);
+        vr[p] = *(const u32x4*)(vb + at);
+        ok |= 1u << p;
+      }
+    }
+  };
+  f32x16 o[NHB];
+#pragma unroll
+  for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[hb][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const char* vtr = vt_s + (4 * kh + (lane & 15) / 4) * L::ROW +
+                    ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+
+  if (tid < 2) flags[tid] = 0;
+  if (t0 < t1) {
+    load_pages(t0);
+    load_tile(t0);
+    load_pages(t0 + 1);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int j0 = t * kKeys;
+    __syncthreads();  // every wave is done with the tile before
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      *(u32x4*)(kt_s + (p * RPP + sr) * L::ROW + sd * 2) = kr[p];
+      *(u32x4*)(vt_s + (p * RPP + sr) * L::ROW + sd * 2) = vr[p];
+      if (sd == 0) seen[p * RPP + sr] = ok >> p & 1;
+    }
+    // 1: keys are missing; 2: values that are not finite where some rows may not see
+    // them (they must not meet a weight of 0 in a product)
+    int f = ok != (1u << NP) - 1 ? 1 : 0;
+    if (j0 + kKeys - 1 > all_lim) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) f |= not_finite(vr[p]) ? 2 : 0;
+    }
+    if (f) atomicOr(&flags[t & 1], f);
+    __syncthreads();
+    const int flag = __builtin_amdgcn_readfirstlane(flags[t & 1]);
+    if (tid == 0) flags[~t & 1] = 0;
+    if (t + 1 < t1) {
+      load_tile(t + 1);
+      load_pages(t + 2);
+    }
+    if (j0 > wave_lim) continue;
+
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 ak =
+            as_bf16x8(*(const u32x4*)(kt_s + (b * 32 + rl) * L::ROW + (c * 16 + 8 * kh) * 2));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
+      }
+    }
+    // key of score v of block b: j0 + 32 b + 8 (v / 4) + 4 kh + v mod 4
+    if (j0 + kKeys - 1 > all_lim || flag) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
+          if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[b][v]);
+    float other = mx;
+    swap32(mx, other);
+    mx = fmaxf(mx, other);
+    const float mnew = fmaxf(m, mx);
+    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+    if (__any(mnew > m)) {
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+      l *= c;
+#pragma unroll
+      for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[hb][i] *= c;
+    }
+    m = mnew;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[b][v] = __builtin_amdgcn_exp2f(fmaf(s[b][v], a.scale_log2, -mref));
+        l += s[b][v];
+      }
+    if (flag & 2) {
+      // one key at a time, for the rows that see it
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            const int kk = 32 * b + 8 * (v / 4) + 4 * half + v % 4;
+            const float w = __shfl(s[b][v], rl + 32 * half, AIO_WAVE);
+            if (j0 + kk > lim || !seen[kk]) continue;
+#pragma unroll
+            for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int d = hb * 32 + 8 * (i / 4) + 4 * kh + i % 4;
+                o[hb][i] += w * bf16_to_f32(*(const uint16_t*)(vt_s + kk * L::ROW + d * 2));
+              }
+          }
+      continue;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = s[c / 2][8 * (c & 1) + e];
+      bf16x8 pt[NT];
+      terms<NT>(p, pt);
+#pragma unroll
+      for (int hb = 0; hb < NHB; ++hb) {
+        const uint2 v0 = lds_read_tr16(vtr + 16 * c * L::ROW + hb * 64);
+        const uint2 v1 = lds_read_tr16(vtr + (16 * c + 8) * L::ROW + hb * 64);
+        const bf16x8 av = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[hb] = mfma32(av, pt[n], o[hb]);
+      }
+    }
+  }
+  if (!live) return;
+  l += __shfl_xor(l, 32, AIO_WAVE);
+  if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
+  const int64_t rh = (int64_t)(first + row) * a.H + h0 + g;
+  if (a.S > 1) {
+    const int64_t at = (int64_t)split * a.n_rows * a.H + rh;
+    if (kh == 0) {
+      a.part_ml[at * 2] = m * a.scale_log2;
+      a.part_ml[at * 2 + 1] = l;
+    }
+    if (m == -INFINITY) return;
+#pragma unroll
+    for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(a.part_o + at * HD + hb * 32 + 8 * i + 4 * kh) =
+            f32x4{o[hb][4 * i], o[hb][4 * i + 1], o[hb][4 * i + 2], o[hb][4 * i + 3]};
+    return;
+  }
+  const bool none = l == 0.f;  // no visible key
+  const float inv = none ? 0.f : 1.f / l;
+  if (kh == 0 && a.lse) a.lse[rh] = none ? -INFINITY : m * a.scale_log2 * kLn2 + logf(l);
+  const int64_t to = (int64_t)(first + row) * a.ldo + (int64_t)(h0 + g) * HD + 4 * kh;
+#pragma unroll
+  for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = {o[hb][4 * i] * inv, o[hb][4 * i + 1] * inv, o[hb][4 * i + 2] * inv,
+                       o[hb][4 * i + 3] * inv};
+      const int64_t at = to + hb * 32 + 8 * i;
+      if constexpr (NT == 3) {
+        *(f32x4*)((float*)a.out + at) = v;
+      } else {
+        const uint2 w = {f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16,
+                         f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
+        *(uint2*)((uint16_t*)a.out + at) = w;
+      }
+    }
+}
+
+// Joins the splits of a row and head: one wave each.
+template <int HD, bool F32>
+__global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
+  const int lane = threadIdx.x & (AIO_WAVE - 1);
+  const int64_t rh = (int64_t)blockIdx.x * kWaves + threadIdx.x / AIO_WAVE;
+  const int64_t all = (int64_t)a.n_rows * a.H;
+  if (rh >= all) return;
+  const int row = (int)(rh / a.H), head = (int)(rh - (int64_t)row * a.H);
+  // rows of no sequence are left alone
+  if (a.cu_q && (row < a.cu_q[0] || row >= a.cu_q[a.n_seqs])) return;
+  float M = -INFINITY;
+  for (int s = lane; s < a.S; s += AIO_WAVE) M = fmaxf(M, a.part_ml[(s * all + rh) * 2]);
+  M = wave_max(M);
+  constexpr int PER = HD / AIO_WAVE;
+  float os[PER] = {}, ls = 0.f;
+  for (int s = 0; s < a.S; ++s) {
+    const int64_t at = s * all + rh;
+    const float x = a.part_ml[at * 2];
+    if (x == -INFINITY) continue;  // (its other values were not written)
+    const float c = __builtin_amdgcn_exp2f(x - M);
+    ls += c * a.part_ml[at * 2 + 1];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) os[i] += c * a.part_o[at * HD + i * AIO_WAVE + lane];
+  }
+  const bool none = ls == 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    store_out(a, F32, (int64_t)row * a.ldo + (int64_t)head * HD + i * AIO_WAVE + lane,
+              none ? 0.f : os[i] / ls);
+  if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
+}
+
+template <int HD, int NT>
+hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  if (!p.rows)
+    hipLaunchKernelGGL((k_attn_step<HD, NT>), dim3((unsigned)p.groups), dim3(kBlock), 0, stream, a);
+  else if (a.kv.table)
+    hipLaunchKernelGGL((k_attn_rows<HD, NT, true>), dim3((unsigned)p.groups), dim3(kBlock), 0,
+                       stream, a);
+  else
+    hipLaunchKernelGGL((k_attn_rows<HD, NT, false>), dim3((unsigned)p.groups), dim3(kBlock), 0,
+                       stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.S == 1) return e;
+  const int64_t rh = (int64_t)a.n_rows * a.H;
+  hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
+                     dim3(kBlock), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
+  *p = AttnPlan{};
+  if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0) return AIO_ERANGE;
+  if (Hkv < 1 || H < 1 || H % Hkv) return AIO_EINVAL;
+  if (H / Hkv > kMaxGroup || (hd != 64 && hd != 128)) return AIO_EUNSUPPORTED;
+  p->rows = s.cu_q_dev || s.cu_k_dev;
+  if (!p->rows && s.n_rows != s.n_seqs) return AIO_ERANGE;
+  const int64_t G = H / Hkv;
+  p->splits = 1;
+  if (!p->rows) {
+    // splits of at least 128 keys (a block of 32 per wave)
+    const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 127) / 128);
+    const int64_t base = std::max<int64_t>(1, (int64_t)s.n_seqs * Hkv);
+    const int64_t want = std::max<int64_t>(1, std::min(units, 4 * kCUs / base));
+    p->chunk = (int)((units + want - 1) / want * 128);
+    p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
+    p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
+  } else {
+    p->tiles = ((int64_t)s.n_rows * G) / kRows + s.n_seqs;
+    const int64_t base = std::max<int64_t>(1, p->tiles * Hkv);
+    const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 4 * kKeys - 1) / (4 * kKeys));
+    p->splits = (int)std::max<int64_t>(1, std::min(units, 2 * kCUs / base));
+    p->groups = p->tiles * Hkv * p->splits;
+  }
+  if (p->groups > 0x7fffffff || (int64_t)s.n_rows * H > 0x7fffffff) return AIO_ERANGE;
+  if (p->rows && (int64_t)s.n_rows * G > 0x7fffffff - kRows) return AIO_ERANGE;
+  if (p->splits > 1) p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
+  return AIO_OK;
+}
+
+hipError_t aio_launch_attention(const AttnArgs& a, const AttnPlan& p, int hd, int dtype,
+                                hipStream_t stream) {
+  if (hd == 128)
+    return dtype == AIO_F32 ? launch<128, 3>(a, p, stream) : launch<128, 1>(a, p, stream);
+  return dtype == AIO_F32 ? launch<64, 3>(a, p, stream) : launch<64, 1>(a, p, stream);
+}

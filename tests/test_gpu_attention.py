@@ -1,0 +1,397 @@
+"""Attention over paged and packed keys against a plain 64-bit evaluation: one
+new token per sequence and the rows of prompts, at the lengths, heads, pages,
+holes, strides and values where it can go wrong."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_09752_amd import binding as B
+from tests.paged_cases import PoolCase, attention64, check_attention, cu
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def rows(n, H, hd, dtype, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn((n, H, hd), generator=g).to(dtype)
+
+
+def run_step(case, q, lse=True, **kw):
+    k, v, lens, table = case.device()
+    qd = q.cuda()
+    out = torch.full_like(qd, float("nan"))
+    l = torch.full(q.shape[:2], float("nan"), device="cuda") if lse else None
+    B.aio_paged_attention(qd, k, v, lens, table, out, lse=l, **kw)
+    torch.cuda.synchronize()
+    return out, l
+
+
+LENS = [0, 1, 2, 31, 32, 33, 64, 127, 128, 129, 257, 500]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd,page", [
+    (4, 4, 64, 16), (16, 8, 128, 16), (6, 2, 64, 8), (8, 2, 128, 32), (16, 1, 64, 64),
+    (8, 1, 128, 256), (15, 3, 128, 128)])
+def test_step(H, Hkv, hd, page, dtype):
+    case = PoolCase(LENS, Hkv, hd, page, seed=H)
+    q = rows(len(LENS), H, hd, dtype)
+    ref = attention64(q, case.keys, case.values, [1] * len(LENS), LENS)
+    for max_len in (None, 500):
+        out, l = run_step(case, q, max_len=max_len)
+        check_attention(out, l, ref, "max_len %s" % max_len)
+    # the same without the log-sum-exp
+    again, _ = run_step(case, q, lse=False, max_len=500)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,length", [(1, 1), (1, 129), (1, 4096), (3, 2999), (2, 9001)])
+def test_step_split_over_the_keys(n, length, dtype):
+    lens = [length - 7 * i for i in range(n)]
+    lens[-1] = max(lens[-1], 1)
+    case = PoolCase(lens, 2, 128, 16, seed=length)
+    q = rows(n, 8, 128, dtype)
+    ref = attention64(q, case.keys, case.values, [1] * n, lens)
+    out, l = run_step(case, q, max_len=max(lens))
+    check_attention(out, l, ref)
+    # a far too large bound splits differently and leaves splits empty
+    out, l = run_step(case, q, max_len=40000)
+    check_attention(out, l, ref)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_step_holes(dtype):
+    lens = [100, 40, 16, 700]
+    holes = [(0, 0), (0, 3), (1, 1), (2, 0), (3, 5), (3, 43)]  # sequence 2 has nothing left
+    case = PoolCase(lens, 2, 64, 16, holes=holes)
+    q = rows(4, 4, 64, dtype)
+    ref = attention64(q, case.keys, case.values, [1] * 4, lens, case.visible)
+    for max_len in (None, 700):
+        out, l = run_step(case, q, max_len=max_len)
+        check_attention(out, l, ref)
+    assert (out[2] == 0).all() and (l[2] == -math.inf).all()
+
+
+def test_step_lengths_are_bounded():
+    """Lengths past max_len or the table's width, or negative, read nothing else."""
+    case = PoolCase([64, 64, 64, 64], 2, 64, 16, width_more=0)
+    case.lens = torch.tensor([1 << 30, -5, 64, 65], dtype=torch.int32)
+    q = rows(4, 4, 64, F32)
+    for max_len, n in ((None, 64), (50, 50)):
+        ref = attention64(q, [k[:n] for k in case.keys], [v[:n] for v in case.values], [1] * 4,
+                          [n, 0, n, n])
+        # (a sequence of 0 keys whose row comes last sees nothing)
+        out, l = run_step(case, q, max_len=max_len)
+        check_attention(out, l, ref)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_step_strides(dtype):
+    """K and V interleaved per page, queries and outputs inside wider rows."""
+    lens = [70, 5, 300]
+    case = PoolCase(lens, 2, 128, 16, layout="interleaved")
+    q = rows(3, 4, 128, dtype)
+    ref = attention64(q, case.keys, case.values, [1] * 3, lens)
+    k, v, ln, table = case.device()
+    assert not k.is_contiguous()
+    wide = torch.zeros((3, 6, 128), dtype=dtype, device="cuda")
+    wide[:, 1:5] = q.cuda()
+    into = torch.full((3, 9, 128), 7.0, dtype=dtype, device="cuda")
+    tab = torch.full((3, table.shape[1] + 3), -9, dtype=torch.int32, device="cuda")
+    tab[:, : table.shape[1]] = table
+    B.aio_paged_attention(wide[:, 1:5], k, v, ln, tab[:, : table.shape[1]], into[:, 2:6],
+                          scale=0.3)
+    ref = attention64(q, case.keys, case.values, [1] * 3, lens, scale=0.3)
+    check_attention(into[:, 2:6], None, ref)
+    assert (into[:, :2] == 7).all() and (into[:, 6:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_step_scores_of_any_size(dtype):
+    """Scores up to a few thousand and all equal; a row that is NaN stays NaN, alone."""
+    lens = [200, 200, 200]
+    case = PoolCase(lens, 1, 64, 16)
+    q = rows(3, 2, 64, dtype)
+    q[0] *= 400
+    q[1] = 0
+    ref = attention64(q, case.keys, case.values, [1] * 3, lens)
+    out, l = run_step(case, q)
+    check_attention(out, l, ref)
+    q[1, 1] = float("nan")
+    for max_len in (200, 100000):
+        out2, l2 = run_step(case, q, max_len=max_len)
+        assert torch.isnan(out2[1, 1]).all() and torch.isnan(l2[1, 1])
+        out2[1, 1], l2[1, 1] = out[1, 1], l[1, 1]
+        check_attention(out2, l2, ref)
+
+
+def test_step_values_that_are_not_finite():
+    """A visible infinity or NaN reaches its own dimension and nothing else."""
+    lens = [90]
+    case = PoolCase(lens, 1, 64, 16)
+    q = rows(1, 1, 64, F32)
+    page = int(case.table[0, 2])
+    case.v[page, 0, 3, 5] = float("inf")
+    case.v[page, 0, 4, 9] = float("nan")
+    out, _ = run_step(case, q)
+    ref = attention64(q, case.keys, case.values, [1], lens)
+    assert out[0, 0, 5] == math.inf and torch.isnan(out[0, 0, 9])
+    keep = [d for d in range(64) if d not in (5, 9)]
+    assert ((out[0, 0, keep].double().cpu() - ref[0][0, 0, keep]).abs() <= ref[2][0, 0, keep]).all()
+
+
+# ------------------------------------------------------------------- prompts
+
+PROMPTS = [  # (rows, keys) per sequence
+    [(1, 1)],
+    [(5, 5), (1, 1), (0, 0), (33, 33), (64, 64), (65, 65)],
+    [(128, 128), (0, 9), (129, 129), (31, 31)],
+    [(3, 100), (40, 300), (1, 64), (17, 17), (2, 1000)],
+    [(10, 4), (3, 0), (70, 66), (1, 0)],     # rows before the first key
+    [(200, 263)],
+]
+
+
+def run_packed(q, keys, values, qc, kc, extra=0, **kw):
+    k, v = torch.cat(keys).cuda(), torch.cat(values).cuda()
+    qd = q.cuda()
+    out = torch.full_like(qd, 9.0)
+    l = torch.full(q.shape[:2], 9.0, device="cuda")
+    B.aio_packed_attention(qd, k, v, qc.cuda(), kc.cuda(), out, lse=l, **kw)
+    torch.cuda.synchronize()
+    return out, l
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 64), (4, 2, 128), (6, 1, 64), (16, 1, 128)])
+@pytest.mark.parametrize("which", range(len(PROMPTS)))
+def test_prompts(which, H, Hkv, hd, dtype):
+    ql, kl = [a for a, _ in PROMPTS[which]], [b for _, b in PROMPTS[which]]
+    case = PoolCase(kl, Hkv, hd, 16, seed=which)
+    n = sum(ql)
+    behind = 3  # rows of no sequence
+    q = rows(n + behind, H, hd, dtype, seed=which)
+    ref = attention64(q[:n], case.keys, case.values, ql, kl)
+    out, l = run_packed(q, case.keys, case.values, cu(ql), cu(kl))
+    check_attention(out, l, ref, "packed")
+    assert (out[n:] == 9).all() and (l[n:] == 9).all()
+    k, v, lens, table = case.device()
+    for max_len in (None, max(kl), 30000):
+        out = torch.full_like(out, 9.0)
+        l = torch.full_like(l, 9.0)
+        B.aio_paged_attention(q.cuda(), k, v, lens, table, out, cu_q=cu(ql).cuda(), lse=l,
+                              max_len=max_len)
+        check_attention(out, l, ref, "paged, max_len %s" % max_len)
+        assert (out[n:] == 9).all() and (l[n:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_holes(dtype):
+    ql, kl = [20, 70, 5, 16], [20, 200, 64, 16]
+    holes = [(0, 0), (1, 2), (1, 7), (1, 12), (2, 3), (3, 0)]
+    case = PoolCase(kl, 2, 128, 16, holes=holes)
+    q = rows(sum(ql), 4, 128, dtype)
+    ref = attention64(q, case.keys, case.values, ql, kl, case.visible)
+    k, v, lens, table = case.device()
+    out, l = torch.full_like(q, 9.0).cuda(), torch.full(q.shape[:2], 9.0, device="cuda")
+    B.aio_paged_attention(q.cuda(), k, v, lens, table, out, cu_q=cu(ql).cuda(), lse=l)
+    check_attention(out, l, ref)
+    assert (out[0:16] == 0).all() and (l[0:16] == -math.inf).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("length", [60, 150])
+def test_prompt_values_a_row_does_not_see(length, dtype, bad):
+    """A later key or value that is not finite changes no row before it."""
+    case = PoolCase([length], 1, 64, 16)
+    q = rows(length, 2, 64, dtype)
+    at = length - 25
+    keys, values = [case.keys[0].clone()], [case.values[0].clone()]
+    values[0][at, 0, 7] = bad
+    keys[0][at + 5, 0, 3] = bad
+    ref = attention64(q, case.keys, case.values, [length], [length])
+    before = [t[:at] for t in ref]
+    for form in ("packed", "paged"):
+        if form == "packed":
+            out, l = run_packed(q, keys, values, cu([length]), cu([length]))
+        else:
+            other = PoolCase([length], 1, 64, 16)
+            for p in (at, at + 5):
+                pg, sl = int(other.table[0, p // 16]), p % 16
+                other.k[pg, :, sl], other.v[pg, :, sl] = keys[0][p], values[0][p]
+            k, v, lens, table = other.device()
+            out, l = torch.empty_like(q).cuda(), torch.empty(q.shape[:2], device="cuda")
+            B.aio_paged_attention(q.cuda(), k, v, lens, table, out, cu_q=cu([length]).cuda(),
+                                  lse=l)
+        check_attention(out[:at], l[:at], before, form)
+        # rows that see the value only, not yet the key
+        mid = out[at: at + 5].float().cpu()
+        assert not torch.isfinite(mid[:, :, 7]).any()
+        keep = [d for d in range(64) if d != 7]
+        err = (mid[:, :, keep].double() - ref[0][at: at + 5][:, :, keep]).abs()
+        assert (err <= ref[2][at: at + 5][:, :, keep]).all(), form
+
+
+def test_prompt_nan_row():
+    q = rows(70, 2, 64, F32)
+    case = PoolCase([70], 2, 64, 16)
+    ref = attention64(q, case.keys, case.values, [70], [70])
+    q[40, 1] = float("nan")
+    out, l = run_packed(q, case.keys, case.values, cu([70]), cu([70]))
+    assert torch.isnan(out[40, 1]).all() and torch.isnan(l[40, 1])
+    out[40, 1], l[40, 1] = ref[0][40, 1].to(out), ref[1][40, 1].to(l)
+    check_attention(out, l, ref)
+
+
+def test_packed_strides():
+    """Keys head by head ([heads][rows][dim]) and inside wider rows."""
+    ql = [30, 75]
+    case = PoolCase(ql, 2, 64, 16)
+    q = rows(sum(ql), 4, 64, BF16)
+    ref = attention64(q, case.keys, case.values, ql, ql)
+    c = cu(ql).cuda()
+    k, v = torch.cat(case.keys).cuda(), torch.cat(case.values).cuda()
+    by_head = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (k, v)]
+    wide = [torch.cat((t, t), dim=2)[:, :, :64] for t in (k, v)]
+    for kk, vv in (by_head, wide):
+        assert not kk.is_contiguous()
+        out = torch.empty_like(q).cuda()
+        B.aio_packed_attention(q.cuda(), kk, vv, c, c, out)
+        check_attention(out, None, ref)
+
+
+def test_packed_boundaries_are_bounded():
+    """Boundaries past the buffers read and write nothing outside them."""
+    q = rows(40, 2, 64, F32)
+    case = PoolCase([40], 2, 64, 16)
+    bad_q = torch.tensor([0, 1 << 30], dtype=torch.int32)
+    bad_k = torch.tensor([0, 1 << 30], dtype=torch.int32)
+    ref = attention64(q, case.keys, case.values, [40], [40])
+    out, l = run_packed(q, case.keys, case.values, bad_q, bad_k)
+    check_attention(out, l, ref)
+    neg = torch.tensor([-7, -3], dtype=torch.int32)
+    out, l = run_packed(q, case.keys, case.values, neg, neg)
+    assert (out == 9).all()
+
+
+def test_many_sequences():
+    """More sequences than a wave searches at once, most of them of one row."""
+    ql = [1 + (i % 3 == 0) * (i % 40) for i in range(150)]
+    ql[77] = 0
+    case = PoolCase(ql, 1, 64, 16)
+    q = rows(sum(ql), 2, 64, BF16)
+    ref = attention64(q, case.keys, case.values, ql, ql)
+    out, l = run_packed(q, case.keys, case.values, cu(ql), cu(ql))
+    check_attention(out, l, ref)
+
+
+# ------------------------------------------------------- streams and graphs
+
+def test_other_streams_and_workspaces():
+    """Two calls on two streams, each with its own workspace, and a workspace full of
+    NaN."""
+    lens = [3000]
+    case = PoolCase(lens, 2, 128, 16)
+    k, v, ln, table = case.device()
+    torch.cuda.synchronize()
+    qs = [rows(1, 8, 128, F32, seed=s) for s in (5, 6)]
+    need = B.aio_attn_workspace_bytes(1, 1, 3000, 8, 2, 128)
+    assert need > 0
+    outs, keep = [], []
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for q, st in zip(qs, streams):
+        with torch.cuda.stream(st):
+            qd = q.cuda()
+            ws = torch.full((need // 4,), float("nan"), device="cuda")
+            out = torch.empty_like(qd)
+            B.aio_paged_attention(qd, k, v, ln, table, out, max_len=3000, ws=ws)
+            outs.append(out)
+            keep += [qd, ws]
+    torch.cuda.synchronize()
+    for q, out in zip(qs, outs):
+        check_attention(out, None, attention64(q, case.keys, case.values, [1], lens))
+    with pytest.raises(ValueError):
+        B.aio_paged_attention(keep[0], k, v, ln, table, outs[0], max_len=3000,
+                              ws=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
+
+
+def test_captured_and_replayed():
+    """A captured step follows lengths and pages in device memory, replay by replay,
+    with eager work between the replays."""
+    lens = [600, 37]
+    case = PoolCase(lens, 2, 64, 16)
+    k, v, ln, table = case.device()
+    q = rows(2, 4, 64, F32).cuda()
+    out, l = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ql = [9, 25]
+    pq = rows(sum(ql), 4, 64, BF16).cuda()
+    pout, c = torch.empty_like(pq), cu(ql).cuda()
+
+    def step():
+        B.aio_paged_attention(q, k, v, ln, table, out, lse=l, max_len=600)
+        B.aio_paged_attention(pq, k, v, ln, table, pout, cu_q=c, max_len=600)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        step()
+    torch.cuda.current_stream().wait_stream(st)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for a, b in ((600, 37), (599, 30), (64, 33), (0, 25), (600, 37)):
+        ln.copy_(torch.tensor([a, b], dtype=torch.int32))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, l, pout)]
+        kk, vv = [case.keys[0][:a], case.keys[1][:b]], [case.values[0][:a], case.values[1][:b]]
+        check_attention(got[0], got[1], attention64(q.cpu(), kk, vv, [1, 1], [a, b]))
+        check_attention(got[2], None, attention64(pq.cpu(), kk, vv, ql, [a, b]))
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (out, l, pout)):
+            assert torch.equal(x, y)
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 2^31 elements and 2^32 bytes: the last pages."""
+    page, Hkv, hd = 256, 8, 128
+    per = Hkv * page * hd                       # 2^18 elements
+    n_pages = (1 << 31) // per + 5
+    pool = torch.zeros((n_pages, Hkv, page, hd), dtype=BF16, device="cuda")
+    case = PoolCase([300], Hkv, hd, page)
+    ids = [n_pages - 1, n_pages - 2]
+    vpool = torch.zeros_like(pool)
+    for j, g in enumerate(ids):
+        m = min(page, 300 - j * page)
+        pool[g, :, :m] = case.keys[0][j * page: j * page + m].transpose(0, 1).cuda()
+        vpool[g, :, :m] = case.values[0][j * page: j * page + m].transpose(0, 1).cuda()
+    table = torch.tensor([ids], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([300], dtype=torch.int32, device="cuda")
+    q = rows(7, 16, hd, F32)
+    out = torch.empty((1, 16, hd), device="cuda")
+    B.aio_paged_attention(q[:1].cuda(), pool, vpool, lens, table, out)
+    check_attention(out, None, attention64(q[:1], case.keys, case.values, [1], [300]))
+    out = torch.empty((7, 16, hd), device="cuda")
+    B.aio_paged_attention(q.cuda(), pool, vpool, lens, table, out, cu_q=cu([7]).cuda())
+    check_attention(out, None, attention64(q, case.keys, case.values, [7], [300]))
+
+
+def test_binding_refuses():
+    case = PoolCase([20], 2, 64, 16)
+    k, v, lens, table = case.device()
+    q = rows(1, 4, 64, F32).cuda()
+    out = torch.empty_like(q)
+    for bad in (dict(q=q.double()), dict(q=q.cpu()), dict(out=out.bfloat16()),
+                dict(lens=lens.long()), dict(table=table[0]), dict(k=k.float()),
+                dict(out=torch.empty((2, 4, 64), device="cuda")), dict(q=q.transpose(1, 2)),
+                dict(cu_q=cu([1, 0]).cuda()), dict(lse=torch.empty((4, 1), device="cuda"))):
+        a = dict(q=q, k=k, v=v, lens=lens, table=table, out=out)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            B.aio_paged_attention(**a)
