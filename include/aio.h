@@ -560,6 +560,48 @@ int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t
                   int64_t page_stride_bytes, int64_t page_bytes, const int32_t* src,
                   const int32_t* dst, int32_t n, void* hip_stream);
 
+/* A whole model's paged cache: layer l's keys and values are those of `first`
+ * l layer_stride elements further on. */
+typedef struct aio_paged_pool {
+  aio_paged_kv first;
+  int64_t layer_stride; /* elements, a multiple of 8 */
+  int32_t n_layers;
+} aio_paged_pool;
+
+/* The most rows of one aio_paged_forward. */
+#define AIO_MAX_PAGED_ROWS 2048
+
+/* One pass of a model over the next tokens of several sequences, whose keys
+ * and values live in pages instead of the handle's own cache: decode steps,
+ * prompts and continued prompts together, the weights read once for all of
+ * them (the products of aio_prefill, aio_page_append and aio_paged_attention
+ * per layer).  Host arrays: sequence i consumes rows[i] >= 0 tokens (`tokens`
+ * holds them one sequence after the other, at most AIO_MAX_PAGED_ROWS in all)
+ * at positions lens[i] - rows[i] .. lens[i] - 1, and its pages are
+ * table[i][0 .. table_stride); a page id below 0 is a hole, allowed before the
+ * page of its first new token.  Every row attends over the sequence's keys up
+ * to its own.  The logits (fp32 [n_out][vocab]) of rows out_rows[0 .. n_out) of the
+ * packed tokens go to logits_dev (16-byte aligned): the last row of each
+ * sequence to generate, every row to score a prompt or drafts.  Rows equal
+ * those of aio_prefill or aio_decode_step on a cache of their own up to
+ * rounding.  scratch_dev: aio_paged_forward_bytes bytes, 256-byte aligned, its
+ * contents of no matter.  Enqueued on the model's stream; the host arrays are
+ * read before the call returns.  Not for graph capture (it copies from host
+ * memory).
+ * AIO_EINVAL: a null or misaligned pointer, a pool whose shape is not the
+ * model's, a scratch too small, or two sequences that would write the same page.
+ * AIO_ERANGE: counts, lengths (up to max_ctx and the table's width), tokens,
+ * pages or out_rows out of range. */
+int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
+                      const int32_t* rows, const int32_t* lens, const int32_t* table,
+                      int32_t table_stride, const int32_t* tokens, const int32_t* out_rows,
+                      int32_t n_out, float* logits_dev, void* scratch_dev, size_t scratch_bytes);
+
+/* Scratch bytes for up to n_rows rows of up to n_seqs sequences with tables
+ * up to table_stride wide (0 for a bad config or sizes).  Pure host. */
+size_t aio_paged_forward_bytes(const aio_config* cfg, int32_t n_seqs, int32_t n_rows,
+                               int32_t table_stride);
+
 /* Log probabilities of logit rows ([rows][n], fp32 or bf16, rows `stride`
  * elements apart, 4- or 2-byte aligned): logprob[r] = x[target[r]] - log sum_j
  * e^x[j], entropy[r] the Shannon entropy in nats of the row's softmax, and the

@@ -58,6 +58,11 @@ class aio_paged_kv(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim")]
 
 
+class aio_paged_pool(ctypes.Structure):
+    _fields_ = [("first", aio_paged_kv), ("layer_stride", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32)]
+
+
 class aio_packed_kv(ctypes.Structure):
     _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
                 ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)] + \
@@ -143,6 +148,10 @@ def lib():
         L.aio_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.aio_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
         L.aio_logprobs_workspace_bytes.restype = sz
+        L.aio_paged_forward.argtypes = [vp, P(aio_paged_pool), i32, vp, vp, vp, i32, vp, vp, i32,
+                                        vp, vp, sz]
+        L.aio_paged_forward_bytes.argtypes = [P(aio_config), i32, i32, i32]
+        L.aio_paged_forward_bytes.restype = sz
         L.aio_pages_create.argtypes = [i32, i32, i32, P(vp)]
         L.aio_pages_destroy.argtypes = [vp]
         L.aio_pages_destroy.restype = None
@@ -773,6 +782,45 @@ class DeviceModel:
     @property
     def prefill_noalloc_rows(self) -> int:
         return int(lib().aio_prefill_noalloc_rows(ctypes.byref(self.c)))
+
+    def new_pool(self, n_pages: int, page_size: int = 16) -> torch.Tensor:
+        """A paged cache for this model: bf16 [layer, K/V, page, kv head, slot, dim]."""
+        c = self.c
+        return torch.zeros((c.n_layers, 2, n_pages, c.n_kv_heads, page_size, c.head_dim),
+                           dtype=torch.bfloat16, device=self.device)
+
+    def paged_forward(self, pool: torch.Tensor, rows, lens, table, tokens, out_rows,
+                      logits: torch.Tensor) -> None:
+        """One pass over the next tokens of several sequences in ``pool`` (a
+        new_pool tensor): rows[i] tokens of sequence i, which then has lens[i]
+        and the pages table[i] (host arrays).  logits [len(out_rows), vocab]
+        receives those of the packed rows out_rows.  On the model's stream."""
+        c = self.c
+        _need(pool.dim() == 6 and pool.dtype == torch.bfloat16 and pool.is_contiguous() and
+              pool.device == self.device and pool.shape[:2] == (c.n_layers, 2),
+              "pool: a contiguous bf16 [layers, 2, n_pages, kv_heads, page_size, head_dim]")
+        a = [np.ascontiguousarray(x, dtype=np.int32) for x in (rows, lens, table, tokens, out_rows)]
+        n = a[0].size
+        _need(a[1].size == n and a[2].ndim == 2 and a[2].shape[0] == n and
+              a[3].size == a[0].sum(dtype=np.int64), "rows, lens, table and tokens do not match")
+        _need(logits.dtype == torch.float32 and logits.is_contiguous() and
+              logits.numel() >= a[4].size * c.vocab, "logits: contiguous fp32 [out rows, vocab]")
+        kv = aio_paged_kv(pool.data_ptr(), pool[0, 1].data_ptr(), pool.stride(2), pool.stride(3),
+                          pool.shape[2], pool.shape[4], pool.shape[3], pool.shape[5])
+        p = aio_paged_pool(kv, pool.stride(0), pool.shape[0])
+        need = int(lib().aio_paged_forward_bytes(ctypes.byref(c), n, int(a[3].size),
+                                                 a[2].shape[1]))
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            if getattr(self, "_paged_scratch", None) is None or \
+                    self._paged_scratch.numel() < need:
+                self._paged_scratch = torch.empty(max(need, 256), dtype=torch.uint8,
+                                                  device=self.device)
+            s = self._paged_scratch
+            _check(lib().aio_paged_forward(self.handle, ctypes.byref(p), n, a[0].ctypes.data,
+                                           a[1].ctypes.data, a[2].ctypes.data, a[2].shape[1],
+                                           a[3].ctypes.data, a[4].ctypes.data, int(a[4].size),
+                                           _ptr(logits), s.data_ptr(), s.numel()),
+                   "aio_paged_forward")
 
     def tune(self, token: int, pos: int, logits: torch.Tensor, rounds: int = 4) -> None:
         """Calibrate the persistent kernel's gate/up split (aio_tune_step)."""

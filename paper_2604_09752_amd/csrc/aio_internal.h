@@ -173,3 +173,22 @@ extern "C" int aio_prefill_plan(const aio_config* c, int rows, int num_cus, int3
 // One chunk of R <= b.rcap rows (tokens already in b.tokens) at positions
 // pos0 .. pos0 + R - 1.
 hipError_t aio_launch_prefill_chunk(const aio_model& m, const PfBuffers& b, int R, int pos0);
+
+// The same rows as the next tokens of several sequences (aio_paged_forward):
+// each row's position is its own, so its rotation is gathered first, and the
+// products write K and V as if to a cache of R positions (k, v: [Hkv][R][hd]),
+// from which they go to the pages.
+struct PagedPass {
+  const int32_t* pos;  // [R] positions
+  float2* rope;        // [R][hd / 2]
+  uint16_t* k;
+  uint16_t* v;
+  aio_paged_pool pool;
+  aio_seqs seqs;
+  void* ws;
+  size_t ws_bytes;
+};
+hipError_t aio_launch_paged_pass(const aio_model& m, const PfBuffers& b, int R,
+                                 const PagedPass& pass);
+// Rows idx[0 .. n) of the chunk's residual rows to the workspace's (lay.x).
+hipError_t aio_launch_gather_rows(const aio_model& m, const float* x, const int32_t* idx, int n);

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "aio_internal.h"
+#include "paged.h"
 
 // Scratch of aio_prefill_noalloc: one array per GPU the library runs on,
 // held until the process ends.  In host code `scratch` is only a stand-in
@@ -790,6 +791,173 @@ int aio_category_entropy(aio_model* m, const float* logits_dev, const int32_t* l
     if (label_ids[i] < 0 || label_ids[i] >= m->cfg.vocab) return AIO_ERANGE;
   const hipError_t e = aio_launch_category_entropy(*m, logits_dev, label_ids, n_labels, out_dev);
   return e == hipSuccess ? AIO_OK : hip_fail(e);
+}
+
+// ------------------------------------ several sequences over a paged pool
+
+namespace {
+
+// The scratch of one paged pass: the prefill's, and behind it the rows' K and V
+// and rotations, the call's host arrays, and the attention's workspace.
+struct PagedScratch {
+  PfBuffers pf;
+  uint16_t *k, *v;
+  float2* rope;
+  int32_t* ints;  // tokens, positions, lens, cu_q, table, logit rows
+  size_t n_ints;
+  char* ws;
+  size_t ws_bytes, bytes;
+};
+
+PagedScratch paged_scratch(const aio_config& c, char* base, int32_t n_seqs, int32_t R,
+                           int32_t stride) {
+  PagedScratch s{};
+  s.pf = aio_prefill_buffers(c, base, R);
+  size_t off = s.pf.bytes;
+  auto take = [&](size_t bytes) {
+    char* p = base + off;
+    off = align256(off + bytes);
+    return p;
+  };
+  const size_t kv = (size_t)c.n_kv_heads * R * c.head_dim * 2;
+  s.k = (uint16_t*)take(kv);
+  s.v = (uint16_t*)take(kv);
+  s.rope = (float2*)take((size_t)R * (c.head_dim / 2) * sizeof(float2));
+  s.n_ints = 3 * (size_t)R + 2 * (size_t)n_seqs + 1 + (size_t)n_seqs * stride;
+  s.ints = (int32_t*)take(4 * s.n_ints);
+  s.ws_bytes = aio_attn_workspace_bound(c.n_heads, c.n_kv_heads, c.head_dim);
+  s.ws = take(s.ws_bytes);
+  s.bytes = off;
+  return s;
+}
+
+bool paged_sizes_ok(int64_t n_seqs, int64_t n_rows, int64_t stride) {
+  return n_seqs >= 1 && n_seqs <= (1 << 20) && n_rows >= 1 && n_rows <= AIO_MAX_PAGED_ROWS &&
+         stride >= 1 && n_seqs * stride <= (1 << 28);
+}
+
+// The checks of aio_paged_forward that need no device; *R receives the rows.
+int check_paged_forward(const aio_model* m, const aio_paged_pool& p, int32_t n_seqs,
+                        const int32_t* rows, const int32_t* lens, const int32_t* table,
+                        int32_t stride, const int32_t* tokens, const int32_t* out_rows,
+                        int32_t n_out, int32_t* R) {
+  const aio_config& c = m->cfg;
+  const aio_paged_kv& kv = p.first;
+  const int rc = aio_check_paged(kv);
+  if (rc) return rc;
+  if (kv.n_kv_heads != c.n_kv_heads || kv.head_dim != c.head_dim || p.n_layers != c.n_layers ||
+      p.layer_stride < 0 || p.layer_stride % 8)
+    return AIO_EINVAL;
+  if (n_seqs < 1 || n_seqs > (1 << 20) || n_out < 0) return AIO_ERANGE;
+  int64_t total = 0;
+  for (int32_t i = 0; i < n_seqs; ++i) {
+    if (rows[i] < 0 || lens[i] < rows[i] || lens[i] > c.max_ctx ||
+        lens[i] > (int64_t)stride * kv.page_size)
+      return AIO_ERANGE;
+    total += rows[i];
+  }
+  if (!paged_sizes_ok(n_seqs, total, stride)) return AIO_ERANGE;
+  for (int64_t t = 0; t < total; ++t)
+    if (tokens[t] < 0 || tokens[t] >= c.vocab) return AIO_ERANGE;
+  for (int32_t i = 0; i < n_out; ++i)
+    if (out_rows[i] < 0 || out_rows[i] >= total) return AIO_ERANGE;
+  std::vector<std::pair<int32_t, int32_t>> written;  // page, sequence
+  for (int32_t i = 0; i < n_seqs; ++i) {
+    const int32_t* t = table + (size_t)i * stride;
+    const int32_t first = (lens[i] - rows[i]) / kv.page_size;  // page of the first new token
+    for (int32_t j = 0; (int64_t)j * kv.page_size < lens[i]; ++j) {
+      const bool fresh = rows[i] > 0 && j >= first;
+      if (t[j] >= kv.n_pages || (fresh && t[j] < 0)) return AIO_ERANGE;
+      if (fresh) written.push_back({t[j], i});
+    }
+  }
+  // a page is written by one sequence, and once in it
+  std::sort(written.begin(), written.end());
+  for (size_t i = 1; i < written.size(); ++i)
+    if (written[i].first == written[i - 1].first) return AIO_EINVAL;
+  *R = (int32_t)total;
+  return AIO_OK;
+}
+
+}  // namespace
+
+size_t aio_paged_forward_bytes(const aio_config* cfg, int32_t n_seqs, int32_t n_rows,
+                               int32_t table_stride) {
+  if (aio_check_config(cfg) != AIO_OK || !paged_sizes_ok(n_seqs, n_rows, table_stride)) return 0;
+  return paged_scratch(*cfg, nullptr, n_seqs, n_rows, table_stride).bytes;
+}
+
+int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
+                      const int32_t* rows, const int32_t* lens, const int32_t* table,
+                      int32_t table_stride, const int32_t* tokens, const int32_t* out_rows,
+                      int32_t n_out, float* logits_dev, void* scratch_dev, size_t scratch_bytes) {
+  if (!m || !pool || !rows || !lens || !table || !tokens || (n_out > 0 && !out_rows))
+    return AIO_EINVAL;
+  if ((n_out > 0 && !logits_dev) || !aligned16(logits_dev) || !scratch_dev ||
+      ((uintptr_t)scratch_dev & 255u))
+    return AIO_EINVAL;
+  try {
+    int32_t R = 0;
+    int rc = check_paged_forward(m, *pool, n_seqs, rows, lens, table, table_stride, tokens,
+                                 out_rows, n_out, &R);
+    if (rc) return rc;
+    const aio_config& c = m->cfg;
+    PagedScratch s = paged_scratch(c, (char*)scratch_dev, n_seqs, R, table_stride);
+    if (s.bytes > scratch_bytes) return AIO_EINVAL;
+    PagedPass pass{};
+    pass.pool = *pool;
+    pass.rope = s.rope;
+    pass.k = s.k;
+    pass.v = s.v;
+    pass.ws = s.ws;
+    pass.ws_bytes = s.ws_bytes;
+    // the call's arrays, in one copy: tokens and positions of the rows, then the sequences'
+    std::vector<int32_t> host;
+    host.reserve(s.n_ints);
+    host.insert(host.end(), tokens, tokens + R);
+    bool one_each = true;
+    int32_t max_len = 0;
+    for (int32_t i = 0; i < n_seqs; ++i) {
+      for (int32_t r = 0; r < rows[i]; ++r) host.push_back(lens[i] - rows[i] + r);
+      one_each &= rows[i] == 1;
+      max_len = std::max(max_len, lens[i]);
+    }
+    host.insert(host.end(), lens, lens + n_seqs);
+    host.push_back(0);
+    for (int32_t i = 0; i < n_seqs; ++i) host.push_back(host.back() + rows[i]);
+    host.insert(host.end(), table, table + (size_t)n_seqs * table_stride);
+    // (rows asked for more than once go out in several copies of R)
+    s.pf.tokens = s.ints;
+    pass.pos = s.ints + R;
+    pass.seqs.n_seqs = n_seqs;
+    pass.seqs.n_rows = R;
+    pass.seqs.max_len = max_len;
+    pass.seqs.lens_dev = s.ints + 2 * (size_t)R;
+    const int32_t* cu_q = pass.seqs.lens_dev + n_seqs;
+    pass.seqs.cu_q_dev = one_each ? nullptr : cu_q;
+    pass.seqs.table_dev = cu_q + n_seqs + 1;
+    pass.seqs.table_stride = table_stride;
+    int32_t* out_dev = (int32_t*)pass.seqs.table_dev + (size_t)n_seqs * table_stride;
+    hipError_t e = hipMemcpyAsync(s.ints, host.data(), host.size() * 4, hipMemcpyHostToDevice,
+                                  m->stream);
+    if (e == hipSuccess) e = aio_launch_paged_pass(*m, s.pf, R, pass);
+    for (int32_t at = 0; at < n_out && e == hipSuccess; at += R) {
+      const int32_t some = std::min(n_out - at, R);
+      e = hipMemcpyAsync(out_dev, out_rows + at, (size_t)some * 4, hipMemcpyHostToDevice,
+                         m->stream);
+      for (int32_t i = 0; i < some && e == hipSuccess; i += c.max_verify) {
+        const int n = std::min(some - i, c.max_verify);
+        e = aio_launch_gather_rows(*m, s.pf.x, out_dev + i, n);
+        if (e == hipSuccess)
+          e = aio_launch_lm_rows(*m, n, logits_dev + (size_t)(at + i) * c.vocab);
+      }
+    }
+    return e == hipSuccess ? AIO_OK : hip_fail(e);
+  } catch (const std::bad_alloc&) {
+    return AIO_ENOMEM;
+  } catch (...) {
+    return AIO_EINVAL;
+  }
 }
 
 // ------------------------------------------------ draft-model speculation

@@ -656,6 +656,9 @@ hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 
 }  // namespace
 
+// Workgroups up to which the keys are split.
+constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
+
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
   *p = AttnPlan{};
   if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0) return AIO_ERANGE;
@@ -669,7 +672,7 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
     // splits of at least 128 keys (a block of 32 per wave)
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 127) / 128);
     const int64_t base = std::max<int64_t>(1, (int64_t)s.n_seqs * Hkv);
-    const int64_t want = std::max<int64_t>(1, std::min(units, 4 * kCUs / base));
+    const int64_t want = std::max<int64_t>(1, std::min(units, kStepGroups / base));
     p->chunk = (int)((units + want - 1) / want * 128);
     p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
     p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
@@ -677,13 +680,20 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
     p->tiles = ((int64_t)s.n_rows * G) / kRows + s.n_seqs;
     const int64_t base = std::max<int64_t>(1, p->tiles * Hkv);
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 4 * kKeys - 1) / (4 * kKeys));
-    p->splits = (int)std::max<int64_t>(1, std::min(units, 2 * kCUs / base));
+    p->splits = (int)std::max<int64_t>(1, std::min(units, kRowsGroups / base));
     p->groups = p->tiles * Hkv * p->splits;
   }
   if (p->groups > 0x7fffffff || (int64_t)s.n_rows * H > 0x7fffffff) return AIO_ERANGE;
   if (p->rows && (int64_t)s.n_rows * G > 0x7fffffff - kRows) return AIO_ERANGE;
   if (p->splits > 1) p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
   return AIO_OK;
+}
+
+size_t aio_attn_workspace_bound(int H, int Hkv, int hd) {
+  // step: splits n Hkv <= kStepGroups, so splits n H <= kStepGroups G; rows: splits tiles
+  // Hkv <= kRowsGroups and n_rows G <= kRows tiles, so splits n_rows H <= kRowsGroups kRows
+  const size_t rh = std::max<size_t>((size_t)kStepGroups * (H / Hkv), (size_t)kRowsGroups * kRows);
+  return rh * (hd + 2) * 4;
 }
 
 hipError_t aio_launch_attention(const AttnArgs& a, const AttnPlan& p, int hd, int dtype,

@@ -19,16 +19,6 @@ int done(hipError_t e) { return e == hipSuccess ? AIO_OK : aio_hip_fail(e); }
 
 bool page_size_ok(int32_t n) { return n >= kMinPage && n <= kMaxPage && (n & (n - 1)) == 0; }
 
-int check_paged(const aio_paged_kv& kv) {
-  if (!good(kv.k_dev, 16) || !good(kv.v_dev, 16)) return AIO_EINVAL;
-  if (kv.n_pages < 1 || kv.n_kv_heads < 1 || kv.page_stride < 0 || kv.page_stride % 8 ||
-      kv.head_stride < 0 || kv.head_stride % 8)
-    return AIO_EINVAL;
-  if (!page_size_ok(kv.page_size) || (kv.head_dim != 64 && kv.head_dim != 128))
-    return AIO_EUNSUPPORTED;
-  return AIO_OK;
-}
-
 int check_table(const aio_seqs& s) {
   if (s.n_seqs == 0) return AIO_OK;
   if (!good(s.lens_dev, 4) || !good(s.table_dev, 4) || !aligned(s.cu_q_dev, 4)) return AIO_EINVAL;
@@ -94,6 +84,16 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
 }
 
 }  // namespace
+
+int aio_check_paged(const aio_paged_kv& kv) {
+  if (!good(kv.k_dev, 16) || !good(kv.v_dev, 16)) return AIO_EINVAL;
+  if (kv.n_pages < 1 || kv.n_kv_heads < 1 || kv.page_stride < 0 || kv.page_stride % 8 ||
+      kv.head_stride < 0 || kv.head_stride % 8)
+    return AIO_EINVAL;
+  if (!page_size_ok(kv.page_size) || (kv.head_dim != 64 && kv.head_dim != 128))
+    return AIO_EUNSUPPORTED;
+  return AIO_OK;
+}
 
 // ------------------------------------------------------------- page tables
 
@@ -169,7 +169,7 @@ int aio_paged_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_att
                         void* ws_dev, size_t ws_bytes, void* hip_stream) {
   if (!kv || !s || !a) return AIO_EINVAL;
   if (s->cu_k_dev) return AIO_EINVAL;
-  int rc = check_paged(*kv);
+  int rc = aio_check_paged(*kv);
   if (rc == AIO_OK) rc = check_table(*s);
   if (rc) return rc;
   return attention(paged_keys(*kv, *s), kv->n_kv_heads, kv->head_dim, *s, *a, ws_dev, ws_bytes,
@@ -202,7 +202,7 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
                     const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                     int64_t head_stride, void* hip_stream) {
   if (!kv || !s) return AIO_EINVAL;
-  int rc = check_paged(*kv);
+  int rc = aio_check_paged(*kv);
   if (rc == AIO_OK) rc = check_table(*s);
   if (rc) return rc;
   if (s->n_seqs < 0 || s->n_rows < 0 || s->max_len < 0) return AIO_ERANGE;

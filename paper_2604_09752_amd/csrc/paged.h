@@ -18,6 +18,9 @@ constexpr int kMaxGroup = 16;
 // (Sizes of workspaces are asked for without a device.)
 constexpr int kCUs = 256;
 
+// AIO_OK, or what the entry points return for this pool.
+int aio_check_paged(const aio_paged_kv& kv);
+
 // A pure host description of one attention's launch.
 struct AttnPlan {
   bool rows;       // several rows per sequence (k_attn_rows), else one (k_attn_step)
@@ -29,6 +32,8 @@ struct AttnPlan {
 };
 // AIO_OK, or the error that the entry points return for these sizes.
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p);
+// No attention of these heads takes more workspace, whatever its sequences.
+size_t aio_attn_workspace_bound(int H, int Hkv, int hd);
 
 // Where an attention's keys lie: pages, or (table null) packed rows.
 struct KeysArgs {

@@ -1846,10 +1846,72 @@ PfBuffers aio_prefill_buffers(const aio_config& c, char* base, int rcap) {
   return b;
 }
 
+namespace {
+
+// Each row's rotation (a table row of its own position).
+__global__ __launch_bounds__(128) void k_rope_rows(const float2* rope, const int32_t* pos, int half,
+                                                   float2* out) {
+  const int r = blockIdx.x, i = threadIdx.x;
+  if (i < half) out[(size_t)r * half + i] = rope[(size_t)pos[r] * half + i];
+}
+
+__global__ __launch_bounds__(256) void k_gather_rows(const float* x, const int32_t* idx, int d,
+                                                     float* out) {
+  const int r = blockIdx.x;
+  const float* from = x + (size_t)idx[r] * d;
+  for (int e = threadIdx.x; e < d; e += 256) out[(size_t)r * d + e] = from[e];
+}
+
+// A layer's rows into their pages and the attention over them (b.q -> b.actA).
+int paged_attention(const aio_model& m, const PfBuffers& b, int R, int l, const PagedPass& pass) {
+  const aio_config& c = m.cfg;
+  aio_paged_kv kv = pass.pool.first;
+  kv.k_dev = (uint16_t*)kv.k_dev + (size_t)l * pass.pool.layer_stride;
+  kv.v_dev = (uint16_t*)kv.v_dev + (size_t)l * pass.pool.layer_stride;
+  const int rc = aio_page_append(&kv, &pass.seqs, pass.k, pass.v, AIO_BF16, c.head_dim,
+                                 (int64_t)R * c.head_dim, m.stream);
+  if (rc) return rc;
+  aio_attn a{};
+  a.q_dev = b.q;
+  a.out_dev = b.actA;
+  a.q_stride = c.n_heads * c.head_dim;
+  a.out_stride = b.lda_a;
+  a.dtype = AIO_F32;
+  a.n_heads = c.n_heads;
+  a.scale = (float)(1.0 / sqrt((double)c.head_dim));
+  return aio_paged_attention(&kv, &pass.seqs, &a, pass.ws, pass.ws_bytes, m.stream);
+}
+
+hipError_t launch_rows(const aio_model& m, const PfBuffers& b, int R, int pos0,
+                       const PagedPass* pass);
+
+}  // namespace
+
 // One chunk of R <= b.rcap prompt rows at positions pos0 .. pos0 + R - 1;
 // their tokens are in b.tokens.  On return (enqueued) the cache holds their
 // K/V rows in every layer and b.x row R - 1 the last row's final residual.
 hipError_t aio_launch_prefill_chunk(const aio_model& m, const PfBuffers& b, int R, int pos0) {
+  return launch_rows(m, b, R, pos0, nullptr);
+}
+
+hipError_t aio_launch_paged_pass(const aio_model& m, const PfBuffers& b, int R,
+                                 const PagedPass& pass) {
+  hipLaunchKernelGGL(k_rope_rows, dim3(R), dim3(128), 0, m.stream, m.rope, pass.pos,
+                     m.cfg.head_dim / 2, pass.rope);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_rows(m, b, R, 0, &pass);
+}
+
+hipError_t aio_launch_gather_rows(const aio_model& m, const float* x, const int32_t* idx, int n) {
+  hipLaunchKernelGGL(k_gather_rows, dim3(n), dim3(256), 0, m.stream, x, idx, m.cfg.d_model,
+                     m.at<float>(m.lay.x));
+  return hipGetLastError();
+}
+
+namespace {
+
+hipError_t launch_rows(const aio_model& m, const PfBuffers& b, int R, int pos0,
+                       const PagedPass* pass) {
   const aio_config& c = m.cfg;
   const int d = c.d_model, H = c.n_heads, Hkv = c.n_kv_heads, hd = c.head_dim;
   const int nss = d / 64;
@@ -1872,20 +1934,29 @@ hipError_t aio_launch_prefill_chunk(const aio_model& m, const PfBuffers& b, int 
     g.kc = m.kv_layer(l, 0); g.vc = m.kv_layer(l, 1);
     g.rope = m.rope; g.pos0 = pos0;
     g.H = H; g.Hkv = Hkv; g.hd = hd; g.max_ctx = c.max_ctx;
+    if (pass) {
+      g.kc = pass->k; g.vc = pass->v;
+      g.rope = pass->rope; g.max_ctx = R;
+    }
     // (the last argument of a product: activations idle meanwhile, for the partial
     // sums of a K split)
     if ((e = launch_pgemm<PE_QKV>(m, g, PF_QKV, b.actN)) != hipSuccess) return e;
 
-    PAttnArgs t{};
-    t.q = b.q; t.ldq = H * hd;
-    t.kc = g.kc; t.vc = g.vc;
-    t.act = b.actA; t.lda = b.lda_a;
-    t.R = R; t.pos0 = pos0; t.H = H; t.Hkv = Hkv; t.max_ctx = c.max_ctx;
-    t.by_g = make_udiv((unsigned)(H / Hkv), (unsigned)H);
-    t.by_hpx = make_udiv((unsigned)std::max(H / 8, 1), (unsigned)H * (unsigned)((R + 31) / 32));
-    t.scale_log2 = (float)(1.4426950408889634 / sqrt((double)hd));
-    e = hd == 128 ? launch_pattn_t<128>(m, t) : launch_pattn_t<64>(m, t);
-    if (e != hipSuccess) return e;
+    if (pass) {
+      const int rc = paged_attention(m, b, R, l, *pass);
+      if (rc) return rc == AIO_EHIP ? (hipError_t)aio_last_hip_error() : hipErrorInvalidValue;
+    } else {
+      PAttnArgs t{};
+      t.q = b.q; t.ldq = H * hd;
+      t.kc = g.kc; t.vc = g.vc;
+      t.act = b.actA; t.lda = b.lda_a;
+      t.R = R; t.pos0 = pos0; t.H = H; t.Hkv = Hkv; t.max_ctx = c.max_ctx;
+      t.by_g = make_udiv((unsigned)(H / Hkv), (unsigned)H);
+      t.by_hpx = make_udiv((unsigned)std::max(H / 8, 1), (unsigned)H * (unsigned)((R + 31) / 32));
+      t.scale_log2 = (float)(1.4426950408889634 / sqrt((double)hd));
+      e = hd == 128 ? launch_pattn_t<128>(m, t) : launch_pattn_t<64>(m, t);
+      if (e != hipSuccess) return e;
+    }
 
     PGemmArgs o{};
     o.act = b.actA; o.lda = b.lda_a; o.R = R;
@@ -1916,3 +1987,5 @@ hipError_t aio_launch_prefill_chunk(const aio_model& m, const PfBuffers& b, int 
   }
   return hipSuccess;
 }
+
+}  // namespace

@@ -317,3 +317,10 @@ def test_page_table_refusals(L):
     assert p.rows([t], 4)[1].tolist() == before
     assert L.aio_pages_free(None) == B.AIO_EINVAL
     L.aio_pages_destroy(None)
+
+
+def test_paged_forward_rejects_without_a_device(L):
+    i = (ctypes.c_int32 * 1)(1)
+    p = B.aio_paged_pool(paged(), 64, 2)
+    assert L.aio_paged_forward(None, R(p), 1, i, i, i, 1, i, i, 1, P16, 256, 1 << 30) == B.AIO_EINVAL
+    assert L.aio_paged_forward_bytes(None, 1, 1, 1) == 0
