@@ -391,84 +391,92 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _on_device(t: torch.Tensor, *others) -> None:
-    _need(t.is_cuda, "a device tensor is needed")
+# (A decode step's calls are as short as their launches: the checks below look
+# at each tensor once, and a stream is asked for as a number.)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _device_of(first: torch.Tensor, *others) -> int:
+    """The index of the one device of the tensors (None: not given)."""
+    at = first.get_device()
+    _need(at >= 0, "a device tensor is needed")
     for o in others:
-        _need(o is None or o.device == t.device, "tensors on different devices")
+        if o is not None and o.get_device() != at:
+            raise ValueError("tensors on different devices")
+    return at
 
 
-class _Call:
-    """The tensor's device made current for a call, and its current stream."""
-
-    def __init__(self, t: torch.Tensor):
-        self.index = t.device.index
-
-    def __enter__(self):
-        self.old = torch.cuda.current_device()
-        if self.old != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.old != self.index:
-            torch.cuda.set_device(self.old)
+def _launch(at: int, call, *args) -> int:
+    """call(*args, stream) with device ``at`` current, on its current stream."""
+    if torch.cuda.current_device() == at:
+        return call(*args, _raw_stream(at))
+    with torch.cuda.device(at):
+        return call(*args, _raw_stream(at))
 
 
 def _i32(t: torch.Tensor, dim: int, what: str) -> None:
-    _need(t.dtype == torch.int32 and t.dim() == dim and (t.numel() == 0 or t.stride(-1) == 1),
-          what + ": an int32 tensor with %d dimension(s) is needed" % dim)
+    if t.dtype is not torch.int32 or t.dim() != dim or (t.stride(-1) != 1 and t.numel() > 1):
+        raise ValueError(what + ": an int32 tensor with %d dimension(s) is needed" % dim)
 
 
-def _rows3(t: torch.Tensor, what: str) -> int:
+def _rows3(t: torch.Tensor, shape, what: str) -> int:
     """[rows][heads][head_dim] with the last two dimensions contiguous; its row stride."""
-    _need(t.dim() == 3 and t.dtype in _DTYPES, what + ": fp32 or bf16 [rows, heads, head_dim]")
-    n, h, d = t.shape
-    _need(t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)),
-          what + ": heads and dimensions have to be contiguous")
-    return t.stride(0) if n > 1 else h * d
+    n, h, d = shape
+    row, head, one = t.stride()
+    if (one != 1 and d > 1) or (head != d and h > 1):
+        _need(t.numel() == 0, what + ": heads and dimensions have to be contiguous")
+    return row if n > 1 else h * d
 
 
 def _paged(k: torch.Tensor, v: torch.Tensor) -> aio_paged_kv:
-    _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype == torch.bfloat16,
-          "pages: two bf16 [n_pages, kv_heads, page_size, head_dim]")
-    _need(k.stride() == v.stride() and k.stride(3) == 1 and k.stride(2) == k.shape[3],
-          "pages: K and V of the same strides, slots and dimensions contiguous")
-    return aio_paged_kv(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0],
-                        k.shape[2], k.shape[1], k.shape[3])
+    shape, stride = k.shape, k.stride()
+    if (len(shape) != 4 or v.shape != shape or k.dtype is not torch.bfloat16 or
+            v.dtype is not torch.bfloat16):
+        raise ValueError("pages: two bf16 [n_pages, kv_heads, page_size, head_dim]")
+    if v.stride() != stride or stride[3] != 1 or stride[2] != shape[3]:
+        raise ValueError("pages: K and V of the same strides, slots and dimensions contiguous")
+    return aio_paged_kv(k.data_ptr(), v.data_ptr(), stride[0], stride[1], shape[0], shape[2],
+                        shape[1], shape[3])
 
 
 def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_seqs:
     _i32(lens, 1, "lens")
     _i32(table, 2, "table")
-    n = lens.shape[0]
-    _need(table.shape[0] == n, "lens and table are of different batches")
+    n, width = table.shape
+    _need(lens.shape[0] == n, "lens and table are of different batches")
+    cu = None
     if cu_q is not None:
         _i32(cu_q, 1, "cu_q")
         _need(cu_q.shape[0] == n + 1, "cu_q: one more entry than sequences")
+        cu = cu_q.data_ptr()
     if max_len is None:
-        max_len = table.shape[1] * page_size
-    return aio_seqs(n, n_rows, min(int(max_len), 0x7fffffff), _ptr(cu_q), lens.data_ptr(),
-                    table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], None)
+        max_len = width * page_size
+    return aio_seqs(n, n_rows, min(int(max_len), 0x7fffffff), cu, lens.data_ptr(),
+                    table.data_ptr(), table.stride(0) if n > 1 else width, None)
 
 
 def _attn(q, out, lse, scale) -> aio_attn:
-    sq, so = _rows3(q, "q"), _rows3(out, "out")
-    _need(q.shape == out.shape and q.dtype == out.dtype, "q and out differ in shape or type")
-    if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous(),
-              "lse: contiguous fp32 [rows, heads]")
-    return aio_attn(q.data_ptr(), out.data_ptr(), _ptr(lse), sq, so, _DTYPES[q.dtype], q.shape[1],
-                    q.shape[2] ** -0.5 if scale is None else float(scale))
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or out.shape != shape or out.dtype is not dtype or dtype not in _DTYPES:
+        raise ValueError("q and out: both fp32 or both bf16 [rows, heads, head_dim]")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != shape[:2] or
+                            not lse.is_contiguous()):
+        raise ValueError("lse: contiguous fp32 [rows, heads]")
+    return aio_attn(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                    _rows3(q, shape, "q"), _rows3(out, shape, "out"), _DTYPES[dtype], shape[1],
+                    shape[2] ** -0.5 if scale is None else scale)
 
 
-def _workspace(nbytes: int, ws, like: torch.Tensor):
+def _workspace(nbytes: int, ws, device):
+    """(tensor or None, pointer) of a workspace of nbytes."""
     if nbytes == 0:
-        return None
+        return None, None
     if ws is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    _need(ws.is_contiguous() and ws.numel() * ws.element_size() >= nbytes,
-          "the workspace is smaller than %d bytes" % nbytes)
-    return ws
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    else:
+        _need(ws.is_contiguous() and ws.numel() * ws.element_size() >= nbytes,
+              "the workspace is smaller than %d bytes" % nbytes)
+    return ws, ws.data_ptr()
 
 
 def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: int,
@@ -479,13 +487,14 @@ def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: in
     return int(lib().aio_attn_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
 
 
-def _attend(name, kv, s, a, q, n_kv_heads, ws):
+def _attend(name, at, kv, s, a, n_kv_heads, head_dim, device, ws):
     L = lib()
-    n = L.aio_attn_workspace_bytes(ctypes.byref(s), a.n_heads, n_kv_heads, q.shape[2])
-    with _Call(q) as stream:
-        w = _workspace(n, ws, q)
-        _check(getattr(L, name)(ctypes.byref(kv), ctypes.byref(s), ctypes.byref(a), _ptr(w), n,
-                                stream), name)
+    s, a = ctypes.byref(s), ctypes.byref(a)
+    n = L.aio_attn_workspace_bytes(s, a._obj.n_heads, n_kv_heads, head_dim)
+    ws, w = _workspace(n, ws, device)
+    rc = _launch(at, getattr(L, name), ctypes.byref(kv), s, a, w, n)
+    if rc:
+        raise AioError(rc, name)
 
 
 def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
@@ -497,11 +506,12 @@ def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens:
     keys and table pages: one row per sequence, or with cu_q the rows of
     prompts, causal.  max_len: no sequence is longer (default: the table's
     width; a closer one gives a better split of the work)."""
-    _on_device(q, k, v, lens, table, out, cu_q, lse, ws)
+    at = _device_of(q, k, v, lens, table, out, cu_q, lse, ws)
     kv, a = _paged(k, v), _attn(q, out, lse, scale)
-    _need(q.shape[2] == k.shape[3], "q and k differ in head_dim")
-    s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, k.shape[2])
-    _attend("aio_paged_attention", kv, s, a, q, k.shape[1], ws)
+    rows, _, hd = q.shape
+    _need(hd == kv.head_dim, "q and k differ in head_dim")
+    s = _paged_seqs(lens, table, cu_q, rows, max_len, kv.page_size)
+    _attend("aio_paged_attention", at, kv, s, a, kv.n_kv_heads, hd, q.device, ws)
 
 
 def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
@@ -511,7 +521,7 @@ def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q
     """Causal attention of the packed rows q over packed keys and values k, v
     (bf16 [keys, kv_heads, head_dim]); cu_q and cu_k give each sequence's first
     row and key."""
-    _on_device(q, k, v, cu_q, cu_k, out, lse, ws)
+    at = _device_of(q, k, v, cu_q, cu_k, out, lse, ws)
     a = _attn(q, out, lse, scale)
     _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype == torch.bfloat16 and
           k.shape[2] == q.shape[2], "k, v: two bf16 [keys, kv_heads, head_dim]")
@@ -524,7 +534,7 @@ def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q
                        k.shape[1], k.shape[2])
     s = aio_seqs(cu_q.shape[0] - 1, q.shape[0], k.shape[0] if max_len is None else int(max_len),
                  cu_q.data_ptr(), None, None, 0, cu_k.data_ptr())
-    _attend("aio_packed_attention", kv, s, a, q, k.shape[1], ws)
+    _attend("aio_packed_attention", at, kv, s, a, kv.n_kv_heads, kv.head_dim, q.device, ws)
 
 
 def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -532,35 +542,38 @@ def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor,
                     max_len: int | None = None) -> None:
     """Write the new rows' keys and values ([rows, kv_heads, head_dim], fp32 or
     bf16) into their pages; lens counts them already."""
-    _on_device(k_rows, v_rows, k, v, lens, table, cu_q)
+    at = _device_of(k, v, k_rows, v_rows, lens, table, cu_q)
     kv = _paged(k, v)
-    _need(k_rows.dim() == 3 and k_rows.shape == v_rows.shape and k_rows.dtype == v_rows.dtype and
-          k_rows.dtype in _DTYPES and k_rows.shape[1] == k.shape[1] and
-          k_rows.shape[2] == k.shape[3], "rows: two fp32 or bf16 [rows, kv_heads, head_dim]")
-    _need(k_rows.stride() == v_rows.stride() and (k_rows.numel() == 0 or k_rows.stride(2) == 1),
-          "rows: the same strides, dimensions contiguous")
-    s = _paged_seqs(lens, table, cu_q, k_rows.shape[0], max_len, k.shape[2])
-    with _Call(k) as stream:
-        _check(lib().aio_page_append(ctypes.byref(kv), ctypes.byref(s), k_rows.data_ptr(),
-                                     v_rows.data_ptr(), _DTYPES[k_rows.dtype], k_rows.stride(0),
-                                     k_rows.stride(1), stream), "aio_page_append")
+    shape, stride, dtype = k_rows.shape, k_rows.stride(), k_rows.dtype
+    if (len(shape) != 3 or v_rows.shape != shape or v_rows.dtype is not dtype or
+            dtype not in _DTYPES or shape[1] != kv.n_kv_heads or shape[2] != kv.head_dim):
+        raise ValueError("rows: two fp32 or bf16 [rows, kv_heads, head_dim]")
+    if v_rows.stride() != stride or stride[2] != 1:
+        _need(k_rows.numel() == 0, "rows: the same strides, dimensions contiguous")
+    s = _paged_seqs(lens, table, cu_q, shape[0], max_len, kv.page_size)
+    rc = _launch(at, lib().aio_page_append, ctypes.byref(kv), ctypes.byref(s), k_rows.data_ptr(),
+                 v_rows.data_ptr(), _DTYPES[dtype], stride[0], stride[1])
+    if rc:
+        raise AioError(rc, "aio_page_append")
 
 
 def aio_page_copy(pool: torch.Tensor, src, dst) -> None:
     """Copy pages src[i] to dst[i] (host int32 arrays) in every plane of the pool
     [planes, n_pages, ...], whose pages are contiguous."""
-    _on_device(pool)
-    _need(pool.dim() >= 3 and pool[0, 0].is_contiguous(),
-          "pool: [planes, n_pages, ...] with contiguous pages")
+    at = _device_of(pool)
+    shape, stride, inner = pool.shape, pool.stride(), 1
+    _need(len(shape) >= 3 and pool.numel() > 0, "pool: [planes, n_pages, ...]")
+    for n, st in zip(shape[:1:-1], stride[:1:-1]):
+        _need(n == 1 or st == inner, "pool: pages have to be contiguous")
+        inner *= n
     a, b = np.ascontiguousarray(src, dtype=np.int32), np.ascontiguousarray(dst, dtype=np.int32)
     _need(a.ndim == 1 and a.shape == b.shape, "src and dst differ in length")
     size = pool.element_size()
-    page = pool.stride(1) if pool.shape[1] > 1 else pool[0, 0].numel()
-    with _Call(pool) as stream:
-        _check(lib().aio_page_copy(pool.data_ptr(), pool.shape[0], pool.stride(0) * size,
-                                   pool.shape[1], page * size, pool[0, 0].numel() * size,
-                                   a.ctypes.data, b.ctypes.data, a.size, stream),
-               "aio_page_copy")
+    rc = _launch(at, lib().aio_page_copy, pool.data_ptr(), shape[0], stride[0] * size, shape[1],
+                 (stride[1] if shape[1] > 1 else inner) * size, inner * size, a.ctypes.data,
+                 b.ctypes.data, a.size)
+    if rc:
+        raise AioError(rc, "aio_page_copy")
 
 
 def aio_logprobs_workspace_bytes(rows: int, n: int, top: int) -> int:
@@ -573,33 +586,35 @@ def aio_logprobs(logits: torch.Tensor, targets: torch.Tensor | None,
                  ws: torch.Tensor | None = None) -> None:
     """Log probabilities of the targets, entropies and the top alternatives of
     logits [rows, n] (fp32 or bf16); each output may be None."""
-    _on_device(logits, targets, logprob, entropy, top_ids, top_logprobs, ws)
-    _need(logits.dim() == 2 and logits.dtype in _DTYPES and
-          (logits.numel() == 0 or logits.shape[1] == 1 or logits.stride(1) == 1),
-          "logits: fp32 or bf16 [rows, n]")
+    at = _device_of(logits, targets, logprob, entropy, top_ids, top_logprobs, ws)
+    dtype = logits.dtype
+    _need(logits.dim() == 2 and dtype in _DTYPES, "logits: fp32 or bf16 [rows, n]")
     rows, n = logits.shape
+    _need(n <= 1 or rows == 0 or logits.stride(1) == 1, "logits: rows have to be contiguous")
     if targets is not None:
         _i32(targets, 1, "targets")
-    for t in (targets, logprob, entropy):
-        _need(t is None or (t.shape == (rows,) and t.is_contiguous()), "one value per row")
-    for t in (logprob, entropy, top_logprobs):
-        _need(t is None or t.dtype == torch.float32, "fp32 outputs")
+        _need(targets.shape[0] == rows, "one target per row")
+    for t in (logprob, entropy):
+        if t is not None and (t.dtype is not torch.float32 or t.shape != (rows,) or
+                              not t.is_contiguous()):
+            raise ValueError("logprob, entropy: contiguous fp32 [rows]")
     _need((top_ids is None) == (top_logprobs is None), "top_ids and top_logprobs go together")
     top = 0
     if top_ids is not None:
         _i32(top_ids, 2, "top_ids")
-        _need(top_ids.shape == top_logprobs.shape and top_ids.shape[0] == rows and
-              top_ids.is_contiguous() and top_logprobs.is_contiguous(),
-              "top_ids, top_logprobs: contiguous [rows, top]")
         top = top_ids.shape[1]
+        if (top_ids.shape[0] != rows or top_logprobs.shape != top_ids.shape or
+                top_logprobs.dtype is not torch.float32 or not top_ids.is_contiguous() or
+                not top_logprobs.is_contiguous()):
+            raise ValueError("top_ids, top_logprobs: contiguous int32 and fp32 [rows, top]")
     L = lib()
     need = L.aio_logprobs_workspace_bytes(rows, n, top)
-    with _Call(logits) as stream:
-        w = _workspace(need, ws, logits)
-        _check(L.aio_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], rows, n,
-                              logits.stride(0) if rows > 1 else n, _ptr(targets), top,
-                              _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
-                              _ptr(w), need, stream), "aio_logprobs")
+    ws, w = _workspace(need, ws, logits.device)
+    rc = _launch(at, L.aio_logprobs, logits.data_ptr(), _DTYPES[dtype], rows, n,
+                 logits.stride(0) if rows > 1 else n, _ptr(targets), top, _ptr(logprob),
+                 _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), w, need)
+    if rc:
+        raise AioError(rc, "aio_logprobs")
 
 
 class Pages:

@@ -619,15 +619,41 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   M = wave_max(M);
   constexpr int PER = HD / AIO_WAVE;
   float os[PER] = {}, ls = 0.f;
-  for (int s = 0; s < a.S; ++s) {
-    const int64_t at = s * all + rh;
-    const float x = a.part_ml[at * 2];
-    if (x == -INFINITY) continue;  // (its other values were not written)
-    const float c = __builtin_amdgcn_exp2f(x - M);
-    ls += c * a.part_ml[at * 2 + 1];
+  // a split's weight in its lane, then the splits with keys (the others' values were
+  // not written), their loads independent of one another
+  for (int s0 = 0; s0 < a.S; s0 += AIO_WAVE) {
+    float c = 0.f;
+    if (s0 + lane < a.S) {
+      const float* ml = a.part_ml + ((s0 + lane) * all + rh) * 2;
+      const float x = ml[0];
+      if (x != -INFINITY) {
+        c = __builtin_amdgcn_exp2f(x - M);
+        ls += c * ml[1];
+      }
+    }
+    const uint64_t some = __ballot(c != 0.f);
+    if (!some) continue;
+    const int n = min(a.S - s0, AIO_WAVE), valid = __ffsll((unsigned long long)some) - 1;
+    constexpr int B = 8;
+    for (int s1 = 0; s1 < n; s1 += B) {
+      float v[B][PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) os[i] += c * a.part_o[at * HD + i * AIO_WAVE + lane];
+      for (int b = 0; b < B; ++b) {
+        const int s = s1 + b < n && some >> (s1 + b) & 1 ? s1 + b : valid;
+        const float* o = a.part_o + ((s0 + s) * all + rh) * HD + lane;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[b][i] = o[i * AIO_WAVE];
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        if (s1 + b >= n || !(some >> (s1 + b) & 1)) continue;
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c), s1 + b));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) os[i] += w * v[b][i];
+      }
+    }
   }
+  ls = wave_sum(ls);
   const bool none = ls == 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i)

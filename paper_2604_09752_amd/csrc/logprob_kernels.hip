@@ -16,7 +16,8 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kPer = 32;                  // values per thread and chunk
-constexpr int kChunk = kBlock * kPer;
+constexpr int kPerFew = 8;                // ... where a row is split
+constexpr int kMaxSlices = 64;
 // A chunk's candidates: the values from the top-th largest of the threads'
 // maxima on.  Only the `top` threads of the largest maxima hold any, at most
 // kPer each; the best `top` of the chunks before join them.
@@ -107,79 +108,175 @@ AIO_DEV void finish_row(const LogprobArgs& a, int row, const Stats& s, const uin
   }
 }
 
+// kPer values per thread from c0 on, in groups of 16 bytes where rows allow
+// it, and their indices; behind `hi`, -inf.
+template <class T, int PER, bool VEC>
+struct Chunk {
+  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;  // values per load
+  static constexpr int N = kBlock * PER;
+  float v[PER];
+  AIO_DEV static int index(int c0, int i) {
+    return c0 + (i / V * kBlock + (int)threadIdx.x) * V + i % V;
+  }
+  AIO_DEV void load(const T* x, int c0, int hi) {
+    if (VEC && c0 + N <= hi) {
+#pragma unroll
+      for (int i = 0; i < PER; i += V) {
+        const u32x4 w = *(const u32x4*)(x + index(c0, i));
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[i + j] = __uint_as_float(w[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[i + j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = index(c0, i);
+      v[i] = e < hi ? load1(x, e) : -INFINITY;
+    }
+  }
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
 // Workgroup (slice, row): the slice's statistics and its best candidates; with
 // one slice per row, the row's results.
-template <class T>
-__global__ __launch_bounds__(kBlock) void k_logprobs(LogprobArgs a) {
+//
+// A chunk's candidates are the values from a cut on: for the first chunk the
+// `top`-th largest of the maxima of the 64 groups of four threads, later the
+// smallest of the best so far (its equals come later and lose).  That leaves
+// about as many as are asked for.  Where it does not (equal values, rising ones, NaN),
+// the chunk's cut is made exactly: the top-th largest (value, index) among the
+// threads' own, which lets at most PER top through.
+//
+// Measured at 2048 rows of 32000 fp32 logits, top 8: see the launch below.
+template <class T, int PER, bool VEC>
+__global__ __launch_bounds__(kBlock, 4) void k_logprobs(LogprobArgs a) {
+  using C = Chunk<T, PER, VEC>;
   __shared__ uint64_t cand[kCand];
   __shared__ uint64_t maxima[kBlock];
   __shared__ uint64_t best[AIO_MAX_TOP];
-  __shared__ uint64_t cut;
+  __shared__ uint32_t group_max[2][kBlock / 4];
+  __shared__ uint64_t cut_s;
   __shared__ int n_cand;
   __shared__ Stats ws[kBlock / AIO_WAVE];
-  const int tid = threadIdx.x, row = blockIdx.y, slice = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int row = blockIdx.y, slice = blockIdx.x;
   const T* x = (const T*)a.x + row * a.stride;
   const int lo = slice * a.per, hi = min(a.n, lo + a.per);
   Stats st{-INFINITY, 0.0, 0.0};
   if (tid < AIO_MAX_TOP) best[tid] = 0;
-  for (int c0 = lo; c0 < hi; c0 += kChunk) {
-    float v[kPer];
-    float m = -INFINITY;
+  if (tid == 0) n_cand = 0;
+  int parity = 0;
+  for (int c0 = lo; c0 < hi; c0 += C::N, parity ^= 1) {
+    C c;
+    c.load(x, c0, hi);
+    float m = c.v[0];
+    bool nan = c.v[0] != c.v[0];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = c0 + i * kBlock + tid;
-      v[i] = e < hi ? load1(x, e) : -INFINITY;
-      m = fmaxf(m, v[i]);
+    for (int i = 1; i < PER; ++i) {
+      m = fmaxf(m, c.v[i]);
+      nan |= c.v[i] != c.v[i];
     }
     Stats s{m, 0.0, 0.0};
-    bool nan = false;
+    if (nan) {
+      s.z = s.w = (double)__uint_as_float(0x7fc00000u);
+    } else if (m != -INFINITY) {
+      // z in 64 bits, so that a 1 does not swallow the rest; w's terms are 0 there.
+      // e^-150 is 0: the clamp only keeps 0 x -inf out of w
+      float w = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) nan |= v[i] != v[i];
-    if (m != -INFINITY || nan) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const float d = v[i] - m;
-        const float e = expf(d);
+      for (int i = 0; i < PER; ++i) {
+        const float d = fmaxf(c.v[i] - m, -150.f);
+        const float e = __builtin_amdgcn_exp2f(d * kLog2e);
         s.z += (double)e;
-        s.w += v[i] == -INFINITY ? 0.0 : (double)e * (double)d;
+        w = fmaf(e, d, w);
       }
+      s.w = (double)w;
+      if (m == INFINITY) s.z = (double)__uint_as_float(0x7fc00000u);
     }
     st = join(st, s);
-    if (a.top > 0) {
+    if (a.top == 0) continue;
+    // the largest of the thread as a sortable number, 0 for none
+    const uint32_t mine = nan ? 0xffffffffu
+                              : (C::index(c0, 0) < hi ? (uint32_t)(order_key(m, 0) >> 32) : 0u);
+    uint32_t g = max(mine, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0xB1, 0xF, 0xF, false));
+    g = max(g, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)g, 0x4E, 0xF, 0xF, false));
+    if ((tid & 3) == 0) group_max[parity][tid / 4] = g;
+    __syncthreads();  // (also: the chunk before is ranked, n_cand is 0)
+    g = group_max[parity][lane];
+    uint32_t cut;
+    const uint64_t kth = best[a.top - 1];
+    if (kth) {
+      cut = (uint32_t)(kth >> 32);
+      if (cut != 0xffffffffu) ++cut;
+      if (!__any(g >= cut)) continue;
+    } else {
+      int r = 0;
+#pragma unroll 8
+      for (int j = 0; j < kBlock / 4; ++j) {
+        const uint32_t o = group_max[parity][j];
+        r += o > g || (o == g && j < lane);
+      }
+      const uint64_t at = __ballot(r == a.top - 1);
+      cut = __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)at) - 1);
+      if (cut == 0) cut = 1;
+    }
+    bool exact = __any(g == 0xffffffffu);
+    if (!exact) {
+      if (mine >= cut) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const uint64_t k = order_key(c.v[i], C::index(c0, i));
+          if ((uint32_t)(k >> 32) >= cut && C::index(c0, i) < hi) {
+            const int to = atomicAdd(&n_cand, 1);
+            if (to < kCand - AIO_MAX_TOP) cand[to] = k;
+          }
+        }
+      }
+      __syncthreads();
+      exact = n_cand > kCand - AIO_MAX_TOP;
+    }
+    if (exact) {
       uint64_t mk = 0;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = c0 + i * kBlock + tid;
-        if (e < hi) mk = max(mk, order_key(v[i], e));
-      }
-      __syncthreads();  // the chunk before is ranked
+      for (int i = 0; i < PER; ++i)
+        if (C::index(c0, i) < hi) mk = max(mk, order_key(c.v[i], C::index(c0, i)));
+      __syncthreads();  // every thread has read n_cand
       maxima[tid] = mk;
       if (tid == 0) {
-        cut = 0;
+        cut_s = 1;
         n_cand = 0;
       }
       __syncthreads();
       int r = 0;
       for (int j = 0; j < kBlock; ++j) r += maxima[j] > mk;
-      if (mk && r == a.top - 1) cut = mk;
+      if (mk && r == a.top - 1) cut_s = mk;
       __syncthreads();
-      // (fewer than `top` threads with values: cut is 0, and all values are candidates)
-      const uint64_t from = max(cut, best[a.top - 1]);
+      const uint64_t from = max(cut_s, kth);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = c0 + i * kBlock + tid;
-        if (e < hi) {
-          const uint64_t k = order_key(v[i], e);
-          if (k >= from) cand[atomicAdd(&n_cand, 1)] = k;
-        }
+      for (int i = 0; i < PER; ++i) {
+        const uint64_t k = order_key(c.v[i], C::index(c0, i));
+        if (k >= from && C::index(c0, i) < hi) cand[atomicAdd(&n_cand, 1)] = k;
       }
-      if (tid < a.top && best[tid]) cand[atomicAdd(&n_cand, 1)] = best[tid];
       __syncthreads();
-      rank_candidates(cand, n_cand, a.top, best);
     }
+    // the best so far join them
+    const int n = n_cand;
+    const uint64_t old = tid < a.top ? best[tid] : 0;
+    const int have = __popcll(__ballot(old != 0));  // (a prefix; wave 0 holds them all)
+    if (old) cand[n + tid] = old;
+    if (tid == 0) maxima[0] = have;
+    __syncthreads();
+    rank_candidates(cand, n + (int)maxima[0], a.top, best);
+    if (tid == 0) n_cand = 0;
   }
   st = wave_join(st);
-  if ((tid & (AIO_WAVE - 1)) == 0) ws[tid / AIO_WAVE] = st;
+  if (lane == 0) ws[tid / AIO_WAVE] = st;
   __syncthreads();
   st = ws[0];
 #pragma unroll
@@ -197,24 +294,30 @@ __global__ __launch_bounds__(kBlock) void k_logprobs(LogprobArgs a) {
   if (tid < a.top) a.part_top[at * a.top + tid] = best[tid];
 }
 
-// One workgroup per row: joins its slices.
+// One workgroup per row: joins its slices (at most 64).
 template <class T>
 __global__ __launch_bounds__(kBlock) void k_logprobs_join(LogprobArgs a) {
-  __shared__ uint64_t cand[kCand];
+  __shared__ uint64_t cand[kMaxSlices * AIO_MAX_TOP];
   __shared__ uint64_t best[AIO_MAX_TOP];
-  const int tid = threadIdx.x, row = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1), row = blockIdx.x;
   const int64_t at = (int64_t)row * a.slices;
-  Stats st{-INFINITY, 0.0, 0.0};
-  for (int s = 0; s < a.slices; ++s) {
-    const double* p = a.part + (at + s) * 3;
-    st = join(st, Stats{(float)p[0], p[1], p[2]});
-  }
   const int n = a.slices * a.top;
   for (int i = tid; i < n; i += kBlock) cand[i] = a.part_top[at * a.top + i];
+  Stats st{-INFINITY, 0.0, 0.0};
+  if (lane < a.slices) {
+    const double* p = a.part + (at + lane) * 3;
+    st = Stats{(float)p[0], p[1], p[2]};
+  }
+  st = wave_join(st);
   __syncthreads();
   rank_candidates(cand, n, a.top, best);
   __syncthreads();
   finish_row<T>(a, row, st, best);
+}
+
+template <class T, int PER, bool VEC>
+void launch_slices(const LogprobArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((k_logprobs<T, PER, VEC>), dim3(a.slices, a.rows), dim3(kBlock), 0, stream, a);
 }
 
 template <class T>
@@ -230,7 +333,11 @@ void launch(const LogprobArgs& a, hipStream_t stream) {
       b.ids = a.ids + (int64_t)r0 * a.top;
       b.top_lp = a.top_lp + (int64_t)r0 * a.top;
     }
-    hipLaunchKernelGGL(k_logprobs<T>, dim3(a.slices, b.rows), dim3(kBlock), 0, stream, b);
+    const bool vec = ((uintptr_t)b.x | (uintptr_t)(b.stride * sizeof(T))) % 16 == 0;
+    if (a.slices > 1)
+      vec ? launch_slices<T, kPerFew, true>(b, stream) : launch_slices<T, kPerFew, false>(b, stream);
+    else
+      vec ? launch_slices<T, kPer, true>(b, stream) : launch_slices<T, kPer, false>(b, stream);
     if (a.slices > 1)
       hipLaunchKernelGGL(k_logprobs_join<T>, dim3(b.rows), dim3(kBlock), 0, stream, b);
   }
@@ -240,12 +347,12 @@ void launch(const LogprobArgs& a, hipStream_t stream) {
 
 LogprobPlan aio_logprob_plan(int rows, int n, int top) {
   LogprobPlan p{1, std::max(n, 1), 0};
-  const int chunks = (n + kChunk - 1) / kChunk;
   // few rows: a row goes to several workgroups, each at least one chunk
-  const int want = std::max(1, std::min({chunks, kCUs / std::max(rows, 1), 32}));
+  constexpr int chunk = kBlock * kPerFew;
+  const int chunks = (n + chunk - 1) / chunk;
+  const int want = std::min({chunks, 2 * kCUs / std::max(rows, 1), kMaxSlices});
   if (want > 1) {
-    const int each = (chunks + want - 1) / want;
-    p.per = each * kChunk;
+    p.per = (chunks + want - 1) / want * chunk;
     p.slices = (n + p.per - 1) / p.per;
   }
   if (p.slices > 1) p.ws = (size_t)std::min(rows, 65535) * p.slices * (24 + 8 * (size_t)top);

@@ -87,12 +87,14 @@ def check_attention(got, lse, ref, what=""):
 
 
 def logprobs64(x, targets, top):
-    """(logprob, entropy, ids, top_logprobs, tolerances) of fp32/bf16 rows.
+    """(logprob, entropy, ids, top_logprobs, lp_tol, ent_tol) of fp32/bf16 rows.
 
-    Tolerances.  A term of the sum is off by 2^-22 of itself and by the rounding
-    of its argument, u |d| e^d <= u; sums are 64 bits: log z is off by 2^-21 at
-    most.  The weighted sum's terms are off alike: 2^-21 (1 + |w / z|).
-    Results round once."""
+    Tolerances.  With d = x - m, W = sum p |d|, W2 = sum p d^2: a term e^d is
+    off by 2^-23 of itself (the exponential) and |d| (2^-24 + 2^-25) (the rounded
+    product d log2 e, the rounded constant), and d by 2^-24 |d|; so log z is off
+    by at most 2^-23 + 2^-22 W.  The terms of the weighted sum are off alike and by the
+    rounding of up to 32 additions: 2^-23 W + 2^-22 W2 + 2^-19 W.  A result is
+    rounded once, 2^-24 of itself."""
     x = x.double()
     m = x.amax(-1, keepdim=True)
     # against the maximum, not against the log-sum-exp itself: next to logits of
@@ -102,7 +104,10 @@ def logprobs64(x, targets, top):
     p = y.exp()
     ent = -torch.where(p > 0, p * y, torch.zeros_like(y)).sum(-1)
     ent = torch.where(torch.isfinite(logz), ent, torch.full_like(ent, math.nan))
-    w = (ent - logz).abs()
+    d = torch.where(p > 0, x - m, torch.zeros_like(y))
+    W, W2 = (p * d.abs()).sum(-1), (p * d * d).sum(-1)
+    lp_tol = 2.0 ** -23 + 2.0 ** -22 * W
+    ent_tol = lp_tol + 2.0 ** -18 * W + 2.0 ** -22 * W2
     order = torch.from_numpy(np.argsort(
         np.where(np.isnan(x.numpy()), -math.inf, -x.numpy()), axis=-1, kind="stable"))
     # NaN first, in index order (argsort puts -inf first; real +Inf come after NaN)
@@ -117,7 +122,7 @@ def logprobs64(x, targets, top):
         ok = (targets >= 0) & (targets < x.shape[1])
         lp = y.gather(1, targets.clamp(0, x.shape[1] - 1).long()[:, None])[:, 0]
         lp = torch.where(ok, lp, torch.full_like(lp, math.nan))
-    return lp, ent, ids, y.gather(1, ids), w
+    return lp, ent, ids, y.gather(1, ids), lp_tol, ent_tol
 
 
 def close(got, want, tol):

@@ -24,13 +24,13 @@ def run(x, targets, top, ws=None):
 
 def check(x, targets, top, device_x=None):
     lp, ent, ids, tlp = run(x.cuda() if device_x is None else device_x, targets, top)
-    wlp, went, wids, wtlp, w = logprobs64(x, targets, top)
-    close(ent, went, 2.0 ** -21 * (1 + w) + 2.0 ** -24 * went.abs())
+    wlp, went, wids, wtlp, ltol, etol = logprobs64(x, targets, top)
+    close(ent, went, etol + 2.0 ** -24 * went.abs())
     if targets is not None:
-        close(lp, wlp, 2.0 ** -21 + 2.0 ** -24 * wlp.abs())
+        close(lp, wlp, ltol + 2.0 ** -24 * wlp.abs())
     if top:
         assert torch.equal(ids.cpu().long(), wids)
-        close(tlp, wtlp, 2.0 ** -21 + 2.0 ** -24 * wtlp.abs())
+        close(tlp, wtlp, ltol[:, None] + 2.0 ** -24 * wtlp.abs())
 
 
 SHAPES = [(1, 1, 1), (1, 2, 2), (3, 7, 5), (2, 64, 32), (5, 255, 1), (4, 256, 32), (1, 8192, 8),
@@ -99,7 +99,7 @@ def test_confident_rows(gap):
     x[1, 4999] = gap
     t = torch.tensor([17, 4999], dtype=torch.int32)
     lp, ent, _, _ = run(x.cuda(), t, 0)
-    wlp, went, _, _, w = logprobs64(x, t, 0)
+    _, went, _, _, _, _ = logprobs64(x, t, 0)
     exact = -math.log1p(4999 * math.exp(-gap))
     # a 32-bit e^-gap is off by its argument's rounding (24 bits of `gap`) and 2^-22
     rel = 2.0 ** -23 * gap + 2.0 ** -20
