@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -100,7 +101,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // the split, and the waves' states join in LDS.
 template <int HD>
 struct StepLds {
-  static constexpr int VROW = HD * 2 + 16;        // bytes of a value row
+  static constexpr int VROW = HD * 2 + 32;        // bytes of a value row: 8 rows in distinct banks
   static constexpr int VBYTES = 32 * VROW;        // a wave's value tile
   static constexpr int OROW = HD + 4;             // floats of an output row
   static constexpr int OBYTES = kWaves * kMaxGroup * OROW * 4;
@@ -299,10 +300,14 @@ __global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
 constexpr int kRows = kWaves * 32;
 constexpr int kKeys = 64;
 
+// Two buffers of a key and of a value tile: while one is multiplied, the next is
+// written.  The row pitches put the rows that one LDS access takes (16 of the keys,
+// 4 of the values) into distinct banks.
 template <int HD>
 struct RowsLds {
-  static constexpr int ROW = HD * 2 + 16;  // bytes of a key or value row
-  static constexpr int TILE = kKeys * ROW;
+  static constexpr int KROW = HD * 2 + 16, VROW = HD * 2 + 64;  // bytes
+  static constexpr int KBYTES = kKeys * KROW, VBYTES = kKeys * VROW;
+  static constexpr int BYTES = 2 * (KBYTES + VBYTES);
 };
 
 // Tile `t` of the launch: its sequence, the tile within it and how many the
@@ -326,12 +331,13 @@ AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile, int& tiles
     const uint64_t past = __ballot(incl > t);
     if (past) {
       const int at = __ffsll((unsigned long long)past) - 1;
+      // (lane reads, not shuffles: what follows from them is scalar)
       seq = base + at;
-      tiles = __shfl(n, at, AIO_WAVE);
-      tile = t - (__shfl(incl, at, AIO_WAVE) - tiles);
+      tiles = __builtin_amdgcn_readlane(n, at);
+      tile = t - (__builtin_amdgcn_readlane(incl, at) - tiles);
       return true;
     }
-    t -= __shfl(incl, AIO_WAVE - 1, AIO_WAVE);
+    t -= __builtin_amdgcn_readlane(incl, AIO_WAVE - 1);
   }
   return false;
 }
@@ -344,17 +350,22 @@ AIO_DEV bool not_finite(u32x4 w) {  // of eight bf16
   return bad;
 }
 
+// A row's weights refer to a maximum that is raised only when it would be passed by
+// 2^kSlack: weights then reach 2^kSlack instead of 1, which costs no precision (they
+// are floating point), and the outputs are rarely rescaled (in the first few dozen
+// blocks nearly every block raises the maximum of one of a wave's 32 rows).
+constexpr float kSlack = 8.f;
+
 template <int HD, int NT, bool PAGED>
 __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   using L = RowsLds<HD>;
-  __shared__ __align__(16) char kt_s[L::TILE];
-  __shared__ __align__(16) char vt_s[L::TILE];
+  extern __shared__ __align__(16) char smem[];
   __shared__ uint8_t seen[kKeys];
-  __shared__ int flags[2];
   constexpr int NC = HD / 16;                      // k chunks of a score product
   constexpr int NHB = HD / 32;                     // output tiles
   constexpr int TPR = HD / 8;                      // threads of a row
   constexpr int RPP = kBlock / TPR;                // rows per pass
+  constexpr int RPW = AIO_WAVE / TPR;              // ... of a wave: 4 or 8, all in one page
   constexpr int NP = kKeys / RPP;                  // passes of a tile
   const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
@@ -398,167 +409,280 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
   for (int c = 0; c < NC; ++c)
     load_query<NT>(a, first + row, h0 + g, HD, c * 16 + 8 * kh, live, q[c]);
 
-  // staging: pass p of this thread is row p RPP + tid / TPR, 8 dims
-  const int sr = tid / TPR, sd = tid % TPR * 8;
-  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride + sd;
-  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride + sd;
+  // staging: pass p of this wave is rows p RPP + wid RPW .. + RPW - 1, of a lane 16
+  // bytes of one
+  const int wr = wid * RPW, lr = lane / TPR, sd = lane % TPR * 8;
+  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride;
+  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride;
+  const int64_t lane_at = PAGED ? lr * HD + sd : lr * a.kv.stride + sd;
   const int32_t* table = PAGED ? a.kv.table + (int64_t)seq * a.kv.tstride : nullptr;
-  int page[NP];
-  u32x4 kr[NP], vr[NP];
-  uint32_t ok = 0;  // bit p: the row of pass p is there
-  auto load_pages = [&](int t) {
-    if constexpr (PAGED) {
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int key = t * kKeys + p * RPP + sr;
-        page[p] = key < len && t < t1 ? table[key >> a.kv.shift] : -1;
-      }
+  const int pmask = (1 << a.kv.shift) - 1;
+
+  // Plain tiles t0 .. tp - 1: every row sees every key of them.
+  int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
+  if constexpr (PAGED) {
+    // (not with holes among them)
+    if (tp > t0) {
+      bool hole = false;
+      const int e1 = (tp * kKeys - 1) >> a.kv.shift;
+      for (int e = (t0 * kKeys >> a.kv.shift) + tid; e <= e1; e += kBlock)
+        hole |= (unsigned)table[e] >= (unsigned)a.kv.limit;
+      if (__syncthreads_or(hole)) tp = t0;
     }
-  };
-  auto load_tile = [&](int t) {
-    ok = 0;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int key = t * kKeys + p * RPP + sr;
-      bool there = key < len;
-      int64_t at;
-      if constexpr (PAGED) {
-        there = (unsigned)page[p] < (unsigned)a.kv.limit;
-        at = page[p] * a.kv.stride + (int64_t)(key & ((1 << a.kv.shift) - 1)) * HD;
-      } else {
-        at = (int64_t)(key0 + key) * a.kv.stride;
-      }
-      kr[p] = vr[p] = u32x4{0, 0, 0, 0};
-      if (there) {
-        kr[p] = *(const u32x4*)(kb + at);
-        vr[p] = *(const u32x4*)(vb + at);
-        ok |= 1u << p;
-      }
-    }
-  };
+  }
+
   f32x16 o[NHB];
 #pragma unroll
   for (int hb = 0; hb < NHB; ++hb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[hb][i] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  const char* vtr = vt_s + (4 * kh + (lane & 15) / 4) * L::ROW +
-                    ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
-
-  if (tid < 2) flags[tid] = 0;
-  if (t0 < t1) {
-    load_pages(t0);
-    load_tile(t0);
-    load_pages(t0 + 1);
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int j0 = t * kKeys;
-    __syncthreads();  // every wave is done with the tile before
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      *(u32x4*)(kt_s + (p * RPP + sr) * L::ROW + sd * 2) = kr[p];
-      *(u32x4*)(vt_s + (p * RPP + sr) * L::ROW + sd * 2) = vr[p];
-      if (sd == 0) seen[p * RPP + sr] = ok >> p & 1;
-    }
-    // 1: keys are missing; 2: values that are not finite where some rows may not see
-    // them (they must not meet a weight of 0 in a product)
-    int f = ok != (1u << NP) - 1 ? 1 : 0;
-    if (j0 + kKeys - 1 > all_lim) {
-#pragma unroll
-      for (int p = 0; p < NP; ++p) f |= not_finite(vr[p]) ? 2 : 0;
-    }
-    if (f) atomicOr(&flags[t & 1], f);
-    __syncthreads();
-    const int flag = __builtin_amdgcn_readfirstlane(flags[t & 1]);
-    if (tid == 0) flags[~t & 1] = 0;
-    if (t + 1 < t1) {
-      load_tile(t + 1);
-      load_pages(t + 2);
-    }
-    if (j0 > wave_lim) continue;
-
-    f32x16 s[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 ak =
-            as_bf16x8(*(const u32x4*)(kt_s + (b * 32 + rl) * L::ROW + (c * 16 + 8 * kh) * 2));
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
-      }
-    }
-    // key of score v of block b: j0 + 32 b + 8 (v / 4) + 4 kh + v mod 4
-    if (j0 + kKeys - 1 > all_lim || flag) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
-          if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
-        }
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[b][v]);
+  float m = -INFINITY, l = 0.f;  // m: reference of the weights, in log2 units
+  const int st_at = (wr + lr) * L::KROW + sd * 2, sv_at = (wr + lr) * L::VROW + sd * 2;
+  const int k_at = rl * L::KROW + 16 * kh;
+  const int v_at = (4 * kh + (lane & 15) / 4) * L::VROW +
+                   ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+  auto key_frag = [&](int buf, int i) {  // i: block of 32 keys, chunk of 16 dims
+    return as_bf16x8(*(const u32x4*)(smem + buf * L::KBYTES + k_at + i / NC * 32 * L::KROW +
+                                     i % NC * 32));
+  };
+  auto value_frag = [&](int buf, int i) {  // i: chunk of 16 keys, tile of 32 dims
+    const char* v = smem + 2 * L::KBYTES + buf * L::VBYTES + v_at + i / NHB * 16 * L::VROW +
+                    i % NHB * 64;
+    const uint2 v0 = lds_read_tr16(v), v1 = lds_read_tr16(v + 8 * L::VROW);
+    return as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+  };
+  // The reference of a tile whose largest score in this lane is mx.
+  auto refer = [&](float mx) {
     float other = mx;
     swap32(mx, other);
-    mx = fmaxf(mx, other);
-    const float mnew = fmaxf(m, mx);
-    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
-    if (__any(mnew > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+    mx = fmaxf(mx, other) * a.scale_log2;
+    const bool raise = mx > m + kSlack;  // (the first visible key: above -inf)
+    if (__any(raise)) {
+      const float mnew = raise ? mx : m;
+      // (o holds nothing but what is not finite before the first visible key)
+      const float c = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mnew);
+      m = mnew;
       l *= c;
 #pragma unroll
       for (int hb = 0; hb < NHB; ++hb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[hb][i] *= c;
     }
-    m = mnew;
+    return m == -INFINITY ? 0.f : m;
+  };
+
+  if (tp > t0) {
+    // Tile t into registers: no branches, tiles past the last read it again.
+    auto load_tile = [&](u32x4 (&r)[NP], const uint16_t* from, int t) {
+      const int key = min(t, tp - 1) * kKeys + wr;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if constexpr (PAGED) {
+          const int kp = key + p * RPP;
+          const int64_t at = table[kp >> a.kv.shift] * a.kv.stride + (int64_t)(kp & pmask) * HD;
+          r[p] = *(const u32x4*)(from + at + (uint32_t)lane_at);
+        } else {
+          r[p] = *(const u32x4*)(from + (int64_t)(key0 + key + p * RPP) * a.kv.stride + lane_at);
+        }
+      }
+    };
+    auto store_keys = [&](const u32x4 (&r)[NP], int buf) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        *(u32x4*)(smem + buf * L::KBYTES + st_at + p * RPP * L::KROW) = r[p];
+    };
+    auto store_values = [&](const u32x4 (&r)[NP], int buf) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        *(u32x4*)(smem + 2 * L::KBYTES + buf * L::VBYTES + sv_at + p * RPP * L::VROW) = r[p];
+    };
+    u32x4 kr[NP], vr[NP];
+    float mx;
+    // One tile: its softmax while the next tile's scores (sn) are multiplied, then
+    // its values while the next tile's maximum is taken.  Score v of block b is key 32 b +
+    // 8 (v / 4) + 4 kh + v mod 4 of the tile.
+    auto step = [&](int t, auto buf_c, f32x16 (&s)[2], f32x16 (&sn)[2]) {
+      constexpr int buf = decltype(buf_c)::value;
+      // K of t + 1 and V of t are in their buffers; every wave is done with K of t and
+      // V of t - 1, whose buffers take K of t + 2 and V of t + 1
+      __syncthreads();
+      store_keys(kr, buf);
+      store_values(vr, buf ^ 1);
+      const float mref = refer(mx);
+      // Matrix instructions with a few vector instructions behind each: those then
+      // cost next to nothing (8 of these MFMAs with 16 exponentials among them
+      // take as long as without, with 48 multiply-adds 14 % longer; one kind after the
+      // other, two waves per SIMD hide about half).  LDS reads run two ahead.
+      bf16x8 pt[4][NT];
+      bf16x8 ak[3];
+      ak[0] = key_frag(buf ^ 1, 0);
+      ak[1] = key_frag(buf ^ 1, 1);
+#pragma unroll
+      for (int i = 0; i < 2 * NC; ++i) {
+        if (i + 2 < 2 * NC) ak[(i + 2) % 3] = key_frag(buf ^ 1, i + 2);
+        if (i % NC == 0) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sn[i / NC][e] = 0.f;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sn[i / NC] = mfma32(ak[i % 3], q[i % NC][n], sn[i / NC]);
+        constexpr int E = 16 / NC;  // scores of this step
+#pragma unroll
+        for (int e = i * E; e < (i + 1) * E; ++e) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale_log2, -mref));
+          s[e / 16][e % 16] = x;
+          l += x;
+        }
+        if ((i + 1) * E % 8 == 0) {
+          const int c = ((i + 1) * E - 1) / 8;
+          float p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = s[c / 2][8 * (c & 1) + e];
+          terms<NT>(p, pt[c]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      load_tile(kr, kb, t + 3);
+      load_tile(vr, vb, t + 2);
+      bf16x8 av[3];
+      av[0] = value_frag(buf, 0);
+      av[1] = value_frag(buf, 1);
+      mx = sn[0][0];
+#pragma unroll
+      for (int i = 0; i < 4 * NHB; ++i) {
+        if (i + 2 < 4 * NHB) av[(i + 2) % 3] = value_frag(buf, i + 2);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[i % NHB] = mfma32(av[i % 3], pt[i / NHB][n], o[i % NHB]);
+        constexpr int E = 32 / (4 * NHB);  // scores of the next tile to take the maximum of
+#pragma unroll
+        for (int e = i * E; e < (i + 1) * E; ++e) mx = fmaxf(mx, sn[e / 16][e % 16]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // (buffers by t - t0's parity: K of t0 in 0, of t0 + 1 in 1, V of t0 in 0)
+    f32x16 sa[2], sb[2];
+    load_tile(kr, kb, t0);
+    load_tile(vr, vb, t0);
+    store_keys(kr, 0);
+    store_values(vr, 0);
+    load_tile(kr, kb, t0 + 1);
+    store_keys(kr, 1);
+    load_tile(kr, kb, t0 + 2);
+    load_tile(vr, vb, t0 + 1);
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sa[b][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 ak = key_frag(0, b * NC + c);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sa[b] = mfma32(ak, q[c][n], sa[b]);
+      }
+    }
+    mx = sa[0][0];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[b][v] = __builtin_amdgcn_exp2f(fmaf(s[b][v], a.scale_log2, -mref));
-        l += s[b][v];
-      }
-    if (flag & 2) {
-      // one key at a time, for the rows that see it
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            const int kk = 32 * b + 8 * (v / 4) + 4 * half + v % 4;
-            const float w = __shfl(s[b][v], rl + 32 * half, AIO_WAVE);
-            if (j0 + kk > lim || !seen[kk]) continue;
-#pragma unroll
-            for (int hb = 0; hb < NHB; ++hb)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int d = hb * 32 + 8 * (i / 4) + 4 * kh + i % 4;
-                o[hb][i] += w * bf16_to_f32(*(const uint16_t*)(vt_s + kk * L::ROW + d * 2));
-              }
-          }
-      continue;
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sa[b][v]);
+    int t = t0;
+    for (; t + 1 < tp; t += 2) {
+      step(t, std::integral_constant<int, 0>{}, sa, sb);
+      step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
     }
+    if (t < tp) step(t, std::integral_constant<int, 0>{}, sa, sb);
+  }
+
+  // The other tiles, one after the other: at the causal edge or the keys' end, or with
+  // holes.
+  for (int t = tp; t < t1; ++t) {
+    const int j0 = t * kKeys;
+    u32x4 kr[NP], vr[NP];
+    uint32_t ok = 0;  // bit p: the row of pass p is there
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int key = j0 + p * RPP + wr;
+      bool there = key + lr < len;
+      int64_t at = (int64_t)(key0 + key) * a.kv.stride;
+      if constexpr (PAGED) {
+        const int page = key < len ? table[key >> a.kv.shift] : -1;
+        there &= (unsigned)page < (unsigned)a.kv.limit;
+        at = page * a.kv.stride + (int64_t)(key & pmask) * HD;
+      }
+      kr[p] = vr[p] = u32x4{0, 0, 0, 0};
+      if (there) {
+        kr[p] = *(const u32x4*)(kb + at + lane_at);
+        vr[p] = *(const u32x4*)(vb + at + lane_at);
+        ok |= 1u << p;
+      }
+    }
+    __syncthreads();  // every wave is done with the tile before
+    bool odd = false;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      *(u32x4*)(smem + st_at + p * RPP * L::KROW) = kr[p];
+      *(u32x4*)(smem + 2 * L::KBYTES + sv_at + p * RPP * L::VROW) = vr[p];
+      if (sd == 0) seen[p * RPP + wr + lr] = ok >> p & 1;
+      odd |= not_finite(vr[p]);
+    }
+    if (__syncthreads_or(odd)) {
+      // Values that are not finite must not meet a weight of 0 in a product: they go
+      // straight to the rows that see them, and out of the tile.
+      char* v = smem + 2 * L::KBYTES;
+#pragma unroll 1
+      for (int kk = 0; kk < kKeys; ++kk) {
+        if (j0 + kk > lim || !seen[kk]) continue;
+#pragma unroll
+        for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int d = hb * 32 + 8 * (i / 4) + 4 * kh + i % 4;
+            const uint16_t x = *(const uint16_t*)(v + kk * L::VROW + d * 2);
+            if ((x & 0x7f80u) == 0x7f80u) o[hb][i] += bf16_to_f32(x);
+          }
+      }
+      __syncthreads();
+      for (int e = tid; e < kKeys * HD; e += kBlock) {
+        uint16_t* x = (uint16_t*)(v + e / HD * L::VROW) + e % HD;
+        if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
+      }
+      __syncthreads();
+    }
+    if (j0 > wave_lim) continue;
+    f32x16 s[2];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 ak = key_frag(0, b * NC + c);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
+        if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
+        mx = fmaxf(mx, s[b][v]);
+      }
+    }
+    const float mref = refer(mx);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[c / 2][8 * (c & 1) + e];
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(s[c / 2][8 * (c & 1) + e], a.scale_log2, -mref));
+        l += p[e];
+      }
       bf16x8 pt[NT];
       terms<NT>(p, pt);
 #pragma unroll
       for (int hb = 0; hb < NHB; ++hb) {
-        const uint2 v0 = lds_read_tr16(vtr + 16 * c * L::ROW + hb * 64);
-        const uint2 v1 = lds_read_tr16(vtr + (16 * c + 8) * L::ROW + hb * 64);
-        const bf16x8 av = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+        const bf16x8 av = value_frag(0, c * NHB + hb);
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[hb] = mfma32(av, pt[n], o[hb]);
       }
@@ -571,7 +695,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
   if (a.S > 1) {
     const int64_t at = (int64_t)split * a.n_rows * a.H + rh;
     if (kh == 0) {
-      a.part_ml[at * 2] = m * a.scale_log2;
+      a.part_ml[at * 2] = m;
       a.part_ml[at * 2 + 1] = l;
     }
     if (m == -INFINITY) return;
@@ -585,7 +709,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
   }
   const bool none = l == 0.f;  // no visible key
   const float inv = none ? 0.f : 1.f / l;
-  if (kh == 0 && a.lse) a.lse[rh] = none ? -INFINITY : m * a.scale_log2 * kLn2 + logf(l);
+  if (kh == 0 && a.lse) a.lse[rh] = none ? -INFINITY : m * kLn2 + logf(l);
   const int64_t to = (int64_t)(first + row) * a.ldo + (int64_t)(h0 + g) * HD + 4 * kh;
 #pragma unroll
   for (int hb = 0; hb < NHB; ++hb)
@@ -662,17 +786,26 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
 }
 
+template <int HD, int NT, bool PAGED>
+hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  constexpr int lds = RowsLds<HD>::BYTES;
+  const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<HD, NT, PAGED>,
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_attn_rows<HD, NT, PAGED>), dim3((unsigned)p.groups), dim3(kBlock), lds,
+                     stream, a);
+  return hipGetLastError();
+}
+
 template <int HD, int NT>
 hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  if (!p.rows)
+  hipError_t e;
+  if (!p.rows) {
     hipLaunchKernelGGL((k_attn_step<HD, NT>), dim3((unsigned)p.groups), dim3(kBlock), 0, stream, a);
-  else if (a.kv.table)
-    hipLaunchKernelGGL((k_attn_rows<HD, NT, true>), dim3((unsigned)p.groups), dim3(kBlock), 0,
-                       stream, a);
-  else
-    hipLaunchKernelGGL((k_attn_rows<HD, NT, false>), dim3((unsigned)p.groups), dim3(kBlock), 0,
-                       stream, a);
-  hipError_t e = hipGetLastError();
+    e = hipGetLastError();
+  } else {
+    e = a.kv.table ? launch_rows<HD, NT, true>(a, p, stream) : launch_rows<HD, NT, false>(a, p, stream);
+  }
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t rh = (int64_t)a.n_rows * a.H;
   hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
