@@ -294,10 +294,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
 
 // A sequence's rows and the G heads of a kv head form one list of q G packed
 // rows (row-major: packed row r G + g is row r of head h0 + g), cut into tiles of
-// kRows; workgroup (tile, kv head, split).  Each wave owns 32 packed rows (the columns of
-// 32-wide tiles) and all of them share the key and value tiles in LDS, kKeys keys
+// 32 W; workgroup (tile, kv head, split) of W waves.  Each wave owns 32 packed rows (the
+// columns of 32-wide tiles) and all of them share the key and value tiles in LDS, kKeys keys
 // at a time, the next ones in flight in registers.
-constexpr int kRows = kWaves * 32;
 constexpr int kKeys = 64;
 
 // Two buffers of a key and of a value tile: while one is multiplied, the next is
@@ -310,17 +309,61 @@ struct RowsLds {
   static constexpr int BYTES = 2 * (KBYTES + VBYTES);
 };
 
-// Tile `t` of the launch: its sequence, the tile within it and how many the
-// sequence has; false behind the last.
-AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile, int& tiles) {
+// First key and number of keys of sequence i.
+template <bool PAGED>
+AIO_DEV void seq_keys(const AttnArgs& a, int i, int& key0, int& len) {
+  if constexpr (PAGED) {
+    key0 = 0;
+    len = paged_len(a.kv, i, a.max_len);
+  } else {
+    key0 = min(max(a.kv.cu_k[i], 0), a.kv.limit);
+    len = min(max(min(a.kv.cu_k[i + 1], a.kv.limit) - key0, 0), a.max_len);
+  }
+}
+
+// Workgroups start in index order, and a causal tile's work grows with its last
+// position: the longest first.  Tile `t` of the launch in that order, for up to 64
+// sequences: a tile's level is its number in the sequence plus the rows in tiles
+// that the sequence has had before; the tiles of the highest level come first (eight
+// packed prompts of 540 to 2048 rows, sequence after sequence: 134 us, so 124).  With
+// more sequences they come one after the other, each from its end.
+// seq and tile receive its place; false behind the last.
+template <int ROWS, bool PAGED>
+AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile) {
   const int lane = threadIdx.x & (AIO_WAVE - 1);
   for (int base = 0; base < a.n_seqs; base += AIO_WAVE) {
     const int i = base + lane;
-    int n = 0;
+    int n = 0, first, count = 0;
     if (i < a.n_seqs) {
-      int first, count;
       seq_rows(a.cu_q, a.n_rows, i, first, count);
-      n = (int)(((int64_t)count * a.G + kRows - 1) / kRows);
+      n = (int)(((int64_t)count * a.G + ROWS - 1) / ROWS);
+    }
+    if (a.n_seqs <= AIO_WAVE && a.n_seqs > 1) {
+      int key0, len = 0;
+      if (n > 0) seq_keys<PAGED>(a, i, key0, len);
+      const int64_t before = (int64_t)max(len - count, 0) * a.G / ROWS;
+      const int lo = (int)min(before, (int64_t)1 << 22), hi = lo + n;
+      // tiles of at least level v (below 2^24 of them: exact)
+      auto from = [&](int v) {
+        return (int)__builtin_amdgcn_readfirstlane(
+            (int)wave_sum((float)max(hi - max(v, lo), 0)));
+      };
+      if (from(0) <= t) return false;
+      int at = 0, past = (int)wave_max((float)(n > 0 ? hi : 0));  // from(at) > t >= from(past)
+      past = __builtin_amdgcn_readfirstlane(past);
+      while (past - at > 1) {
+        const int mid = (at + past) / 2;
+        if (from(mid) > t) at = mid;
+        else past = mid;
+      }
+      const int r = t - from(at + 1);  // the r-th of the sequences with a tile of this level
+      const uint64_t has = __ballot(lo <= at && at < hi);
+      const int before_me = __popcll(has & ((1ull << lane) - 1));
+      const uint64_t me = __ballot((has >> lane & 1) && before_me == r);
+      if (!me) return false;  // (boundaries that overlap)
+      seq = __ffsll((unsigned long long)me) - 1;
+      tile = at - __builtin_amdgcn_readlane(lo, seq);
+      return true;
     }
     int incl = n;
 #pragma unroll
@@ -333,8 +376,7 @@ AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile, int& tiles
       const int at = __ffsll((unsigned long long)past) - 1;
       // (lane reads, not shuffles: what follows from them is scalar)
       seq = base + at;
-      tiles = __builtin_amdgcn_readlane(n, at);
-      tile = t - (__builtin_amdgcn_readlane(incl, at) - tiles);
+      tile = __builtin_amdgcn_readlane(incl, at) - 1 - t;
       return true;
     }
     t -= __builtin_amdgcn_readlane(incl, AIO_WAVE - 1);
@@ -356,37 +398,32 @@ AIO_DEV bool not_finite(u32x4 w) {  // of eight bf16
 // blocks nearly every block raises the maximum of one of a wave's 32 rows).
 constexpr float kSlack = 8.f;
 
-template <int HD, int NT, bool PAGED>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
+// Products by which LDS reads run ahead of their use.
+constexpr int kAhead = 4;
+
+template <int HD, int NT, bool PAGED, int W>
+__global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   using L = RowsLds<HD>;
+  constexpr int kThreads = W * AIO_WAVE, kRows = W * 32;
   extern __shared__ __align__(16) char smem[];
   __shared__ uint8_t seen[kKeys];
   constexpr int NC = HD / 16;                      // k chunks of a score product
   constexpr int NHB = HD / 32;                     // output tiles
   constexpr int TPR = HD / 8;                      // threads of a row
-  constexpr int RPP = kBlock / TPR;                // rows per pass
+  constexpr int RPP = kThreads / TPR;                // rows per pass
   constexpr int RPW = AIO_WAVE / TPR;              // ... of a wave: 4 or 8, all in one page
   constexpr int NP = kKeys / RPP;                  // passes of a tile
   const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
   const int rl = lane & 31, kh = lane >> 5;
-  // Tiles from the sequence's end (a causal tile's work grows with its position,
-  // and workgroups start in index order: the longest start first).
   const int split = udiv(blockIdx.x, a.by_s);  // by_s: workgroups per split
   const int lin = blockIdx.x - split * a.by_s.d;
   const int tg = udiv(lin, a.by_hkv), kvh = lin - tg * a.kv.Hkv;
-  int seq, tile, tiles;
-  if (!find_tile(a, tg, seq, tile, tiles)) return;
-  tile = tiles - 1 - tile;
-  int first, count;
+  int seq, tile;
+  if (!find_tile<kRows, PAGED>(a, tg, seq, tile)) return;
+  int first, count, key0, len;
   seq_rows(a.cu_q, a.n_rows, seq, first, count);
-  int len, key0 = 0;
-  if constexpr (PAGED) {
-    len = paged_len(a.kv, seq, a.max_len);
-  } else {
-    key0 = min(max(a.kv.cu_k[seq], 0), a.kv.limit);
-    len = min(max(min(a.kv.cu_k[seq + 1], a.kv.limit) - key0, 0), a.max_len);
-  }
+  seq_keys<PAGED>(a, seq, key0, len);
   const int packed = count * a.G, p0 = tile * kRows;
   const int h0 = kvh * a.G;
   // this lane's query
@@ -425,7 +462,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
     if (tp > t0) {
       bool hole = false;
       const int e1 = (tp * kKeys - 1) >> a.kv.shift;
-      for (int e = (t0 * kKeys >> a.kv.shift) + tid; e <= e1; e += kBlock)
+      for (int e = (t0 * kKeys >> a.kv.shift) + tid; e <= e1; e += kThreads)
         hole |= (unsigned)table[e] >= (unsigned)a.kv.limit;
       if (__syncthreads_or(hole)) tp = t0;
     }
@@ -441,9 +478,9 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
   const int k_at = rl * L::KROW + 16 * kh;
   const int v_at = (4 * kh + (lane & 15) / 4) * L::VROW +
                    ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
-  auto key_frag = [&](int buf, int i) {  // i: block of 32 keys, chunk of 16 dims
-    return as_bf16x8(*(const u32x4*)(smem + buf * L::KBYTES + k_at + i / NC * 32 * L::KROW +
-                                     i % NC * 32));
+  auto key_frag = [&](int buf, int i) {  // i: chunk of 16 dims, block of 32 keys
+    return as_bf16x8(*(const u32x4*)(smem + buf * L::KBYTES + k_at + i % 2 * 32 * L::KROW +
+                                     i / 2 * 32));
   };
   auto value_frag = [&](int buf, int i) {  // i: chunk of 16 keys, tile of 32 dims
     const char* v = smem + 2 * L::KBYTES + buf * L::VBYTES + v_at + i / NHB * 16 * L::VROW +
@@ -512,20 +549,21 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
       // Matrix instructions with a few vector instructions behind each: those then
       // cost next to nothing (8 of these MFMAs with 16 exponentials among them
       // take as long as without, with 48 multiply-adds 14 % longer; one kind after the
-      // other, two waves per SIMD hide about half).  LDS reads run two ahead.
+      // other, two waves per SIMD hide about half).
       bf16x8 pt[4][NT];
-      bf16x8 ak[3];
-      ak[0] = key_frag(buf ^ 1, 0);
-      ak[1] = key_frag(buf ^ 1, 1);
+      bf16x8 ak[kAhead + 1];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ak[i] = key_frag(buf ^ 1, i);
 #pragma unroll
       for (int i = 0; i < 2 * NC; ++i) {
-        if (i + 2 < 2 * NC) ak[(i + 2) % 3] = key_frag(buf ^ 1, i + 2);
-        if (i % NC == 0) {
+        if (i + kAhead < 2 * NC)
+          ak[(i + kAhead) % (kAhead + 1)] = key_frag(buf ^ 1, i + kAhead);
+        if (i < 2) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sn[i / NC][e] = 0.f;
+          for (int e = 0; e < 16; ++e) sn[i][e] = 0.f;
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) sn[i / NC] = mfma32(ak[i % 3], q[i % NC][n], sn[i / NC]);
+        for (int n = 0; n < NT; ++n) sn[i % 2] = mfma32(ak[i % (kAhead + 1)], q[i / 2][n], sn[i % 2]);
         constexpr int E = 16 / NC;  // scores of this step
 #pragma unroll
         for (int e = i * E; e < (i + 1) * E; ++e) {
@@ -544,15 +582,16 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
       }
       load_tile(kr, kb, t + 3);
       load_tile(vr, vb, t + 2);
-      bf16x8 av[3];
-      av[0] = value_frag(buf, 0);
-      av[1] = value_frag(buf, 1);
+      bf16x8 av[kAhead + 1];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) av[i] = value_frag(buf, i);
       mx = sn[0][0];
 #pragma unroll
       for (int i = 0; i < 4 * NHB; ++i) {
-        if (i + 2 < 4 * NHB) av[(i + 2) % 3] = value_frag(buf, i + 2);
+        if (i + kAhead < 4 * NHB)
+          av[(i + kAhead) % (kAhead + 1)] = value_frag(buf, i + kAhead);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) o[i % NHB] = mfma32(av[i % 3], pt[i / NHB][n], o[i % NHB]);
+        for (int n = 0; n < NT; ++n) o[i % NHB] = mfma32(av[i % (kAhead + 1)], pt[i / NHB][n], o[i % NHB]);
         constexpr int E = 32 / (4 * NHB);  // scores of the next tile to take the maximum of
 #pragma unroll
         for (int e = i * E; e < (i + 1) * E; ++e) mx = fmaxf(mx, sn[e / 16][e % 16]);
@@ -576,7 +615,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
       for (int i = 0; i < 16; ++i) sa[b][i] = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const bf16x8 ak = key_frag(0, b * NC + c);
+        const bf16x8 ak = key_frag(0, 2 * c + b);
 #pragma unroll
         for (int n = 0; n < NT; ++n) sa[b] = mfma32(ak, q[c][n], sa[b]);
       }
@@ -643,7 +682,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
           }
       }
       __syncthreads();
-      for (int e = tid; e < kKeys * HD; e += kBlock) {
+      for (int e = tid; e < kKeys * HD; e += kThreads) {
         uint16_t* x = (uint16_t*)(v + e / HD * L::VROW) + e % HD;
         if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
       }
@@ -658,7 +697,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs 
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const bf16x8 ak = key_frag(0, b * NC + c);
+        const bf16x8 ak = key_frag(0, 2 * c + b);
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
       }
@@ -786,15 +825,23 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
 }
 
+template <int HD, int NT, bool PAGED, int W>
+hipError_t launch_rows_w(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  constexpr int lds = RowsLds<HD>::BYTES;
+  const auto fn = k_attn_rows<HD, NT, PAGED, W>;
+  const hipError_t e =
+      hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fn, dim3((unsigned)p.groups), dim3(W * AIO_WAVE), lds, stream, a);
+  return hipGetLastError();
+}
+
 template <int HD, int NT, bool PAGED>
 hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  constexpr int lds = RowsLds<HD>::BYTES;
-  const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<HD, NT, PAGED>,
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_attn_rows<HD, NT, PAGED>), dim3((unsigned)p.groups), dim3(kBlock), lds,
-                     stream, a);
-  return hipGetLastError();
+  if constexpr (NT == 1) {
+    if (p.waves == 8) return launch_rows_w<HD, NT, PAGED, 8>(a, p, stream);
+  }
+  return launch_rows_w<HD, NT, PAGED, 4>(a, p, stream);
 }
 
 template <int HD, int NT>
@@ -818,7 +865,7 @@ hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 // Workgroups up to which the keys are split.
 constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
 
-int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
+int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p) {
   *p = AttnPlan{};
   if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0) return AIO_ERANGE;
   if (Hkv < 1 || H < 1 || H % Hkv) return AIO_EINVAL;
@@ -826,6 +873,7 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
   p->rows = s.cu_q_dev || s.cu_k_dev;
   if (!p->rows && s.n_rows != s.n_seqs) return AIO_ERANGE;
   const int64_t G = H / Hkv;
+  const bool fp32 = dtype == AIO_F32;
   p->splits = 1;
   if (!p->rows) {
     // splits of at least 128 keys (a block of 32 per wave)
@@ -836,22 +884,26 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p) {
     p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
     p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
   } else {
-    p->tiles = ((int64_t)s.n_rows * G) / kRows + s.n_seqs;
+    // Tiles of 256 rows stage each key for twice the rows; where that leaves less than
+    // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594
+    // against 564 us; eight of up to 2048, 8 kv heads: 136 against 143)
+    p->waves = fp32 || (int64_t)s.n_rows * G / 256 * Hkv < 4 * kCUs ? 4 : 8;
+    p->tiles = ((int64_t)s.n_rows * G) / (32 * p->waves) + s.n_seqs;
     const int64_t base = std::max<int64_t>(1, p->tiles * Hkv);
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 4 * kKeys - 1) / (4 * kKeys));
     p->splits = (int)std::max<int64_t>(1, std::min(units, kRowsGroups / base));
     p->groups = p->tiles * Hkv * p->splits;
   }
   if (p->groups > 0x7fffffff || (int64_t)s.n_rows * H > 0x7fffffff) return AIO_ERANGE;
-  if (p->rows && (int64_t)s.n_rows * G > 0x7fffffff - kRows) return AIO_ERANGE;
+  if (p->rows && (int64_t)s.n_rows * G > 0x7fffffff - 256) return AIO_ERANGE;
   if (p->splits > 1) p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
   return AIO_OK;
 }
 
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd) {
   // step: splits n Hkv <= kStepGroups, so splits n H <= kStepGroups G; rows: splits tiles
-  // Hkv <= kRowsGroups and n_rows G <= kRows tiles, so splits n_rows H <= kRowsGroups kRows
-  const size_t rh = std::max<size_t>((size_t)kStepGroups * (H / Hkv), (size_t)kRowsGroups * kRows);
+  // Hkv <= kRowsGroups and n_rows G <= 256 tiles, so splits n_rows H <= 256 kRowsGroups
+  const size_t rh = std::max<size_t>((size_t)kStepGroups * (H / Hkv), (size_t)kRowsGroups * 256);
   return rh * (hd + 2) * 4;
 }
 

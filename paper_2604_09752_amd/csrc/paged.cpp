@@ -45,7 +45,7 @@ KeysArgs paged_keys(const aio_paged_kv& kv, const aio_seqs& s) {
 int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const aio_attn& a,
               void* ws, size_t ws_bytes, void* stream) {
   AttnPlan p;
-  const int rc = aio_attn_plan(s, a.n_heads, Hkv, hd, &p);
+  const int rc = aio_attn_plan(s, a.n_heads, Hkv, hd, a.dtype, &p);
   if (rc) return rc;
   if (a.dtype != AIO_F32 && a.dtype != AIO_BF16) return AIO_EINVAL;
   const int64_t unit = a.dtype == AIO_F32 ? 4 : 8;  // elements in 16 bytes
@@ -161,8 +161,8 @@ extern "C" {
 size_t aio_attn_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
                                 int32_t head_dim) {
   if (!s) return 0;
-  AttnPlan p;
-  return aio_attn_plan(*s, n_heads, n_kv_heads, head_dim, &p) == AIO_OK ? p.ws : 0;
+  AttnPlan p;  // (an attention whose tiles go by the type is not split)
+  return aio_attn_plan(*s, n_heads, n_kv_heads, head_dim, AIO_F32, &p) == AIO_OK ? p.ws : 0;
 }
 
 int aio_paged_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_attn* a,

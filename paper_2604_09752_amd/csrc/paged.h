@@ -25,13 +25,14 @@ int aio_check_paged(const aio_paged_kv& kv);
 struct AttnPlan {
   bool rows;       // several rows per sequence (k_attn_rows), else one (k_attn_step)
   int splits;      // workgroups over the keys
+  int waves;       // of a workgroup (k_attn_rows)
   int chunk;       // keys per split (k_attn_step); 0: the splits share a tile's key blocks
   int64_t tiles;   // row tiles of all sequences, at most (k_attn_rows)
   int64_t groups;  // workgroups
   size_t ws;       // bytes of partial results
 };
 // AIO_OK, or the error that the entry points return for these sizes.
-int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, AttnPlan* p);
+int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p);
 // No attention of these heads takes more workspace, whatever its sequences.
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd);
 
