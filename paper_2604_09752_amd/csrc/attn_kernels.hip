@@ -101,21 +101,24 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // the split, and the waves' states join in LDS.
 template <int HD>
 struct StepLds {
-  static constexpr int VROW = HD * 2 + 32;        // bytes of a value row: 8 rows in distinct banks
-  static constexpr int VBYTES = 32 * VROW;        // a wave's value tile
+  // bytes of a key and a value row: the 16 and the 8 rows that one access takes lie in
+  // distinct banks
+  static constexpr int KROW = HD * 2 + 16, VROW = HD * 2 + 32;
+  static constexpr int TBYTES = 32 * VROW;  // a wave's tile: the keys, then the values
   static constexpr int OROW = HD + 4;             // floats of an output row
   static constexpr int OBYTES = kWaves * kMaxGroup * OROW * 4;
-  static constexpr int BYTES = kWaves * VBYTES > OBYTES ? kWaves * VBYTES : OBYTES;
+  static constexpr int BYTES = kWaves * TBYTES > OBYTES ? kWaves * TBYTES : OBYTES;
 };
 
-template <int HD, int NT>
-__global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
+template <int HD, int NT, bool STREAM>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : 2) void k_attn_step(AttnArgs a) {
   using L = StepLds<HD>;
-  __shared__ __align__(16) char smem[L::BYTES];
+  extern __shared__ __align__(16) char smem[];
   __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
   constexpr int NC = HD / 32;              // k chunks of a score product
-  constexpr int RPL = AIO_WAVE * 8 / HD;   // value rows per load
-  constexpr int NV = 32 / RPL;             // loads of a value tile
+  constexpr int TPR = HD / 8;              // lanes of a row
+  constexpr int RPL = AIO_WAVE / TPR;      // rows per load: 4 or 8, all in one page
+  constexpr int NV = 32 / RPL;             // loads of a tile
   constexpr int ND = HD / 16;              // output tiles
   const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
@@ -145,62 +148,65 @@ __global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
     if (key < c1) p = table[key >> a.kv.shift];
     return (unsigned)p < (unsigned)a.kv.limit ? p : -1;
   };
-  // Keys as the A operand (key row col of 16, dims 32 c + 8 grp ..), values row
-  // by row.  The 8 keys of an aligned group share a page, so pages are wave
-  // uniform: a value load covers 4 or 8 keys, a key load two groups.  Keys that
-  // are not visible read page 0.
-  u32x4 kr[2][NC], vr[NV];
-  auto load_block = [&](int t, int page) {
+  // Rows as they lie in memory, 4 or 8 per load (in the operand's order, a load of the keys
+  // would take half a 128-byte line of 16 rows); the 8 keys of an aligned group share
+  // a page, so pages are wave uniform.  Keys that are not visible read page 0.
+  const int lr = lane / TPR, ld = lane % TPR * 8;
+  u32x4 kr[NV], vr[NV];
+  auto load_block = [&](u32x4 (&r)[NV], const uint16_t* from, int t, int page) {
     const int j0 = c0 + t * 32;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const int64_t lo = max(__builtin_amdgcn_readlane(page, kt * 16), 0) * a.kv.stride;
-      const int64_t hi = max(__builtin_amdgcn_readlane(page, kt * 16 + 8), 0) * a.kv.stride;
-      const uint16_t* p =
-          kb + (col < 8 ? lo : hi) + (((j0 + kt * 16 + col) & pm) * HD + 8 * grp);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) kr[kt][c] = *(const u32x4*)(p + c * 32);
-    }
-#pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t pg = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride;
-      const int kk = i * RPL + lane / (HD / 8);
-      vr[i] = *(const u32x4*)(vb + pg + (((j0 + kk) & pm) * HD + lane % (HD / 8) * 8));
+      const int64_t at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
+                         ((j0 + i * RPL) & pm) * HD;
+      const u32x4* p = (const u32x4*)(from + at + (uint32_t)(lr * HD + ld));
+      r[i] = STREAM ? __builtin_nontemporal_load(p) : *p;
     }
   };
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  char* vt = smem + wid * L::VBYTES;
-  const char* vtr = vt + (4 * grp + col / 4) * L::VROW + (col & 3) * 8;
+  char* tile = smem + wid * L::TBYTES;
+  const char* ktr = tile + col * L::KROW + 16 * grp;
+  const char* vtr = tile + (4 * grp + col / 4) * L::VROW + (col & 3) * 8;
 
   int page = load_page(wid), next = load_page(wid + kWaves);
-  if (wid < nt) load_block(wid, page);
+  if (wid < nt) {
+    load_block(kr, kb, wid, page);
+    load_block(vr, vb, wid, page);
+  }
   for (int t = wid; t < nt; t += kWaves) {
     const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
-    // value rows -> LDS; what no row may see is zero there (0 x NaN is not)
+    // the wave's next block (its last one is read again: no branch)
+    const bool more = t + kWaves < nt;
+    const int tn = more ? t + kWaves : t, pn = more ? next : page;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int kk = i * RPL + lane / (HD / 8);
-      u32x4 w = vr[i];
-      if (vis != 0xffffffffu && !(vis >> kk & 1)) w = u32x4{0, 0, 0, 0};
-      *(u32x4*)(vt + kk * L::VROW + lane % (HD / 8) * 16) = w;
-    }
+    for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = kr[i];
+    load_block(kr, kb, tn, pn);
+    wave_lds_sync();  // the keys are in LDS
     float p[8];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 ak = as_bf16x8(*(const u32x4*)(ktr + kt * 16 * L::KROW + c * 64));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s = mfma16(as_bf16x8(kr[kt][c]), q[c][n], s);
+        for (int n = 0; n < NT; ++n) s = mfma16(ak, q[c][n], s);
+      }
 #pragma unroll
       for (int v = 0; v < 4; ++v) p[4 * kt + v] = s[v];
     }
-    // the wave's next block (its last one is read again: no branch)
-    const bool more = t + kWaves < nt;
-    load_block(more ? t + kWaves : t, more ? next : page);
+    wave_lds_sync();  // ... and read: the values take their place
+    // (those that may not be seen are zero: 0 x NaN is not)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      u32x4 w = vr[i];
+      if (vis != 0xffffffffu && !(vis >> (i * RPL + lr) & 1)) w = u32x4{0, 0, 0, 0};
+      *(u32x4*)(tile + (i * RPL + lr) * L::VROW + ld * 2) = w;
+    }
+    load_block(vr, vb, tn, pn);
     page = next;
     next = load_page(t + 2 * kWaves);
     if (vis != 0xffffffffu) {
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_attn_step(AttnArgs a) {
     }
     bf16x8 pt[NT];
     terms<NT>(p, pt);
-    wave_lds_sync();  // the value tile is in LDS
+    wave_lds_sync();  // the values are in LDS
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       const uint2 v0 = lds_read_tr16(vtr + d * 32);
@@ -848,7 +854,11 @@ template <int HD, int NT>
 hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   hipError_t e;
   if (!p.rows) {
-    hipLaunchKernelGGL((k_attn_step<HD, NT>), dim3((unsigned)p.groups), dim3(kBlock), 0, stream, a);
+    constexpr int lds = StepLds<HD>::BYTES;
+    const auto fn = p.stream ? k_attn_step<HD, NT, true> : k_attn_step<HD, NT, false>;
+    e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(fn, dim3((unsigned)p.groups), dim3(kBlock), lds, stream, a);
     e = hipGetLastError();
   } else {
     e = a.kv.table ? launch_rows<HD, NT, true>(a, p, stream) : launch_rows<HD, NT, false>(a, p, stream);
@@ -863,7 +873,7 @@ hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 }  // namespace
 
 // Workgroups up to which the keys are split.
-constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
+constexpr int64_t kStepGroups = 2 * kCUs, kRowsGroups = 2 * kCUs;
 
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p) {
   *p = AttnPlan{};
@@ -876,13 +886,17 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
   const bool fp32 = dtype == AIO_F32;
   p->splits = 1;
   if (!p->rows) {
-    // splits of at least 128 keys (a block of 32 per wave)
+    // splits of at least 128 keys (a block of 32 per wave), none up to 512: a launch that
+    // joins them costs more than four blocks per wave
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 127) / 128);
     const int64_t base = std::max<int64_t>(1, (int64_t)s.n_seqs * Hkv);
-    const int64_t want = std::max<int64_t>(1, std::min(units, kStepGroups / base));
+    const int64_t want = s.max_len <= 512 ? 1 : std::max<int64_t>(1, std::min(units, kStepGroups / base));
     p->chunk = (int)((units + want - 1) / want * 128);
     p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
     p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
+    // Keys that are more than the 256 MB cache in front of memory holds pass it by (1.07
+    // GB: 188 against 173 us); fewer may come from it (217 of at most 403 MB: 45 / 52)
+    p->stream = (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)512 << 20;
   } else {
     // Tiles of 256 rows stage each key for twice the rows; where that leaves less than
     // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594

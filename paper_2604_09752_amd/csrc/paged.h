@@ -26,6 +26,7 @@ struct AttnPlan {
   bool rows;       // several rows per sequence (k_attn_rows), else one (k_attn_step)
   int splits;      // workgroups over the keys
   int waves;       // of a workgroup (k_attn_rows)
+  bool stream;     // keys pass the caches by (k_attn_step)
   int chunk;       // keys per split (k_attn_step); 0: the splits share a tile's key blocks
   int64_t tiles;   // row tiles of all sequences, at most (k_attn_rows)
   int64_t groups;  // workgroups
