@@ -904,8 +904,11 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
     p->waves = fp32 || (int64_t)s.n_rows * G / 256 * Hkv < 4 * kCUs ? 4 : 8;
     p->tiles = ((int64_t)s.n_rows * G) / (32 * p->waves) + s.n_seqs;
     const int64_t base = std::max<int64_t>(1, p->tiles * Hkv);
-    const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 4 * kKeys - 1) / (4 * kKeys));
-    p->splits = (int)std::max<int64_t>(1, std::min(units, kRowsGroups / base));
+    // Few tiles: their keys are split until the workgroups that a CU holds are there (one
+    // with fp32 queries, two with bf16), down to one key tile each (5 rows behind 3000 keys,
+    // at most 256 keys per split: 25 us, 64: 17)
+    const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + kKeys - 1) / kKeys);
+    p->splits = (int)std::max<int64_t>(1, std::min(units, kRowsGroups / (fp32 ? 2 : 1) / base));
     p->groups = p->tiles * Hkv * p->splits;
   }
   if (p->groups > 0x7fffffff || (int64_t)s.n_rows * H > 0x7fffffff) return AIO_ERANGE;

@@ -161,8 +161,8 @@ extern "C" {
 size_t aio_attn_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
                                 int32_t head_dim) {
   if (!s) return 0;
-  AttnPlan p;  // (an attention whose tiles go by the type is not split)
-  return aio_attn_plan(*s, n_heads, n_kv_heads, head_dim, AIO_F32, &p) == AIO_OK ? p.ws : 0;
+  AttnPlan p;  // (fp32 takes no more)
+  return aio_attn_plan(*s, n_heads, n_kv_heads, head_dim, AIO_BF16, &p) == AIO_OK ? p.ws : 0;
 }
 
 int aio_paged_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_attn* a,
