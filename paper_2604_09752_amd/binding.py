@@ -440,19 +440,26 @@ def _paged(k: torch.Tensor, v: torch.Tensor) -> aio_paged_kv:
 
 
 def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_seqs:
-    _i32(lens, 1, "lens")
-    _i32(table, 2, "table")
-    n, width = table.shape
-    _need(lens.shape[0] == n, "lens and table are of different batches")
+    shape, stride = table.shape, table.stride()
+    if (table.dtype is not torch.int32 or lens.dtype is not torch.int32 or len(shape) != 2 or
+            lens.shape != shape[:1]):
+        raise ValueError("lens and table: int32 [n] and [n, width]")
+    n, width = shape
+    if n > 1:
+        _need((width <= 1 or stride[1] == 1) and lens.stride(0) == 1,
+              "lens and table: rows have to be contiguous")
+        width_stride = stride[0]
+    else:
+        _need(width <= 1 or stride[1] == 1, "table: rows have to be contiguous")
+        width_stride = width
     cu = None
     if cu_q is not None:
-        _i32(cu_q, 1, "cu_q")
-        _need(cu_q.shape[0] == n + 1, "cu_q: one more entry than sequences")
+        if cu_q.dtype is not torch.int32 or cu_q.shape != (n + 1,) or (n and cu_q.stride(0) != 1):
+            raise ValueError("cu_q: contiguous int32, one more entry than sequences")
         cu = cu_q.data_ptr()
     if max_len is None:
-        max_len = width * page_size
-    return aio_seqs(n, n_rows, min(int(max_len), 0x7fffffff), cu, lens.data_ptr(),
-                    table.data_ptr(), table.stride(0) if n > 1 else width, None)
+        max_len = min(width * page_size, 0x7fffffff)
+    return aio_seqs(n, n_rows, max_len, cu, lens.data_ptr(), table.data_ptr(), width_stride, None)
 
 
 def _attn(q, out, lse, scale) -> aio_attn:

@@ -38,6 +38,8 @@ AIO_DEV float key_value(uint64_t k) {
   return __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
 
+constexpr float kLog2e = 1.44269504088896340736f;
+
 struct Stats {
   float m;
   double z, w;
@@ -81,25 +83,21 @@ AIO_DEV void rank_candidates(const uint64_t* cand, int n, int top, uint64_t* bes
   }
 }
 
-AIO_DEV void write_stats(const LogprobArgs& a, int row, const Stats& s, double& logz) {
-  // a row with nothing above -inf has no distribution
-  logz = s.m == -INFINITY ? (double)__uint_as_float(0x7fc00000u) : log(s.z);
-  if (threadIdx.x == 0 && a.entropy) a.entropy[row] = (float)(logz - s.w / s.z);
-}
-
 AIO_DEV float load1(const float* x, int64_t i) { return x[i]; }
 AIO_DEV float load1(const uint16_t* x, int64_t i) { return bf16_to_f32(x[i]); }
 
 template <class T>
 AIO_DEV void finish_row(const LogprobArgs& a, int row, const Stats& s, const uint64_t* best) {
-  double logz;
-  write_stats(a, row, s, logz);
+  // a row with nothing above -inf has no distribution, nor one with +inf
+  const double nan = (double)__uint_as_float(0x7fc00000u);
+  const bool none = s.m == -INFINITY || s.m == INFINITY;
+  const double logz = none ? nan : log(s.z);
+  if (threadIdx.x == 0 && a.entropy) a.entropy[row] = (float)(logz - s.w / s.z);
   if (threadIdx.x == 0 && a.logprob) {
     const int t = a.target[row];
-    float lp = __uint_as_float(0x7fc00000u);
-    if ((unsigned)t < (unsigned)a.n)
-      lp = (float)((double)load1((const T*)a.x + row * a.stride, t) - s.m - logz);
-    a.logprob[row] = lp;
+    a.logprob[row] = (unsigned)t < (unsigned)a.n
+                         ? (float)((double)load1((const T*)a.x + row * a.stride, t) - s.m - logz)
+                         : (float)nan;
   }
   if ((int)threadIdx.x < a.top) {
     const uint64_t k = best[threadIdx.x];
@@ -141,8 +139,6 @@ struct Chunk {
   }
 };
 
-constexpr float kLog2e = 1.44269504088896340736f;
-
 // Workgroup (slice, row): the slice's statistics and its best candidates; with
 // one slice per row, the row's results.
 //
@@ -176,29 +172,27 @@ __global__ __launch_bounds__(kBlock, 4) void k_logprobs(LogprobArgs a) {
     C c;
     c.load(x, c0, hi);
     float m = c.v[0];
-    bool nan = c.v[0] != c.v[0];
 #pragma unroll
-    for (int i = 1; i < PER; ++i) {
-      m = fmaxf(m, c.v[i]);
-      nan |= c.v[i] != c.v[i];
-    }
+    for (int i = 1; i < PER; ++i) m = fmaxf(m, c.v[i]);
     Stats s{m, 0.0, 0.0};
-    if (nan) {
-      s.z = s.w = (double)__uint_as_float(0x7fc00000u);
-    } else if (m != -INFINITY) {
-      // z in 64 bits, so that a 1 does not swallow the rest; w's terms are 0 there.
+    if (m != -INFINITY) {
+      // z in 64 bits, so that a 1 does not swallow the rest (w's terms are 0 there);
       // e^-150 is 0: the clamp only keeps 0 x -inf out of w
       float w = 0.f;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const float d = fmaxf(c.v[i] - m, -150.f);
+        const float d = c.v[i] - m;
         const float e = __builtin_amdgcn_exp2f(d * kLog2e);
         s.z += (double)e;
-        w = fmaf(e, d, w);
+        w = fmaf(e, fmaxf(d, -150.f), w);
       }
       s.w = (double)w;
-      if (m == INFINITY) s.z = (double)__uint_as_float(0x7fc00000u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (c.v[i] != c.v[i]) s.z = (double)c.v[i];
     }
+    const bool nan = s.z != s.z;  // (or +inf - inf: its keys are sorted exactly as well)
     st = join(st, s);
     if (a.top == 0) continue;
     // the largest of the thread as a sortable number, 0 for none
@@ -216,36 +210,40 @@ __global__ __launch_bounds__(kBlock, 4) void k_logprobs(LogprobArgs a) {
       if (cut != 0xffffffffu) ++cut;
       if (!__any(g >= cut)) continue;
     } else {
+      // (the last 6 bits give way to the group's number, so that no two are equal)
+      const uint32_t mark = (g & ~63u) | lane;
       int r = 0;
 #pragma unroll 8
-      for (int j = 0; j < kBlock / 4; ++j) {
-        const uint32_t o = group_max[parity][j];
-        r += o > g || (o == g && j < lane);
-      }
+      for (int j = 0; j < kBlock / 4; ++j)
+        r += ((group_max[parity][j] & ~63u) | (uint32_t)j) > mark;
       const uint64_t at = __ballot(r == a.top - 1);
-      cut = __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)at) - 1);
+      cut = __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)at) - 1) & ~63u;
       if (cut == 0) cut = 1;
     }
     bool exact = __any(g == 0xffffffffu);
     if (!exact) {
       if (mine >= cut) {
+        // (a cut below every number lets all through)
+        const float cut_v = key_value((uint64_t)cut << 32);
+        const bool all = cut < 0x00800000u;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const uint64_t k = order_key(c.v[i], C::index(c0, i));
-          if ((uint32_t)(k >> 32) >= cut && C::index(c0, i) < hi) {
+        for (int i = 0; i < PER; ++i)
+          if ((c.v[i] >= cut_v || all) && C::index(c0, i) < hi) {
             const int to = atomicAdd(&n_cand, 1);
-            if (to < kCand - AIO_MAX_TOP) cand[to] = k;
+            if (to < kCand - AIO_MAX_TOP) cand[to] = order_key(c.v[i], C::index(c0, i));
           }
-        }
       }
       __syncthreads();
       exact = n_cand > kCand - AIO_MAX_TOP;
     }
     if (exact) {
+      // (rare: the values are read again, so that their registers are free by now)
       uint64_t mk = 0;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (C::index(c0, i) < hi) mk = max(mk, order_key(c.v[i], C::index(c0, i)));
+#pragma unroll 1
+      for (int i = 0; i < PER; ++i) {
+        const int e = C::index(c0, i);
+        if (e < hi) mk = max(mk, order_key(load1(x, e), e));
+      }
       __syncthreads();  // every thread has read n_cand
       maxima[tid] = mk;
       if (tid == 0) {
@@ -254,14 +252,16 @@ __global__ __launch_bounds__(kBlock, 4) void k_logprobs(LogprobArgs a) {
       }
       __syncthreads();
       int r = 0;
+#pragma unroll 4
       for (int j = 0; j < kBlock; ++j) r += maxima[j] > mk;
       if (mk && r == a.top - 1) cut_s = mk;
       __syncthreads();
       const uint64_t from = max(cut_s, kth);
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < PER; ++i) {
-        const uint64_t k = order_key(c.v[i], C::index(c0, i));
-        if (k >= from && C::index(c0, i) < hi) cand[atomicAdd(&n_cand, 1)] = k;
+        const int e = C::index(c0, i);
+        const uint64_t k = e < hi ? order_key(load1(x, e), e) : 0;
+        if (k >= from) cand[atomicAdd(&n_cand, 1)] = k;
       }
       __syncthreads();
     }
