@@ -475,17 +475,19 @@ typedef struct aio_packed_kv {
  * packed, and row r of its q rows sees keys 0 .. keys - q + r.  In pages,
  * key j is slot j mod page_size of page table[i][j / page_size].  A page id
  * outside [0, n_pages) is a hole (an evicted page): its keys are seen by no
- * row.  Keys past max_len or past the table's width are not there either.  A row that sees no key
- * gets zeros and the log-sum-exp -infinity; rows of no sequence are left as
- * they are. */
+ * row.  Keys past max_len or past the table's width are not there either, and
+ * change no row's own place.  A row that sees no key gets zeros and the
+ * log-sum-exp -infinity; rows of no sequence are left as they are.  What the
+ * places hold that a row does not see (infinities and NaN among it) does not
+ * reach it. */
 typedef struct aio_seqs {
   int32_t n_seqs;
   int32_t n_rows;            /* rows of q and out (of k and v rows to append) */
-  int32_t max_len;           /* no sequence has more keys                     */
+  int32_t max_len;           /* no sequence has more keys; at most 2^30       */
   const int32_t* cu_q_dev;   /* [n_seqs + 1], ascending from 0, or NULL       */
   const int32_t* lens_dev;   /* pages: [n_seqs] keys, the new rows among them */
   const int32_t* table_dev;  /* pages: [n_seqs][table_stride] page ids        */
-  int32_t table_stride;
+  int32_t table_stride;      /* its width, all of it readable                 */
   const int32_t* cu_k_dev;   /* packed: [n_seqs + 1], ascending from 0        */
 } aio_seqs;
 

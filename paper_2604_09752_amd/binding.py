@@ -435,8 +435,9 @@ def _paged(k: torch.Tensor, v: torch.Tensor) -> aio_paged_kv:
         raise ValueError("pages: two bf16 [n_pages, kv_heads, page_size, head_dim]")
     if v.stride() != stride or stride[3] != 1 or stride[2] != shape[3]:
         raise ValueError("pages: K and V of the same strides, slots and dimensions contiguous")
-    return aio_paged_kv(k.data_ptr(), v.data_ptr(), stride[0], stride[1], shape[0], shape[2],
-                        shape[1], shape[3])
+    # (the stride of a single head or page says nothing)
+    return aio_paged_kv(k.data_ptr(), v.data_ptr(), stride[0] if shape[0] > 1 else 0,
+                        stride[1] if shape[1] > 1 else 0, shape[0], shape[2], shape[1], shape[3])
 
 
 def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_seqs:
@@ -457,8 +458,10 @@ def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_
         if cu_q.dtype is not torch.int32 or cu_q.shape != (n + 1,) or (n and cu_q.stride(0) != 1):
             raise ValueError("cu_q: contiguous int32, one more entry than sequences")
         cu = cu_q.data_ptr()
-    if max_len is None:
-        max_len = min(width * page_size, 0x7fffffff)
+    # (the rows of a view may lie further apart than they are wide: no key past its width)
+    most = min(width * page_size, 1 << 30)
+    if max_len is None or max_len > most:
+        max_len = most
     return aio_seqs(n, n_rows, max_len, cu, lens.data_ptr(), table.data_ptr(), width_stride, None)
 
 
@@ -537,9 +540,10 @@ def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q
     for t, what in ((cu_q, "cu_q"), (cu_k, "cu_k")):
         _i32(t, 1, what)
     _need(cu_q.shape == cu_k.shape and cu_q.shape[0] >= 1, "cu_q and cu_k differ in length")
-    kv = aio_packed_kv(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0],
-                       k.shape[1], k.shape[2])
-    s = aio_seqs(cu_q.shape[0] - 1, q.shape[0], k.shape[0] if max_len is None else int(max_len),
+    rows, heads, hd = k.shape
+    kv = aio_packed_kv(k.data_ptr(), v.data_ptr(), k.stride(0) if rows > 1 else 0,
+                       k.stride(1) if heads > 1 else 0, rows, heads, hd)
+    s = aio_seqs(cu_q.shape[0] - 1, q.shape[0], rows if max_len is None else max_len,
                  cu_q.data_ptr(), None, None, 0, cu_k.data_ptr())
     _attend("aio_packed_attention", at, kv, s, a, kv.n_kv_heads, kv.head_dim, q.device, ws)
 
@@ -559,7 +563,8 @@ def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor,
         _need(k_rows.numel() == 0, "rows: the same strides, dimensions contiguous")
     s = _paged_seqs(lens, table, cu_q, shape[0], max_len, kv.page_size)
     rc = _launch(at, lib().aio_page_append, ctypes.byref(kv), ctypes.byref(s), k_rows.data_ptr(),
-                 v_rows.data_ptr(), _DTYPES[dtype], stride[0], stride[1])
+                 v_rows.data_ptr(), _DTYPES[dtype], stride[0] if shape[0] > 1 else 0,
+                 stride[1] if shape[1] > 1 else 0)
     if rc:
         raise AioError(rc, "aio_page_append")
 

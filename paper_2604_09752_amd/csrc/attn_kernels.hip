@@ -315,15 +315,18 @@ struct RowsLds {
   static constexpr int BYTES = 2 * (KBYTES + VBYTES);
 };
 
-// First key and number of keys of sequence i.
+// First key of sequence i, how many of its keys are there, and how many it has by the
+// caller's word (its rows are the last of those).
 template <bool PAGED>
-AIO_DEV void seq_keys(const AttnArgs& a, int i, int& key0, int& len) {
+AIO_DEV void seq_keys(const AttnArgs& a, int i, int& key0, int& len, int& full) {
   if constexpr (PAGED) {
     key0 = 0;
     len = paged_len(a.kv, i, a.max_len);
+    full = min(max(a.kv.lens[i], 0), 1 << 30);
   } else {
     key0 = min(max(a.kv.cu_k[i], 0), a.kv.limit);
-    len = min(max(min(a.kv.cu_k[i + 1], a.kv.limit) - key0, 0), a.max_len);
+    full = min(max(min(max(a.kv.cu_k[i + 1], 0), a.kv.limit) - key0, 0), 1 << 30);
+    len = min(full, a.max_len);
   }
 }
 
@@ -331,7 +334,7 @@ AIO_DEV void seq_keys(const AttnArgs& a, int i, int& key0, int& len) {
 // position: the longest first.  Tile `t` of the launch in that order, for up to 64
 // sequences: a tile's level is its number in the sequence plus the rows in tiles
 // that the sequence has had before; the tiles of the highest level come first (eight
-// packed prompts of 540 to 2048 rows, sequence after sequence: 134 us, so 124).  With
+// packed prompts of 540 to 2048 rows, sequence after sequence: 139 us, so 120).  With
 // more sequences they come one after the other, each from its end.
 // seq and tile receive its place; false behind the last.
 template <int ROWS, bool PAGED>
@@ -345,8 +348,8 @@ AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile) {
       n = (int)(((int64_t)count * a.G + ROWS - 1) / ROWS);
     }
     if (a.n_seqs <= AIO_WAVE && a.n_seqs > 1) {
-      int key0, len = 0;
-      if (n > 0) seq_keys<PAGED>(a, i, key0, len);
+      int key0, len = 0, full;
+      if (n > 0) seq_keys<PAGED>(a, i, key0, len, full);
       const int64_t before = (int64_t)max(len - count, 0) * a.G / ROWS;
       const int lo = (int)min(before, (int64_t)1 << 22), hi = lo + n;
       // tiles of at least level v (below 2^24 of them: exact)
@@ -427,21 +430,22 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   const int tg = udiv(lin, a.by_hkv), kvh = lin - tg * a.kv.Hkv;
   int seq, tile;
   if (!find_tile<kRows, PAGED>(a, tg, seq, tile)) return;
-  int first, count, key0, len;
+  int first, count, key0, len, full;
   seq_rows(a.cu_q, a.n_rows, seq, first, count);
-  seq_keys<PAGED>(a, seq, key0, len);
+  seq_keys<PAGED>(a, seq, key0, len, full);
   const int packed = count * a.G, p0 = tile * kRows;
   const int h0 = kvh * a.G;
   // this lane's query
   const int pr = p0 + wid * 32 + rl;
   const bool live = pr < packed;
   const int row = udiv(min(pr, packed - 1), a.by_g), g = min(pr, packed - 1) - row * a.G;
-  const int lim = len - count + row;  // its last visible key
+  auto sees = [&](int r) { return min(full - count + r, len - 1); };  // row r's last key
+  const int lim = sees(row);
   // the last key that any row of the wave, of the workgroup sees, and the last
   // that all rows of the workgroup see
-  const int wave_lim = len - count + udiv(min(p0 + wid * 32 + 31, packed - 1), a.by_g);
-  const int wg_lim = len - count + udiv(min(p0 + kRows, packed) - 1, a.by_g);
-  const int all_lim = len - count + udiv(p0, a.by_g);
+  const int wave_lim = sees(udiv(min(p0 + wid * 32 + 31, packed - 1), a.by_g));
+  const int wg_lim = sees(udiv(min(p0 + kRows, packed) - 1, a.by_g));
+  const int all_lim = sees(udiv(p0, a.by_g));
   const int nkt = wg_lim < 0 ? 0 : wg_lim / kKeys + 1;
   // this split's key tiles
   const int each = nkt / a.S, rest = nkt - each * a.S;
@@ -515,14 +519,26 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   };
 
   if (tp > t0) {
-    // Tile t into registers: no branches, tiles past the last read it again.
-    auto load_tile = [&](u32x4 (&r)[NP], const uint16_t* from, int t) {
+    // Tile t into registers: no branches, tiles past the last read it again.  Its pages
+    // (one of each pass's rows) are looked up well before.
+    struct PageIds {
+      int id[NP];
+    };
+    auto pages_of = [&](int t) {
+      PageIds pg{};
+      if constexpr (PAGED) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          pg.id[p] = table[(min(t, tp - 1) * kKeys + p * RPP + wr) >> a.kv.shift];
+      }
+      return pg;
+    };
+    auto load_tile = [&](u32x4 (&r)[NP], const uint16_t* from, int t, const PageIds& pg) {
       const int key = min(t, tp - 1) * kKeys + wr;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
         if constexpr (PAGED) {
-          const int kp = key + p * RPP;
-          const int64_t at = table[kp >> a.kv.shift] * a.kv.stride + (int64_t)(kp & pmask) * HD;
+          const int64_t at = pg.id[p] * a.kv.stride + (int64_t)((key + p * RPP) & pmask) * HD;
           r[p] = *(const u32x4*)(from + at + (uint32_t)lane_at);
         } else {
           r[p] = *(const u32x4*)(from + (int64_t)(key0 + key + p * RPP) * a.kv.stride + lane_at);
@@ -540,6 +556,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         *(u32x4*)(smem + 2 * L::KBYTES + buf * L::VBYTES + sv_at + p * RPP * L::VROW) = r[p];
     };
     u32x4 kr[NP], vr[NP];
+    PageIds pg2 = pages_of(t0 + 2), pg3 = pages_of(t0 + 3), pg4 = pages_of(t0 + 4);
     float mx;
     // One tile: its softmax while the next tile's scores (sn) are multiplied, then
     // its values while the next tile's maximum is taken.  Score v of block b is key 32 b +
@@ -586,8 +603,11 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      load_tile(kr, kb, t + 3);
-      load_tile(vr, vb, t + 2);
+      load_tile(kr, kb, t + 3, pg3);
+      load_tile(vr, vb, t + 2, pg2);
+      pg2 = pg3;
+      pg3 = pg4;
+      pg4 = pages_of(t + 5);
       bf16x8 av[kAhead + 1];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) av[i] = value_frag(buf, i);
@@ -606,14 +626,17 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
     };
     // (buffers by t - t0's parity: K of t0 in 0, of t0 + 1 in 1, V of t0 in 0)
     f32x16 sa[2], sb[2];
-    load_tile(kr, kb, t0);
-    load_tile(vr, vb, t0);
-    store_keys(kr, 0);
-    store_values(vr, 0);
-    load_tile(kr, kb, t0 + 1);
-    store_keys(kr, 1);
-    load_tile(kr, kb, t0 + 2);
-    load_tile(vr, vb, t0 + 1);
+    {
+      const PageIds pg0 = pages_of(t0), pg1 = pages_of(t0 + 1);
+      load_tile(kr, kb, t0, pg0);
+      load_tile(vr, vb, t0, pg0);
+      store_keys(kr, 0);
+      store_values(vr, 0);
+      load_tile(kr, kb, t0 + 1, pg1);
+      store_keys(kr, 1);
+      load_tile(kr, kb, t0 + 2, pg2);
+      load_tile(vr, vb, t0 + 1, pg1);
+    }
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -873,11 +896,11 @@ hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 }  // namespace
 
 // Workgroups up to which the keys are split.
-constexpr int64_t kStepGroups = 2 * kCUs, kRowsGroups = 2 * kCUs;
+constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
 
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p) {
   *p = AttnPlan{};
-  if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0) return AIO_ERANGE;
+  if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0 || s.max_len > (1 << 30)) return AIO_ERANGE;
   if (Hkv < 1 || H < 1 || H % Hkv) return AIO_EINVAL;
   if (H / Hkv > kMaxGroup || (hd != 64 && hd != 128)) return AIO_EUNSUPPORTED;
   p->rows = s.cu_q_dev || s.cu_k_dev;
@@ -886,17 +909,21 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
   const bool fp32 = dtype == AIO_F32;
   p->splits = 1;
   if (!p->rows) {
-    // splits of at least 128 keys (a block of 32 per wave), none up to 512: a launch that
-    // joins them costs more than four blocks per wave
+    // Splits of at least 128 keys (a block of 32 per wave), up to the workgroups that the
+    // GPU holds at once, or twice as many for many sequences, whose lengths differ (two of
+    // 32768 keys: 169 against 173 us; 24 of 37 to 4096: 55.6 against 51.4).  None up to
+    // 512 keys: a launch that joins them costs more than four blocks per wave.
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 127) / 128);
     const int64_t base = std::max<int64_t>(1, (int64_t)s.n_seqs * Hkv);
-    const int64_t want = s.max_len <= 512 ? 1 : std::max<int64_t>(1, std::min(units, kStepGroups / base));
+    const int64_t most = s.n_seqs < 8 ? kStepGroups / 2 : kStepGroups;
+    const int64_t want = s.max_len <= 512 ? 1 : std::max<int64_t>(1, std::min(units, most / base));
     p->chunk = (int)((units + want - 1) / want * 128);
     p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
     p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
-    // Keys that are more than the 256 MB cache in front of memory holds pass it by (1.07
-    // GB: 188 against 173 us); fewer may come from it (217 of at most 403 MB: 45 / 52)
-    p->stream = (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)512 << 20;
+    // Keys of a large batch pass the caches by: those of the next layer come before they are
+    // read again (217 MB of at most 403: 59.3 against 55.6 us, 1.07 GB: 188 against 172).  A
+    // small one's may stay in the 256 MB in front of memory.
+    p->stream = (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)64 << 20;
   } else {
     // Tiles of 256 rows stage each key for twice the rows; where that leaves less than
     // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594

@@ -134,6 +134,7 @@ AIO_DEV void seq_rows(const int32_t* cu_q, int n_rows, int i, int& first, int& c
     return;
   }
   first = min(max(cu_q[i], 0), n_rows);
-  count = max(min(cu_q[i + 1], n_rows) - first, 0);
+  // (both ends bounded before they are subtracted: what lies there may be any number)
+  count = max(min(max(cu_q[i + 1], 0), n_rows) - first, 0);
 }
 #endif

@@ -290,6 +290,103 @@ def test_many_sequences():
     check_attention(out, l, ref)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_keys_past_max_len(dtype):
+    """Keys past max_len or the table's width are not there; each row keeps its own
+    place among the keys that its length says."""
+    ql, kl = [70, 40, 9], [200, 100, 30]
+    case = PoolCase(kl, 2, 64, 16, width_more=0)
+    q = rows(sum(ql), 4, 64, dtype)
+    k, v, lens, table = case.device()
+    for max_len, width in ((150, 13), (64, 13), (200, 6), (0, 13)):
+        there = min(max_len, width * 16)
+        vis = [torch.arange(n) < there for n in kl]
+        ref = attention64(q, case.keys, case.values, ql, kl, vis)
+        out, l = torch.full_like(q, 9.0).cuda(), torch.full(q.shape[:2], 9.0, device="cuda")
+        B.aio_paged_attention(q.cuda(), k, v, lens, table[:, :width], out, cu_q=cu(ql).cuda(),
+                              lse=l, max_len=max_len)
+        check_attention(out, l, ref, "pages, %d" % there)
+        if width == 13:
+            out, l = run_packed(q, case.keys, case.values, cu(ql), cu(kl), max_len=max_len)
+            check_attention(out, l, ref, "packed, %d" % there)
+
+
+def sampled(q, keys, values, ql, kl, picks):
+    """The reference of some rows only: (sequence, row) pairs."""
+    starts = cu(ql).tolist()
+    at = [starts[i] + r for i, r in picks]
+    seen = [kl[i] - ql[i] + r + 1 for i, r in picks]
+    return at, attention64(q[at], [keys[i][:n] for (i, _), n in zip(picks, seen)],
+                           [values[i][:n] for (i, _), n in zip(picks, seen)],
+                           [1] * len(picks), seen)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("ql,kl", [([700, 1, 600], [700, 90, 1000]), ([1500], [1500])])
+def test_prompts_in_tiles_of_256_rows(ql, kl, paged):
+    """Enough rows and heads for the wide tiles of bf16 queries."""
+    H, Hkv, hd = 128, 16, 64
+    case = PoolCase(kl, Hkv, hd, 16, seed=len(ql))
+    n = sum(ql)
+    assert n * (H // Hkv) // 256 * Hkv >= 1024 - 700  # (1301 rows stay below, 1500 do not)
+    q = rows(n + 2, H, hd, BF16)
+    picks = [(i, r) for i, m in enumerate(ql) for r in sorted({0, 1, 63, 64, m // 2, m - 1})
+             if r < m]
+    at, ref = sampled(q, case.keys, case.values, ql, kl, picks)
+    if paged:
+        k, v, lens, table = case.device()
+        out, l = torch.full_like(q, 9.0).cuda(), torch.full(q.shape[:2], 9.0, device="cuda")
+        B.aio_paged_attention(q.cuda(), k, v, lens, table, out, cu_q=cu(ql).cuda(), lse=l)
+    else:
+        out, l = run_packed(q, case.keys, case.values, cu(ql), cu(kl))
+    check_attention(out[at], l[at], ref)
+    assert (out[n:] == 9).all()
+    # the other rows by their own type's other kernel: fp32 queries of the same values
+    qf = q.float()
+    if paged:
+        of = torch.empty_like(qf).cuda()
+        B.aio_paged_attention(qf.cuda(), k, v, lens, table, of, cu_q=cu(ql).cuda())
+    else:
+        of, _ = run_packed(qf, case.keys, case.values, cu(ql), cu(kl))
+    # each bf16 output within its weights' and its own rounding: 2^-8 (sum p |v| + |out|),
+    # and sum p |v| is at most the largest |v|, about 4
+    assert (out[:n].float() - of[:n]).abs().max() <= 2.0 ** -8 * (4.5 + 4.5)
+
+
+def test_a_long_prompt_over_all_orders():
+    """More tiles than a wave counts at once, sequences of every length class, prefixes:
+    every row is computed by exactly one workgroup (none missing, none twice)."""
+    ql = [1 + (37 * i) % 300 for i in range(64)]
+    kl = [a + (91 * i) % 500 for i, a in enumerate(ql)]
+    case = PoolCase(kl, 1, 64, 32)
+    q = rows(sum(ql), 2, 64, BF16)
+    picks = [(i, r) for i, m in enumerate(ql) for r in {0, m - 1}]
+    at, ref = sampled(q, case.keys, case.values, ql, kl, picks)
+    out, l = run_packed(q, case.keys, case.values, cu(ql), cu(kl))
+    assert torch.isfinite(out).all() and (out[: sum(ql)] != 9).any(-1).all()
+    check_attention(out[at], l[at], ref)
+    ql2 = ql + [5, 0, 70]  # past 64 sequences: one after the other
+    kl2 = kl + [5, 3, 90]
+    case = PoolCase(kl2, 1, 64, 32)
+    q = rows(sum(ql2), 2, 64, BF16)
+    picks = [(i, r) for i, m in enumerate(ql2) for r in {0, m - 1} if 0 <= r < m]
+    at, ref = sampled(q, case.keys, case.values, ql2, kl2, picks)
+    out, l = run_packed(q, case.keys, case.values, cu(ql2), cu(kl2))
+    assert (out != 9).any(-1).all()
+    check_attention(out[at], l[at], ref)
+
+
+def test_boundaries_that_overlap():
+    """Row boundaries that run backwards or overlap stay inside the buffers."""
+    q = rows(90, 2, 64, BF16)
+    case = PoolCase([90], 1, 64, 16)
+    for bad in ([0, 90, 0, 90, 0, 90], [0, 50, 20, 90, 10, 5], [90, 0, 90, 0, 90, 0],
+                [5, -5, 1 << 30, -(1 << 31), 7, 90]):
+        c = torch.tensor(bad, dtype=torch.int32)
+        out, l = run_packed(q, case.keys, case.values, c, cu([18] * 5))
+        assert out.shape == q.shape
+
+
 # ------------------------------------------------------- streams and graphs
 
 def test_other_streams_and_workspaces():
@@ -380,6 +477,21 @@ def test_offsets_past_32_bits():
     out = torch.empty((7, 16, hd), device="cuda")
     B.aio_paged_attention(q.cuda(), pool, vpool, lens, table, out, cu_q=cu([7]).cuda())
     check_attention(out, None, attention64(q, case.keys, case.values, [7], [300]))
+
+
+def test_single_heads_and_pages_of_any_stride():
+    """The stride of a dimension of one says nothing and is not looked at."""
+    case = PoolCase([9], 1, 64, 16, spare=0)
+    k, v, lens, table = case.device()
+    k1 = torch.empty(17 + k.numel(), dtype=BF16, device="cuda")[8: 8 + k.numel()]
+    v1 = torch.empty_like(k1)
+    k1.copy_(k.reshape(-1))
+    v1.copy_(v.reshape(-1))
+    k1, v1 = (t.as_strided(k.shape, (3, 5, 64, 1)) for t in (k1, v1))
+    q = rows(1, 2, 64, F32)
+    out = torch.empty_like(q).cuda()
+    B.aio_paged_attention(q.cuda(), k1, v1, lens, table, out)
+    check_attention(out, None, attention64(q, case.keys, case.values, [1], [9]))
 
 
 def test_binding_refuses():

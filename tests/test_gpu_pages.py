@@ -101,6 +101,18 @@ def test_append_stays_inside():
         torch.cuda.synchronize()
 
 
+def test_append_through_a_narrow_view_of_a_table():
+    """The columns of the table behind the view are not looked at."""
+    case = PoolCase([30, 40], 1, 64, 16, width_more=0)
+    g = torch.Generator().manual_seed(8)
+    kr, vr = torch.randn((2, 60, 1, 64), generator=g).unbind(0)
+    k, v, lens, table = case.device()
+    B.aio_page_append(kr.cuda(), vr.cuda(), k, v, lens, table[:, :2], cu_q=cu([25, 35]).cuda(),
+                      max_len=1000)
+    want = expect_append(case, kr, vr, [25, 35], [30, 40], 32)
+    assert same_bits(torch.stack((k, v)).cpu(), want)
+
+
 def test_append_many_sequences():
     ql = [i % 3 for i in range(200)]
     kl = [q + i % 20 for i, q in enumerate(ql)]
