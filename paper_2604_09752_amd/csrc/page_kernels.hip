@@ -11,7 +11,8 @@ namespace {
 constexpr int kBlock = 256;
 
 // One workgroup per new row: 8 elements (16 bytes of cache) per thread, K and
-// V.  The row's sequence is the number of sequences that end at or before it,
+// V (2224 rows of the 7B's 32 heads, fp32: 24 us, 4.5 TB/s; 16 rows of the 1B: 3.5,
+// the launch and two dependent reads).  The row's sequence is the number of sequences that end at or before it,
 // counted 64 at a time by ballot.
 template <bool F32>
 __global__ __launch_bounds__(kBlock) void k_page_append(AppendArgs a) {
@@ -65,7 +66,9 @@ __global__ __launch_bounds__(kBlock) void k_page_append(AppendArgs a) {
   }
 }
 
-// Workgroup (chunk, copy, plane): 16 KB of one page of one plane.
+// Workgroup (chunk, copy, plane): 16 KB of one page of one plane, past the caches.
+// 200 pages of the 1B (629 MB read and written): 112 us, 5.6 TB/s, where a large copy
+// runs at 5.2 (through the caches 124 us).
 constexpr int kCopyUnroll = 4;
 constexpr int kCopyChunk = kBlock * 16 * kCopyUnroll;
 
@@ -77,10 +80,10 @@ __global__ __launch_bounds__(kBlock) void k_page_copy(CopyArgs a) {
   u32x4 v[kCopyUnroll];
 #pragma unroll
   for (int i = 0; i < kCopyUnroll; ++i)
-    if (at + i * kBlock * 16 < a.bytes) v[i] = *(const u32x4*)(src + i * kBlock * 16);
+    if (at + i * kBlock * 16 < a.bytes) v[i] = __builtin_nontemporal_load((const u32x4*)(src + i * kBlock * 16));
 #pragma unroll
   for (int i = 0; i < kCopyUnroll; ++i)
-    if (at + i * kBlock * 16 < a.bytes) *(u32x4*)(dst + i * kBlock * 16) = v[i];
+    if (at + i * kBlock * 16 < a.bytes) __builtin_nontemporal_store(v[i], (u32x4*)(dst + i * kBlock * 16));
 }
 
 }  // namespace
