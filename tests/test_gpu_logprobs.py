@@ -64,6 +64,31 @@ def test_order_of_ties_and_runs(dtype):
     check(x.repeat(70, 1), t.repeat(70), 5)  # one slice per row
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n", [(1, 2049), (1, 4100), (2, 8195), (120, 9000), (1, 131072),
+                                    (200, 17000), (3, 600001)])
+def test_joined_slices(rows, n, dtype):
+    """Rows split over workgroups: more alternatives than slices or fewer, the largest
+    values all in the first slice, all in the last, one in each, or nearly nothing left
+    in a slice."""
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn((rows, n), generator=g).to(dtype)
+    kinds = [x[0].clone()]
+    for at in (slice(0, 40), slice(n - 40, n), slice(0, n, max(n // 40, 1))):
+        y = x[0].clone()
+        y[at] += 9
+        kinds.append(y)
+    few = torch.full((n,), -math.inf, dtype=dtype)
+    few[[1, n // 2, n - 1]] = 1.0
+    few[n - 3] = 2.0
+    kinds.append(few)
+    for y in kinds:
+        x[-1] = y
+        t = torch.randint(0, n, (rows,), generator=g, dtype=torch.int32)
+        for top in (1, 7, 32):
+            check(x, t, top)
+
+
 def test_targets_outside():
     x = torch.randn((5, 100))
     t = torch.tensor([-1, 100, -100, 99, 1 << 30], dtype=torch.int32)
