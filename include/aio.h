@@ -493,7 +493,8 @@ typedef struct aio_seqs {
 
 /* Queries and outputs of an attention: [n_rows][n_heads][head_dim], fp32 or
  * bf16 (both the same), rows q_stride and out_stride elements apart (whole
- * numbers of 16 bytes).  fp32 queries keep fp32 accuracy throughout (exact
+ * numbers of 16 bytes; output rows must not overlap).  out_dev may be q_dev with
+ * the same stride.  fp32 queries keep fp32 accuracy throughout (exact
  * splits into three bf16 terms, of the queries and of the softmax weights);
  * with bf16 ones the softmax weights are rounded to bf16 too.  Sums and
  * softmax statistics are fp32 in both.  Query head h reads kv head
@@ -544,7 +545,8 @@ int aio_packed_attention(const aio_packed_kv* kv, const aio_seqs* s, const aio_a
  * fp32 is rounded to the nearest bf16, ties to even, as everywhere in a cache.
  * A row that falls before key 0, past max_len or the table's width, or into a hole
  * is not written.  Two sequences of one call must not write the same slot
- * (aio_pages_extend sees to that).  Errors as aio_paged_attention. */
+ * (aio_pages_extend sees to that), nor may pages or heads of the pool overlap
+ * (AIO_EINVAL where the strides show it).  Errors as aio_paged_attention. */
 int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_rows_dev,
                     const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                     int64_t head_stride, void* hip_stream);

@@ -846,7 +846,7 @@ int check_paged_forward(const aio_model* m, const aio_paged_pool& p, int32_t n_s
   const int rc = aio_check_paged(kv);
   if (rc) return rc;
   if (kv.n_kv_heads != c.n_kv_heads || kv.head_dim != c.head_dim || p.n_layers != c.n_layers ||
-      p.layer_stride < 0 || p.layer_stride % 8)
+      p.layer_stride < 0 || p.layer_stride % 8 || aio_pages_overlap(kv))
     return AIO_EINVAL;
   if (n_seqs < 1 || n_seqs > (1 << 20) || n_out < 0) return AIO_ERANGE;
   int64_t total = 0;
@@ -926,7 +926,6 @@ int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
     host.push_back(0);
     for (int32_t i = 0; i < n_seqs; ++i) host.push_back(host.back() + rows[i]);
     host.insert(host.end(), table, table + (size_t)n_seqs * table_stride);
-    // (rows asked for more than once go out in several copies of R)
     s.pf.tokens = s.ints;
     pass.pos = s.ints + R;
     pass.seqs.n_seqs = n_seqs;
@@ -941,6 +940,7 @@ int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
     hipError_t e = hipMemcpyAsync(s.ints, host.data(), host.size() * 4, hipMemcpyHostToDevice,
                                   m->stream);
     if (e == hipSuccess) e = aio_launch_paged_pass(*m, s.pf, R, pass);
+    // (their places in turn: where rows are asked for more than once, n_out is larger than R)
     for (int32_t at = 0; at < n_out && e == hipSuccess; at += R) {
       const int32_t some = std::min(n_out - at, R);
       e = hipMemcpyAsync(out_dev, out_rows + at, (size_t)some * 4, hipMemcpyHostToDevice,

@@ -52,6 +52,7 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   if (a.q_stride < 0 || a.q_stride % unit || a.out_stride < 0 || a.out_stride % unit)
     return AIO_EINVAL;
   if (!(a.scale > 0.f) || !isfinite(a.scale)) return AIO_EINVAL;
+  if (s.n_rows > 1 && a.out_stride < (int64_t)a.n_heads * hd) return AIO_EINVAL;  // (rows overlap)
   if (s.n_rows == 0 || s.n_seqs == 0) return AIO_OK;
   if (!good(a.q_dev, 16) || !good(a.out_dev, 16) || !aligned(a.lse_dev, 4)) return AIO_EINVAL;
   if (p.ws && (!good(ws, 16) || ws_bytes < p.ws)) return AIO_EINVAL;
@@ -93,6 +94,11 @@ int aio_check_paged(const aio_paged_kv& kv) {
   if (!page_size_ok(kv.page_size) || (kv.head_dim != 64 && kv.head_dim != 128))
     return AIO_EUNSUPPORTED;
   return AIO_OK;
+}
+
+bool aio_pages_overlap(const aio_paged_kv& kv) {
+  const int64_t one = (int64_t)kv.page_size * kv.head_dim;
+  return (kv.n_pages > 1 && kv.page_stride < one) || (kv.n_kv_heads > 1 && kv.head_stride < one);
 }
 
 // ------------------------------------------------------------- page tables
@@ -207,6 +213,8 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
   if (rc) return rc;
   if (s->n_seqs < 0 || s->n_rows < 0 || s->max_len < 0) return AIO_ERANGE;
   if (!s->cu_q_dev && s->n_rows != s->n_seqs) return AIO_ERANGE;
+  if (s->n_rows > kMostGroups) return AIO_ERANGE;
+  if (aio_pages_overlap(*kv)) return AIO_EINVAL;
   if (dtype != AIO_F32 && dtype != AIO_BF16) return AIO_EINVAL;
   const int64_t unit = dtype == AIO_F32 ? 4 : 8;
   if (row_stride < 0 || row_stride % unit || head_stride < 0 || head_stride % unit)
@@ -238,7 +246,7 @@ int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t
     return AIO_EINVAL;
   if (n == 0) return AIO_OK;
   if (!good(pool_dev, 16) || !src || !dst) return AIO_EINVAL;
-  if (page_bytes > ((int64_t)1 << 40)) return AIO_ERANGE;  // (grid.x)
+  if (page_bytes > ((int64_t)1 << 37)) return AIO_ERANGE;  // (below kMostGroups chunks of 16 KB)
   for (int32_t i = 0; i < n; ++i)
     if (src[i] < 0 || src[i] >= n_pages || dst[i] < 0 || dst[i] >= n_pages) return AIO_ERANGE;
   const int rc = guarded([&] {

@@ -17,9 +17,13 @@ constexpr int kMaxGroup = 16;
 // CUs that the splits are made for: those of the one GPU this is written for.
 // (Sizes of workspaces are asked for without a device.)
 constexpr int kCUs = 256;
+// A grid's axis holds fewer than 2^32 threads: workgroups of 256 or 512 of them.
+constexpr int64_t kMostGroups = 0xffffffffll / 256, kMostGroups512 = 0xffffffffll / 512;
 
 // AIO_OK, or what the entry points return for this pool.
 int aio_check_paged(const aio_paged_kv& kv);
+// Pages or heads that would take each other's rows: not to be written.
+bool aio_pages_overlap(const aio_paged_kv& kv);
 
 // A pure host description of one attention's launch.
 struct AttnPlan {

@@ -151,6 +151,32 @@ def test_sizes_past_32_bits_are_refused(L):
     assert L.aio_paged_attention(R(paged()), R(s), R(attn()), P16, 1 << 62, None) == B.AIO_ERANGE
 
 
+def test_grids_past_32_bits_are_refused(L):
+    """A grid's axis holds fewer than 2^32 threads, 2^24 workgroups of 256."""
+    n = 1 << 24
+    s = seqs(n_seqs=n, n_rows=n, max_len=16)
+    assert L.aio_page_append(R(paged()), R(s), P16, P16, B.AIO_F32, 512, 64, None) == B.AIO_ERANGE
+    s = seqs(n_seqs=n // 8, n_rows=n // 8, max_len=16)
+    assert L.aio_paged_attention(R(paged()), R(s), R(attn()), P16, 1 << 62, None) == B.AIO_ERANGE
+    s = seqs(n_seqs=n // 8, n_rows=n // 8, max_len=16, cu_q_dev=P16)
+    assert L.aio_paged_attention(R(paged()), R(s), R(attn()), P16, 1 << 62, None) == B.AIO_ERANGE
+    one = (ctypes.c_int32 * 1)(0)
+    two = (ctypes.c_int32 * 1)(1)
+    for size, code in ((1 << 38, B.AIO_ERANGE), (0, B.AIO_OK)):
+        assert L.aio_page_copy(P16, 1, 2 << 38, 2, 1 << 38, size, ctypes.addressof(one),
+                               ctypes.addressof(two), 1, None) == code
+
+
+def test_outputs_that_overlap_are_refused(L):
+    for a in (attn(out_stride=0), attn(out_stride=16 * 64 - 4)):
+        assert L.aio_paged_attention(R(paged()), R(seqs()), R(a), P16, 1 << 30,
+                                     None) == B.AIO_EINVAL
+    for kv in (paged(page_stride=0), paged(head_stride=0), paged(page_stride=16 * 64 - 8),
+               paged(head_stride=16 * 64 - 8)):
+        assert L.aio_page_append(R(kv), R(seqs()), P16, P16, B.AIO_F32, 512, 64,
+                                 None) == B.AIO_EINVAL
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(dtype=5), B.AIO_EINVAL), (dict(row=514), B.AIO_EINVAL), (dict(head=-4), B.AIO_EINVAL),
     (dict(k=None), B.AIO_EINVAL), (dict(v=8), B.AIO_EINVAL),
