@@ -455,6 +455,51 @@ def test_captured_and_replayed():
             assert torch.equal(x, y)
 
 
+def test_two_graphs_share_a_workspace():
+    """Replayed one after the other on one stream, whatever the other left behind."""
+    lens = [3000, 1700]
+    case = PoolCase(lens, 2, 128, 16)
+    k, v, ln, table = case.device()
+    need = B.aio_attn_workspace_bytes(2, 2, 3000, 8, 2, 128)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    qs = [rows(2, 8, 128, d, seed=s).cuda() for s, d in ((5, F32), (6, BF16))]
+    outs = [torch.empty_like(q) for q in qs]
+    graphs = []
+    for q, out in zip(qs, outs):
+        B.aio_paged_attention(q, k, v, ln, table, out, max_len=3000, ws=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.aio_paged_attention(q, k, v, ln, table, out, max_len=3000, ws=ws)
+        graphs.append(g)
+    refs = [attention64(q.cpu(), case.keys, case.values, [1, 1], lens) for q in qs]
+    first = None
+    for _ in range(3):
+        for out, g in zip(outs, graphs):
+            out.fill_(float("nan"))
+            g.replay()
+        torch.cuda.synchronize()
+        for out, ref in zip(outs, refs):
+            check_attention(out, None, ref)
+        first = first or [o.clone() for o in outs]
+        assert all(torch.equal(a, b) for a, b in zip(first, outs))
+        ws.fill_(255)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens,ql", [([40, 700, 3000], None), ([90, 33, 1500], [70, 33, 300])])
+def test_out_in_the_place_of_the_queries(lens, ql, dtype):
+    case = PoolCase(lens, 2, 64, 16)
+    k, v, ln, table = case.device()
+    q = rows(sum(ql or [1] * len(lens)), 8, 64, dtype)
+    ref = attention64(q, case.keys, case.values, ql or [1] * len(lens), lens)
+    qd = q.cuda()
+    kw = {} if ql is None else {"cu_q": cu(ql).cuda()}
+    B.aio_paged_attention(qd, k, v, ln, table, qd, max_len=max(lens), **kw)
+    torch.cuda.synchronize()
+    check_attention(qd, None, ref)
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 2^31 elements and 2^32 bytes: the last pages."""
     page, Hkv, hd = 256, 8, 128
