@@ -237,6 +237,43 @@ def test_prompt_values_a_row_does_not_see(length, dtype, bad):
         assert (err <= ref[2][at: at + 5][:, :, keep]).all(), form
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd", [(2, 1, 64), (1, 1, 128)])
+@pytest.mark.parametrize("ql,length", [(200, 330), (40, 700), (130, 130)])
+def test_prompt_values_that_are_not_finite(ql, length, H, Hkv, hd, dtype):
+    """An infinite value in one, the next or several of the last key tiles, or in the
+    last key: the rows that see it are not finite there, the others and the other
+    dimensions are as without it.  Infinite or NaN: the weight p > 0 of an fp32 row goes
+    into the product as p1 + p2 + p3, and inf p1 + inf p2 + inf p3 is inf where all three
+    are positive and NaN where p needs fewer than 24 bits and one of them is 0."""
+    case = PoolCase([length], Hkv, hd, 16)
+    q = rows(ql, H, hd, dtype)
+    ref = attention64(q, case.keys, case.values, [ql], [length])
+    first = length - ql  # the last key that all rows see
+    for at in ([length - 1], [length - 30], [first + 1], [length - 100, length - 99],
+               [length - 20, length - 84], list(range(first + 3, length, 61))):
+        at = [a for a in at if a > first]
+        value = case.values[0].clone()
+        for i, a in enumerate(at):
+            value[a, :, i] = float("inf")
+        pool = PoolCase([length], Hkv, hd, 16)
+        for a in at:
+            pg, sl = int(pool.table[0, a // 16]), a % 16
+            pool.v[pg, :, sl] = value[a]
+        k, v, lens, table = pool.device()
+        out, l = torch.empty_like(q).cuda(), torch.empty(q.shape[:2], device="cuda")
+        B.aio_paged_attention(q.cuda(), k, v, lens, table, out, cu_q=cu([ql]).cuda(), lse=l)
+        packed, pl = run_packed(q, case.keys, [value], cu([ql]), cu([length]))
+        for o, s in ((out, l), (packed, pl)):
+            o = o.cpu()
+            want = [t.clone() for t in ref]
+            for i, a in enumerate(at):
+                assert not torch.isfinite(o[a - first:, :, i]).any(), (at, a)
+                # (a row's own last key weighs something: the row is as it was elsewhere)
+                o[a - first:, :, i] = want[0][a - first:, :, i].to(dtype)
+            check_attention(o, s.cpu(), want, at)
+
+
 def test_prompt_nan_row():
     q = rows(70, 2, 64, F32)
     case = PoolCase([70], 2, 64, 16)
