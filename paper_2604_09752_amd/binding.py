@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -139,11 +140,12 @@ def lib():
         L.aio_spec_generate.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp,
                                         P(aio_spec_stats)]
         i64, sz = ctypes.c_int64, ctypes.c_size_t
-        L.aio_attn_workspace_bytes.argtypes = [P(aio_seqs), i32, i32, i32]
+        L.aio_attn_workspace_bytes.argtypes = [vp, i32, i32, i32]
         L.aio_attn_workspace_bytes.restype = sz
-        L.aio_paged_attention.argtypes = [P(aio_paged_kv), P(aio_seqs), P(aio_attn), vp, sz, vp]
-        L.aio_packed_attention.argtypes = [P(aio_packed_kv), P(aio_seqs), P(aio_attn), vp, sz, vp]
-        L.aio_page_append.argtypes = [P(aio_paged_kv), P(aio_seqs), vp, vp, i32, i64, i64, vp]
+        # (structs by address: byref of one, or its bytes)
+        L.aio_paged_attention.argtypes = [vp, vp, vp, vp, sz, vp]
+        L.aio_packed_attention.argtypes = [vp, vp, vp, vp, sz, vp]
+        L.aio_page_append.argtypes = [vp, vp, vp, vp, i32, i64, i64, vp]
         L.aio_page_copy.argtypes = [vp, i32, i64, i32, i64, i64, vp, vp, i32, vp]
         L.aio_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.aio_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
@@ -394,6 +396,26 @@ def _need(ok: bool, what: str):
 # (A decode step's calls are as short as their launches: the checks below look
 # at each tensor once, and a stream is asked for as a number.)
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
+def _packer(cls):
+    """The fields of a struct to its bytes, in a quarter of the time that an
+    instance of cls takes."""
+    codes = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
+    s = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
+    assert s.size == ctypes.sizeof(cls)
+
+    def pack(*fields) -> bytes:
+        try:
+            return s.pack(*fields)
+        except (struct.error, OverflowError) as e:
+            raise ValueError("%s: %s" % (cls.__name__, e)) from None
+    return pack
+
+
+_pack_paged, _pack_packed, _pack_seqs, _pack_attn = map(
+    _packer, (aio_paged_kv, aio_packed_kv, aio_seqs, aio_attn))
 
 
 def _device_of(first: torch.Tensor, *others) -> int:
@@ -408,7 +430,7 @@ def _device_of(first: torch.Tensor, *others) -> int:
 
 def _launch(at: int, call, *args) -> int:
     """call(*args, stream) with device ``at`` current, on its current stream."""
-    if torch.cuda.current_device() == at:
+    if _current_device() == at:
         return call(*args, _raw_stream(at))
     with torch.cuda.device(at):
         return call(*args, _raw_stream(at))
@@ -428,32 +450,35 @@ def _rows3(t: torch.Tensor, shape, what: str) -> int:
     return row if n > 1 else h * d
 
 
-def _paged(k: torch.Tensor, v: torch.Tensor) -> aio_paged_kv:
+def _paged(k: torch.Tensor, v: torch.Tensor):
+    """(aio_paged_kv's bytes, kv heads, page size, head_dim)"""
     shape, stride = k.shape, k.stride()
     if (len(shape) != 4 or v.shape != shape or k.dtype is not torch.bfloat16 or
             v.dtype is not torch.bfloat16):
         raise ValueError("pages: two bf16 [n_pages, kv_heads, page_size, head_dim]")
-    if v.stride() != stride or stride[3] != 1 or stride[2] != shape[3]:
+    pages, heads, size, hd = shape
+    page_stride, head_stride, slot, one = stride
+    if v.stride() != stride or one != 1 or slot != hd:
         raise ValueError("pages: K and V of the same strides, slots and dimensions contiguous")
     # (the stride of a single head or page says nothing)
-    return aio_paged_kv(k.data_ptr(), v.data_ptr(), stride[0] if shape[0] > 1 else 0,
-                        stride[1] if shape[1] > 1 else 0, shape[0], shape[2], shape[1], shape[3])
+    return _pack_paged(k.data_ptr(), v.data_ptr(), page_stride if pages > 1 else 0,
+                       head_stride if heads > 1 else 0, pages, size, heads, hd), heads, size, hd
 
 
-def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_seqs:
-    shape, stride = table.shape, table.stride()
+def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> bytes:
+    shape = table.shape
     if (table.dtype is not torch.int32 or lens.dtype is not torch.int32 or len(shape) != 2 or
             lens.shape != shape[:1]):
         raise ValueError("lens and table: int32 [n] and [n, width]")
     n, width = shape
+    row, one = table.stride()
     if n > 1:
-        _need((width <= 1 or stride[1] == 1) and lens.stride(0) == 1,
+        _need((width <= 1 or one == 1) and lens.stride(0) == 1,
               "lens and table: rows have to be contiguous")
-        width_stride = stride[0]
     else:
-        _need(width <= 1 or stride[1] == 1, "table: rows have to be contiguous")
-        width_stride = width
-    cu = None
+        _need(width <= 1 or one == 1, "table: rows have to be contiguous")
+        row = width
+    cu = 0
     if cu_q is not None:
         if cu_q.dtype is not torch.int32 or cu_q.shape != (n + 1,) or (n and cu_q.stride(0) != 1):
             raise ValueError("cu_q: contiguous int32, one more entry than sequences")
@@ -462,19 +487,25 @@ def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> aio_
     most = min(width * page_size, 1 << 30)
     if max_len is None or max_len > most:
         max_len = most
-    return aio_seqs(n, n_rows, max_len, cu, lens.data_ptr(), table.data_ptr(), width_stride, None)
+    return _pack_seqs(n, n_rows, max_len, cu, lens.data_ptr(), table.data_ptr(), row, 0)
 
 
-def _attn(q, out, lse, scale) -> aio_attn:
+def _attn(q, out, lse, scale) -> bytes:
     shape, dtype = q.shape, q.dtype
     if len(shape) != 3 or out.shape != shape or out.dtype is not dtype or dtype not in _DTYPES:
         raise ValueError("q and out: both fp32 or both bf16 [rows, heads, head_dim]")
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != shape[:2] or
-                            not lse.is_contiguous()):
-        raise ValueError("lse: contiguous fp32 [rows, heads]")
-    return aio_attn(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                    _rows3(q, shape, "q"), _rows3(out, shape, "out"), _DTYPES[dtype], shape[1],
-                    shape[2] ** -0.5 if scale is None else scale)
+    if lse is None:
+        lse_ptr = 0
+    else:
+        if (lse.dtype is not torch.float32 or lse.shape != shape[:2] or
+                not lse.is_contiguous()):
+            raise ValueError("lse: contiguous fp32 [rows, heads]")
+        lse_ptr = lse.data_ptr()
+    _, heads, hd = shape
+    q_stride = heads * hd if q.is_contiguous() else _rows3(q, shape, "q")
+    out_stride = heads * hd if out.is_contiguous() else _rows3(out, shape, "out")
+    return _pack_attn(q.data_ptr(), out.data_ptr(), lse_ptr, q_stride, out_stride, _DTYPES[dtype],
+                      heads, hd ** -0.5 if scale is None else scale)
 
 
 def _workspace(nbytes: int, ws, device):
@@ -497,14 +528,14 @@ def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: in
     return int(lib().aio_attn_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
 
 
-def _attend(name, at, kv, s, a, n_kv_heads, head_dim, device, ws):
-    L = lib()
-    s, a = ctypes.byref(s), ctypes.byref(a)
-    n = L.aio_attn_workspace_bytes(s, a._obj.n_heads, n_kv_heads, head_dim)
-    ws, w = _workspace(n, ws, device)
-    rc = _launch(at, getattr(L, name), ctypes.byref(kv), s, a, w, n)
+def _attend(call, at, kv, s, a, n_heads, n_kv_heads, head_dim, device, ws):
+    n = lib().aio_attn_workspace_bytes(s, n_heads, n_kv_heads, head_dim)
+    w = None
+    if n:
+        ws, w = _workspace(n, ws, device)
+    rc = _launch(at, call, kv, s, a, w, n)
     if rc:
-        raise AioError(rc, name)
+        raise AioError(rc, call.__name__)
 
 
 def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
@@ -517,11 +548,13 @@ def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens:
     prompts, causal.  max_len: no sequence is longer (default: the table's
     width; a closer one gives a better split of the work)."""
     at = _device_of(q, k, v, lens, table, out, cu_q, lse, ws)
-    kv, a = _paged(k, v), _attn(q, out, lse, scale)
-    rows, _, hd = q.shape
-    _need(hd == kv.head_dim, "q and k differ in head_dim")
-    s = _paged_seqs(lens, table, cu_q, rows, max_len, kv.page_size)
-    _attend("aio_paged_attention", at, kv, s, a, kv.n_kv_heads, hd, q.device, ws)
+    kv, kv_heads, page_size, hd = _paged(k, v)
+    a = _attn(q, out, lse, scale)
+    rows, heads, q_hd = q.shape
+    if q_hd != hd:
+        raise ValueError("q and k differ in head_dim")
+    s = _paged_seqs(lens, table, cu_q, rows, max_len, page_size)
+    _attend(lib().aio_paged_attention, at, kv, s, a, heads, kv_heads, hd, q.device, ws)
 
 
 def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
@@ -541,11 +574,11 @@ def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q
         _i32(t, 1, what)
     _need(cu_q.shape == cu_k.shape and cu_q.shape[0] >= 1, "cu_q and cu_k differ in length")
     rows, heads, hd = k.shape
-    kv = aio_packed_kv(k.data_ptr(), v.data_ptr(), k.stride(0) if rows > 1 else 0,
-                       k.stride(1) if heads > 1 else 0, rows, heads, hd)
-    s = aio_seqs(cu_q.shape[0] - 1, q.shape[0], rows if max_len is None else max_len,
-                 cu_q.data_ptr(), None, None, 0, cu_k.data_ptr())
-    _attend("aio_packed_attention", at, kv, s, a, kv.n_kv_heads, kv.head_dim, q.device, ws)
+    kv = _pack_packed(k.data_ptr(), v.data_ptr(), k.stride(0) if rows > 1 else 0,
+                      k.stride(1) if heads > 1 else 0, rows, heads, hd)
+    s = _pack_seqs(cu_q.shape[0] - 1, q.shape[0], rows if max_len is None else max_len,
+                   cu_q.data_ptr(), 0, 0, 0, cu_k.data_ptr())
+    _attend(lib().aio_packed_attention, at, kv, s, a, q.shape[1], heads, hd, q.device, ws)
 
 
 def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -554,15 +587,15 @@ def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor,
     """Write the new rows' keys and values ([rows, kv_heads, head_dim], fp32 or
     bf16) into their pages; lens counts them already."""
     at = _device_of(k, v, k_rows, v_rows, lens, table, cu_q)
-    kv = _paged(k, v)
+    kv, kv_heads, page_size, hd = _paged(k, v)
     shape, stride, dtype = k_rows.shape, k_rows.stride(), k_rows.dtype
     if (len(shape) != 3 or v_rows.shape != shape or v_rows.dtype is not dtype or
-            dtype not in _DTYPES or shape[1] != kv.n_kv_heads or shape[2] != kv.head_dim):
+            dtype not in _DTYPES or shape[1] != kv_heads or shape[2] != hd):
         raise ValueError("rows: two fp32 or bf16 [rows, kv_heads, head_dim]")
     if v_rows.stride() != stride or stride[2] != 1:
         _need(k_rows.numel() == 0, "rows: the same strides, dimensions contiguous")
-    s = _paged_seqs(lens, table, cu_q, shape[0], max_len, kv.page_size)
-    rc = _launch(at, lib().aio_page_append, ctypes.byref(kv), ctypes.byref(s), k_rows.data_ptr(),
+    s = _paged_seqs(lens, table, cu_q, shape[0], max_len, page_size)
+    rc = _launch(at, lib().aio_page_append, kv, s, k_rows.data_ptr(),
                  v_rows.data_ptr(), _DTYPES[dtype], stride[0] if shape[0] > 1 else 0,
                  stride[1] if shape[1] > 1 else 0)
     if rc:

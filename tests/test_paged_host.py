@@ -350,3 +350,21 @@ def test_paged_forward_rejects_without_a_device(L):
     p = B.aio_paged_pool(paged(), 64, 2)
     assert L.aio_paged_forward(None, R(p), 1, i, i, i, 1, i, i, 1, P16, 256, 1 << 30) == B.AIO_EINVAL
     assert L.aio_paged_forward_bytes(None, 1, 1, 1) == 0
+
+
+@pytest.mark.parametrize("cls,pack,fields", [
+    (B.aio_paged_kv, B._pack_paged, (16, 32, 1 << 40, 1 << 33, 10, 16, 8, 64)),
+    (B.aio_packed_kv, B._pack_packed, (16, 32, 1 << 40, 64, 100, 8, 64)),
+    (B.aio_seqs, B._pack_seqs, (4, 5, 100, 16, 32, 48, 8, 64)),
+    (B.aio_attn, B._pack_attn, (16, 32, 0, 1024, 2048, 1, 16, 0.125)),
+])
+def test_packed_structs_are_the_structs(cls, pack, fields):
+    b = pack(*fields)
+    assert len(b) == ctypes.sizeof(cls)
+    s = cls.from_buffer_copy(b)
+    assert tuple(getattr(s, n) or 0 for n, _ in cls._fields_) == fields
+    for i, (_, t) in enumerate(cls._fields_):
+        big = {ctypes.c_int32: 1 << 31, ctypes.c_float: 1e300}.get(t)
+        if big:
+            with pytest.raises(ValueError, match=cls.__name__):
+                pack(*fields[:i], big, *fields[i + 1:])
