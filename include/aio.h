@@ -497,7 +497,8 @@ typedef struct aio_seqs {
  * the same stride.  fp32 queries keep fp32 accuracy throughout (exact
  * splits into three bf16 terms, of the queries and of the softmax weights);
  * with bf16 ones the softmax weights are rounded to bf16 too.  Sums and
- * softmax statistics are fp32 in both.  A value that is not finite makes the
+ * softmax statistics are fp32 in both, long ones carried in two floats (the
+ * weights' sum always, the outputs of fp32 queries).  A value that is not finite makes the
  * outputs that see it not finite (infinite or NaN), and no others.  Query head h
  * reads kv head h / (n_heads / n_kv_heads). */
 typedef struct aio_attn {

@@ -94,6 +94,26 @@ AIO_DEV void store_out(const AttnArgs& a, bool f32, int64_t at, float v) {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// A long sum in two floats: hi becomes the rounded hi + lo, lo what that is off by (exactly
+// where hi is the larger, to 2^-24 of lo else), from which the next additions go on.  In one
+// float, weights that are all alike (repeated keys) round the same way each time: 32768
+// keys of one score, added one by one, left a row's sum 1.8e-4 off, 131072 9e-4.  With
+// the sum carried after every block only the additions within a block round, 16 units of
+// 2^-24 at most for 32 of them.
+template <class T>
+AIO_DEV void carry(T& hi, T& lo) {
+  const T s = hi + lo;
+  lo -= s - hi;
+  hi = s;
+}
+
+// Output tiles of fp32 queries are carried alike, after this many blocks of 32 keys in
+// k_attn_step and of 64 in k_attn_rows: 96 and 384 matrix instructions on one sum in
+// between.  Equal values under 131072 equal keys: 1e-3 off in one sum of the prompt rows,
+// 4e-6 carried every 32 blocks, 2e-6 every 16; 8192 rows of 32 heads take 1406, 1432 and
+// 1457 us.  (bf16 outputs round to 2^-9, which no such chain comes near.)
+constexpr int kStepCarry = 32, kRowsCarry = 32;
+
 // ------------------------------------------------ one new token per sequence
 
 // Workgroup (sequence, kv head, split): the G query heads of the kv head are
@@ -110,11 +130,14 @@ struct StepLds {
   static constexpr int TBYTES = 32 * VROW;  // a wave's tile: the keys, then the values
   static constexpr int OROW = HD + 4;             // floats of an output row
   static constexpr int OBYTES = kWaves * kMaxGroup * OROW * 4;
-  static constexpr int BYTES = kWaves * TBYTES > OBYTES ? kWaves * TBYTES : OBYTES;
+  static constexpr int TILES = kWaves * TBYTES > OBYTES ? kWaves * TBYTES : OBYTES;
+  // the upper parts of a wave's output tile, and the maxima that they refer to
+  static constexpr int HBYTES = HD * 16 * 4 + AIO_WAVE * 4;
+  static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
 };
 
 template <int HD, int NT, bool STREAM>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : 2) void k_attn_step(AttnArgs a) {
+__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(AttnArgs a) {
   using L = StepLds<HD>;
   extern __shared__ __align__(16) char smem[];
   __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
@@ -169,7 +192,15 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : 2) void k_attn_step(AttnArgs 
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, lh = 0.f;
+  // The upper parts of o wait in LDS (in registers, 20 of them spill), with the maximum of
+  // then.
+  f32x4* park = (f32x4*)(smem + L::TILES + wid * L::HBYTES) + lane;
+  float* park_m = (float*)(smem + L::TILES + wid * L::HBYTES + HD * 16 * 4) + lane;
+  auto parked_scale = [&] {
+    const float mh = *park_m;
+    return mh == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mh - m) * a.scale_log2);
+  };
   char* tile = smem + wid * L::TBYTES;
   const char* ktr = tile + col * L::KROW + 16 * grp;
   const char* vtr = tile + (4 * grp + col / 4) * L::VROW + (col & 3) * 8;
@@ -179,80 +210,103 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : 2) void k_attn_step(AttnArgs 
     load_block(kr, kb, wid, page);
     load_block(vr, vb, wid, page);
   }
-  for (int t = wid; t < nt; t += kWaves) {
-    const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
-    // the wave's next block (its last one is read again: no branch)
-    const bool more = t + kWaves < nt;
-    const int tn = more ? t + kWaves : t, pn = more ? next : page;
+  for (int t = wid; t < nt;) {
+    const int te = NT == 3 ? min(nt, t + kStepCarry * kWaves) : nt;
+    for (; t < te; t += kWaves) {
+      const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
+      // the wave's next block (its last one is read again: no branch)
+      const bool more = t + kWaves < nt;
+      const int tn = more ? t + kWaves : t, pn = more ? next : page;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = kr[i];
-    load_block(kr, kb, tn, pn);
-    wave_lds_sync();  // the keys are in LDS
-    float p[8];
+      for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = kr[i];
+      load_block(kr, kb, tn, pn);
+      wave_lds_sync();  // the keys are in LDS
+      float p[8];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < 2; ++kt) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 ak = as_bf16x8(*(const u32x4*)(ktr + kt * 16 * L::KROW + c * 64));
+        for (int c = 0; c < NC; ++c) {
+          const bf16x8 ak = as_bf16x8(*(const u32x4*)(ktr + kt * 16 * L::KROW + c * 64));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s = mfma16(ak, q[c][n], s);
+          for (int n = 0; n < NT; ++n) s = mfma16(ak, q[c][n], s);
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[4 * kt + v] = s[v];
       }
+      wave_lds_sync();  // ... and read: the values take their place
+      // (those that may not be seen are zero: 0 x NaN is not)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) p[4 * kt + v] = s[v];
+      for (int i = 0; i < NV; ++i) {
+        u32x4 w = vr[i];
+        if (vis != 0xffffffffu && !(vis >> (i * RPL + lr) & 1)) w = u32x4{0, 0, 0, 0};
+        *(u32x4*)(tile + (i * RPL + lr) * L::VROW + ld * 2) = w;
+      }
+      load_block(vr, vb, tn, pn);
+      page = next;
+      next = load_page(t + 2 * kWaves);
+      if (vis != 0xffffffffu) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+          if (!(vis >> (v / 4 * 16 + 4 * grp + v % 4) & 1)) p[v] = -INFINITY;
+      }
+      float mx = p[0];
+#pragma unroll
+      for (int v = 1; v < 8; ++v) mx = fmaxf(mx, p[v]);
+      float other = mx;
+      swap32(mx, other);
+      mx = fmaxf(mx, other);
+      other = mx;
+      swap16(mx, other);
+      mx = fmaxf(mx, other);
+      const float mnew = fmaxf(m, mx);
+      const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+      if (__any(mnew > m)) {
+        const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+        l *= c;
+        lh *= c;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= c;
+      }
+      m = mnew;
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], a.scale_log2, -mref));
+        l += p[v];
+      }
+      carry(lh, l);
+      bf16x8 pt[NT];
+      terms<NT>(p, pt);
+      wave_lds_sync();  // the values are in LDS
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const uint2 v0 = lds_read_tr16(vtr + d * 32);
+        const uint2 v1 = lds_read_tr16(vtr + 16 * L::VROW + d * 32);
+        const bf16x8 av = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[d] = mfma16(av, pt[n], o[d]);
+      }
+      wave_lds_sync();  // every read of the tile is done before the next writes
     }
-    wave_lds_sync();  // ... and read: the values take their place
-    // (those that may not be seen are zero: 0 x NaN is not)
+    if (NT == 3 && t < nt) {
+      const bool first = t == wid + kStepCarry * kWaves;
+      const float c = first ? 0.f : parked_scale();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      u32x4 w = vr[i];
-      if (vis != 0xffffffffu && !(vis >> (i * RPL + lr) & 1)) w = u32x4{0, 0, 0, 0};
-      *(u32x4*)(tile + (i * RPL + lr) * L::VROW + ld * 2) = w;
+      for (int d = 0; d < ND; ++d) {
+        f32x4 h = {0.f, 0.f, 0.f, 0.f};
+        if (!first) h = park[d * AIO_WAVE] * c;
+        carry(h, o[d]);
+        park[d * AIO_WAVE] = h;
+      }
+      *park_m = m;
     }
-    load_block(vr, vb, tn, pn);
-    page = next;
-    next = load_page(t + 2 * kWaves);
-    if (vis != 0xffffffffu) {
-#pragma unroll
-      for (int v = 0; v < 8; ++v)
-        if (!(vis >> (v / 4 * 16 + 4 * grp + v % 4) & 1)) p[v] = -INFINITY;
-    }
-    float mx = p[0];
-#pragma unroll
-    for (int v = 1; v < 8; ++v) mx = fmaxf(mx, p[v]);
-    float other = mx;
-    swap32(mx, other);
-    mx = fmaxf(mx, other);
-    other = mx;
-    swap16(mx, other);
-    mx = fmaxf(mx, other);
-    const float mnew = fmaxf(m, mx);
-    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
-    if (__any(mnew > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
-      l *= c;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] *= c;
-    }
-    m = mnew;
-#pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], a.scale_log2, -mref));
-      l += p[v];
-    }
-    bf16x8 pt[NT];
-    terms<NT>(p, pt);
-    wave_lds_sync();  // the values are in LDS
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      const uint2 v0 = lds_read_tr16(vtr + d * 32);
-      const uint2 v1 = lds_read_tr16(vtr + 16 * L::VROW + d * 32);
-      const bf16x8 av = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[d] = mfma16(av, pt[n], o[d]);
-    }
-    wave_lds_sync();  // every read of the tile is done before the next writes
   }
+  if (NT == 3 && wid + kStepCarry * kWaves < nt) {
+    const float c = parked_scale();
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] += park[d * AIO_WAVE] * c;
+  }
+  l += lh;
   l += __shfl_xor(l, 16, AIO_WAVE);
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
@@ -318,7 +372,10 @@ template <int HD>
 struct RowsLds {
   static constexpr int KROW = HD * 2 + 16, VROW = HD * 2 + 64;  // bytes
   static constexpr int KBYTES = kKeys * KROW, VBYTES = kKeys * VROW;
-  static constexpr int BYTES = 2 * (KBYTES + VBYTES);
+  static constexpr int TILES = 2 * (KBYTES + VBYTES);
+  // the upper parts of a wave's output tile, and the references that they have
+  static constexpr int HBYTES = HD * 32 * 4 + AIO_WAVE * 4;
+  static constexpr int BYTES(int NT, int W) { return TILES + (NT == 3 ? W * HBYTES : 0); }
 };
 
 // First key of sequence i, how many of its keys are there, and how many it has by the
@@ -489,7 +546,34 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   for (int hb = 0; hb < NHB; ++hb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[hb][i] = 0.f;
-  float m = -INFINITY, l = 0.f;  // m: reference of the weights, in log2 units
+  float m = -INFINITY, l = 0.f, lh = 0.f;  // m: reference of the weights, in log2 units
+  // The upper parts of o wait in LDS, with the reference of then.
+  f32x4* park = (f32x4*)(smem + L::TILES + wid * L::HBYTES) + lane;
+  float* park_m = (float*)(smem + L::TILES + wid * L::HBYTES + HD * 32 * 4) + lane;
+  bool parked = false;
+  auto parked_scale = [&] {
+    const float mh = *park_m;
+    return mh == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mh - m);
+  };
+  // (after every kRowsCarry of the tiles)
+  auto carry_out = [&](int tiles) {
+    if (NT != 3 || tiles % kRowsCarry) return;
+    const float c = parked ? parked_scale() : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * NHB; ++i) {
+      f32x4 h = {0.f, 0.f, 0.f, 0.f}, low;
+      if (parked) h = park[i * AIO_WAVE] * c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) low[e] = o[i / 4][4 * (i % 4) + e];
+      carry(h, low);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] = low[e];
+      park[i * AIO_WAVE] = h;
+      __builtin_amdgcn_sched_barrier(0);  // (few at a time: registers)
+    }
+    *park_m = m;
+    parked = true;
+  };
   const int st_at = (wr + lr) * L::KROW + sd * 2, sv_at = (wr + lr) * L::VROW + sd * 2;
   const int k_at = rl * L::KROW + 16 * kh;
   const int v_at = (4 * kh + (lane & 15) / 4) * L::VROW +
@@ -516,6 +600,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
       const float c = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mnew);
       m = mnew;
       l *= c;
+      lh *= c;
 #pragma unroll
       for (int hb = 0; hb < NHB; ++hb)
 #pragma unroll
@@ -629,6 +714,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         for (int e = i * E; e < (i + 1) * E; ++e) mx = fmaxf(mx, sn[e / 16][e % 16]);
         __builtin_amdgcn_sched_barrier(0);
       }
+      carry(lh, l);
     };
     // (buffers by t - t0's parity: K of t0 in 0, of t0 + 1 in 1, V of t0 in 0)
     f32x16 sa[2], sb[2];
@@ -664,6 +750,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
     for (; t + 1 < tp; t += 2) {
       step(t, std::integral_constant<int, 0>{}, sa, sb);
       step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
+      carry_out(t + 2 - t0);
     }
     if (t < tp) step(t, std::integral_constant<int, 0>{}, sa, sb);
   }
@@ -761,8 +848,20 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         for (int n = 0; n < NT; ++n) o[hb] = mfma32(av, pt[n], o[hb]);
       }
     }
+    carry(lh, l);
+    carry_out(t + 1 - t0);
   }
   if (!live) return;
+  if (NT == 3 && parked) {
+    const float c = parked_scale();
+#pragma unroll
+    for (int i = 0; i < 4 * NHB; ++i) {
+      const f32x4 h = park[i * AIO_WAVE] * c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] += h[e];
+    }
+  }
+  l += lh;
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
   const int64_t rh = (int64_t)(first + row) * a.H + h0 + g;
@@ -817,7 +916,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   for (int s = lane; s < a.S; s += AIO_WAVE) M = fmaxf(M, a.part_ml[(s * all + rh) * 2]);
   M = wave_max(M);
   constexpr int PER = HD / AIO_WAVE;
-  float os[PER] = {}, ls = 0.f;
+  float os[PER] = {}, oh[PER] = {}, ls = 0.f;
   // a split's weight in its lane, then the splits with keys (the others' values were
   // not written), their loads independent of one another
   for (int s0 = 0; s0 < a.S; s0 += AIO_WAVE) {
@@ -850,6 +949,8 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) os[i] += w * v[b][i];
       }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) carry(oh[i], os[i]);
     }
   }
   ls = wave_sum(ls);
@@ -857,13 +958,13 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     store_out(a, F32, (int64_t)row * a.ldo + (int64_t)head * HD + i * AIO_WAVE + lane,
-              none ? 0.f : os[i] / ls);
+              none ? 0.f : (oh[i] + os[i]) / ls);
   if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
 }
 
 template <int HD, int NT, bool PAGED, int W>
 hipError_t launch_rows_w(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  constexpr int lds = RowsLds<HD>::BYTES;
+  constexpr int lds = RowsLds<HD>::BYTES(NT, W);
   const auto fn = k_attn_rows<HD, NT, PAGED, W>;
   const hipError_t e =
       hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -884,7 +985,7 @@ template <int HD, int NT>
 hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   hipError_t e;
   if (!p.rows) {
-    constexpr int lds = StepLds<HD>::BYTES;
+    constexpr int lds = StepLds<HD>::BYTES(NT);
     const auto fn = p.stream ? k_attn_step<HD, NT, true> : k_attn_step<HD, NT, false>;
     e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
