@@ -498,9 +498,11 @@ typedef struct aio_seqs {
  * splits into three bf16 terms, of the queries and of the softmax weights);
  * with bf16 ones the softmax weights are rounded to bf16 too.  Sums and
  * softmax statistics are fp32 in both, long ones carried in two floats (the
- * weights' sum always, the outputs of fp32 queries).  A value that is not finite makes the
- * outputs that see it not finite (infinite or NaN), and no others.  Query head h
- * reads kv head h / (n_heads / n_kv_heads). */
+ * weights' sum always, the outputs of fp32 queries).  A value that is not
+ * finite makes the outputs that see it not finite (infinite or NaN), however
+ * little it weighs, and no others; a key that is not finite may do so to the
+ * rows that see it, or weigh nothing, its value included, where a score is
+ * -infinity.  Query head h reads kv head h / (n_heads / n_kv_heads). */
 typedef struct aio_attn {
   const void* q_dev;
   void* out_dev;

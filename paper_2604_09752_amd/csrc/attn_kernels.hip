@@ -921,15 +921,18 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   // not written), their loads independent of one another
   for (int s0 = 0; s0 < a.S; s0 += AIO_WAVE) {
     float c = 0.f;
+    bool keys = false;
     if (s0 + lane < a.S) {
       const float* ml = a.part_ml + ((s0 + lane) * all + rh) * 2;
       const float x = ml[0];
-      if (x != -INFINITY) {
+      keys = x != -INFINITY;
+      if (keys) {
         c = __builtin_amdgcn_exp2f(x - M);
         ls += c * ml[1];
       }
     }
-    const uint64_t some = __ballot(c != 0.f);
+    // (those whose weight underflows among them: 0 x inf shows that they saw an infinity)
+    const uint64_t some = __ballot(keys);
     if (!some) continue;
     const int n = min(a.S - s0, AIO_WAVE), valid = __ffsll((unsigned long long)some) - 1;
     constexpr int B = 8;
