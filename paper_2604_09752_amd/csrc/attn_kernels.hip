@@ -1055,6 +1055,17 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
   return AIO_OK;
 }
 
+int aio_attention_plan(const aio_seqs* s, int H, int Hkv, int hd, int dtype, int32_t* out) {
+  if (!s || !out) return AIO_EINVAL;
+  AttnPlan p;
+  const int rc = aio_attn_plan(*s, H, Hkv, hd, dtype, &p);
+  if (rc) return rc;
+  out[0] = p.waves;
+  out[1] = p.splits;
+  out[2] = p.stream;
+  return AIO_OK;
+}
+
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd) {
   // step: splits n Hkv <= kStepGroups, so splits n H <= kStepGroups G; rows: splits tiles
   // Hkv <= kRowsGroups and n_rows G <= 256 tiles, so splits n_rows H <= 256 kRowsGroups

@@ -38,6 +38,11 @@ struct AttnPlan {
 };
 // AIO_OK, or the error that the entry points return for these sizes.
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p);
+// What an attention takes, for the tests (not part of the ABI; pure host): out[3] = waves of
+// a workgroup of prompt rows (0: one new token per sequence), splits of the keys, and
+// whether the keys pass the caches by.
+extern "C" int aio_attention_plan(const aio_seqs* s, int H, int Hkv, int hd, int dtype,
+                                  int32_t* out);
 // No attention of these heads takes more workspace, whatever its sequences.
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd);
 
