@@ -394,66 +394,68 @@ AIO_DEV void seq_keys(const AttnArgs& a, int i, int& key0, int& len, int& full) 
 }
 
 // Workgroups start in index order, and a causal tile's work grows with its last
-// position: the longest first.  Tile `t` of the launch in that order, for up to 64
+// position: the longest first.  Tile `t` of the launch in that order, for 2 to 64
 // sequences: a tile's level is its number in the sequence plus the rows in tiles
 // that the sequence has had before; the tiles of the highest level come first (eight
 // packed prompts of 540 to 2048 rows, sequence after sequence: 139 us, so 120).  With
-// more sequences they come one after the other, each from its end.
-// seq and tile receive its place; false behind the last.
+// more sequences they come one after the other, each from its end: sequence i's from
+// place first(i) G / ROWS + min(i, first(i)) on, which leaves room for its last, partly filled
+// tile, takes none for sequences without rows, and is searched for 64 places at a time.
+// seq and tile receive its place; false where there is none.
 template <int ROWS, bool PAGED>
 AIO_DEV bool find_tile(const AttnArgs& a, int t, int& seq, int& tile) {
   const int lane = threadIdx.x & (AIO_WAVE - 1);
-  for (int base = 0; base < a.n_seqs; base += AIO_WAVE) {
-    const int i = base + lane;
-    int n = 0, first, count = 0;
-    if (i < a.n_seqs) {
-      seq_rows(a.cu_q, a.n_rows, i, first, count);
-      n = (int)(((int64_t)count * a.G + ROWS - 1) / ROWS);
+  auto tiles_of = [&](int rows) { return (int)(((int64_t)rows * a.G + ROWS - 1) / ROWS); };
+  if (a.n_seqs == 1 || a.n_seqs > AIO_WAVE) {
+    auto place = [&](int i) {
+      const int first = min(max(a.cu_q[i], 0), a.n_rows);
+      return (int)((int64_t)first * a.G / ROWS) + min(i, first);
+    };
+    int lo = 0, hi = a.n_seqs;  // the last sequence whose place is at most t is in [lo, hi)
+    while (hi - lo > 1) {
+      const int step = (hi - lo + AIO_WAVE - 1) / AIO_WAVE;
+      const int64_t p = lo + (int64_t)lane * step;
+      const int c = __popcll(__ballot(p < hi && place((int)min(p, (int64_t)hi - 1)) <= t));
+      if (c == 0) return false;
+      lo += (c - 1) * step;
+      hi = min(hi, lo + step);
     }
-    if (a.n_seqs <= AIO_WAVE && a.n_seqs > 1) {
-      int key0, len = 0, full;
-      if (n > 0) seq_keys<PAGED>(a, i, key0, len, full);
-      const int64_t before = (int64_t)max(len - count, 0) * a.G / ROWS;
-      const int lo = (int)min(before, (int64_t)1 << 22), hi = lo + n;
-      // tiles of at least level v (below 2^24 of them: exact)
-      auto from = [&](int v) {
-        return (int)__builtin_amdgcn_readfirstlane(
-            (int)wave_sum((float)max(hi - max(v, lo), 0)));
-      };
-      if (from(0) <= t) return false;
-      int at = 0, past = (int)wave_max((float)(n > 0 ? hi : 0));  // from(at) > t >= from(past)
-      past = __builtin_amdgcn_readfirstlane(past);
-      while (past - at > 1) {
-        const int mid = (at + past) / 2;
-        if (from(mid) > t) at = mid;
-        else past = mid;
-      }
-      const int r = t - from(at + 1);  // the r-th of the sequences with a tile of this level
-      const uint64_t has = __ballot(lo <= at && at < hi);
-      const int before_me = __popcll(has & ((1ull << lane) - 1));
-      const uint64_t me = __ballot((has >> lane & 1) && before_me == r);
-      if (!me) return false;  // (boundaries that overlap)
-      seq = __ffsll((unsigned long long)me) - 1;
-      tile = at - __builtin_amdgcn_readlane(lo, seq);
-      return true;
-    }
-    int incl = n;
-#pragma unroll
-    for (int off = 1; off < AIO_WAVE; off <<= 1) {
-      const int o = __shfl_up(incl, off, AIO_WAVE);
-      if (lane >= off) incl += o;
-    }
-    const uint64_t past = __ballot(incl > t);
-    if (past) {
-      const int at = __ffsll((unsigned long long)past) - 1;
-      // (lane reads, not shuffles: what follows from them is scalar)
-      seq = base + at;
-      tile = __builtin_amdgcn_readlane(incl, at) - 1 - t;
-      return true;
-    }
-    t -= __builtin_amdgcn_readlane(incl, AIO_WAVE - 1);
+    int first, count;
+    seq_rows(a.cu_q, a.n_rows, lo, first, count);
+    const int at = t - place(lo), n = tiles_of(count);
+    if (at < 0 || at >= n) return false;
+    seq = lo;
+    tile = n - 1 - at;
+    return true;
   }
-  return false;
+  int n = 0, first, count = 0, key0, len = 0, full;
+  if (lane < a.n_seqs) {
+    seq_rows(a.cu_q, a.n_rows, lane, first, count);
+    n = tiles_of(count);
+  }
+  if (n > 0) seq_keys<PAGED>(a, lane, key0, len, full);
+  const int64_t before = (int64_t)max(len - count, 0) * a.G / ROWS;
+  const int lo = (int)min(before, (int64_t)1 << 22), hi = lo + n;
+  // tiles of at least level v (below 2^24 of them: exact)
+  auto from = [&](int v) {
+    return (int)__builtin_amdgcn_readfirstlane((int)wave_sum((float)max(hi - max(v, lo), 0)));
+  };
+  if (from(0) <= t) return false;
+  int at = 0, past = (int)wave_max((float)(n > 0 ? hi : 0));  // from(at) > t >= from(past)
+  past = __builtin_amdgcn_readfirstlane(past);
+  while (past - at > 1) {
+    const int mid = (at + past) / 2;
+    if (from(mid) > t) at = mid;
+    else past = mid;
+  }
+  const int r = t - from(at + 1);  // the r-th of the sequences with a tile of this level
+  const uint64_t has = __ballot(lo <= at && at < hi);
+  const int before_me = __popcll(has & ((1ull << lane) - 1));
+  const uint64_t me = __ballot((has >> lane & 1) && before_me == r);
+  if (!me) return false;  // (boundaries that overlap)
+  seq = __ffsll((unsigned long long)me) - 1;
+  tile = at - __builtin_amdgcn_readlane(lo, seq);
+  return true;
 }
 
 AIO_DEV bool not_finite(u32x4 w) {  // of eight bf16
@@ -1040,8 +1042,10 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
     // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594
     // against 564 us; eight of up to 2048, 8 kv heads: 136 against 143)
     p->waves = fp32 || (int64_t)s.n_rows * G / 256 * Hkv < 4 * kCUs ? 4 : 8;
-    p->tiles = ((int64_t)s.n_rows * G) / (32 * p->waves) + s.n_seqs;
-    const int64_t base = std::max<int64_t>(1, p->tiles * Hkv);
+    // (full tiles, and a last one of each sequence that has rows)
+    const int64_t full = (int64_t)s.n_rows * G / (32 * p->waves);
+    p->tiles = full + std::min(s.n_seqs, s.n_rows);
+    const int64_t base = std::max<int64_t>(1, (full + s.n_seqs) * Hkv);
     // Few tiles: their keys are split until the workgroups that a CU holds are there (one
     // with fp32 queries, two with bf16), down to one key tile each (5 rows behind 3000 keys,
     // at most 256 keys per split: 25 us, 64: 17)

@@ -1,0 +1,40 @@
+"""Calls of aio_paged_forward at its limits (needs an MI355X)."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from paper_2604_09752_amd import binding as B
+from tests.gpu_cases import LOGIT_TOL
+
+pytestmark = pytest.mark.gpu
+
+TINY = synth.CONFIGS["tiny"]
+
+
+def model(**kw):
+    cfg = TINY.with_(prompt_len=20, n_steps=8, **kw)
+    return B.DeviceModel(cfg, synth.make_weights(cfg))
+
+
+def idle(n):
+    """One sequence of one token, and n - 1 without any."""
+    one = np.zeros(n, np.int32)
+    one[n // 2] = 1
+    return dict(rows=one, lens=one, table=np.zeros((n, 1), np.int32), tokens=[3], out_rows=[0])
+
+
+@pytest.mark.parametrize("n", [65, 5000, 1 << 20])
+def test_many_idle_sequences(n):
+    """One token of one sequence among up to 2^20 without any: as alone."""
+    dm = model(name="many_kv", d_model=256, ffn_dim=256, n_heads=16, n_kv_heads=16)
+    with torch.cuda.stream(dm.stream):
+        pool, logits, want = dm.new_pool(2), dm.new_logits(1), dm.new_logits(1)
+    dm.paged_forward(pool, **idle(n), logits=logits)
+    dm.paged_forward(pool, [1], [1], [[1]], [3], [0], want)
+    dm.sync()
+    # (alone it takes the kernel of one new token each, fp32 alike: the layers behind the first
+    # differ by roundings)
+    assert (logits - want).abs().max() <= LOGIT_TOL
+    assert torch.equal(pool[0, :, 0], pool[0, :, 1]) and pool[0, :, 0].any()
+    dm.close()
