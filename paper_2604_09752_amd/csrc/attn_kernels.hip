@@ -1033,10 +1033,6 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
     p->chunk = (int)((units + want - 1) / want * 128);
     p->splits = (int)std::max<int64_t>(1, ((int64_t)s.max_len + p->chunk - 1) / p->chunk);
     p->groups = (int64_t)s.n_seqs * Hkv * p->splits;
-    // Keys of a large batch pass the caches by: those of the next layer come before they are
-    // read again (217 MB of at most 403: 59.3 against 55.6 us, 1.07 GB: 188 against 172).  A
-    // small one's may stay in the 256 MB in front of memory.
-    p->stream = (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)64 << 20;
   } else {
     // Tiles of 256 rows stage each key for twice the rows; where that leaves less than
     // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594
@@ -1053,8 +1049,15 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
     p->splits = (int)std::max<int64_t>(1, std::min(units, kRowsGroups / (fp32 ? 2 : 1) / base));
     p->groups = p->tiles * Hkv * p->splits;
   }
-  if (p->groups > (p->waves == 8 ? kMostGroups512 : kMostGroups) || (int64_t)s.n_rows * H > 0x7fffffff) return AIO_ERANGE;
+  if (p->groups > (p->waves == 8 ? kMostGroups512 : kMostGroups) ||
+      (int64_t)s.n_rows * H > 0x7fffffff)
+    return AIO_ERANGE;
   if (p->rows && (int64_t)s.n_rows * G > 0x7fffffff - 256) return AIO_ERANGE;
+  // Keys of a large batch pass the caches by: those of the next layer come before they are
+  // read again (217 MB of at most 403: 59.3 against 55.6 us, 1.07 GB: 188 against 172).  A
+  // small one's may stay in the 256 MB in front of memory.  (Below 2^24 sequences x heads
+  // are left here, so the product stays in 64 bits.)
+  p->stream = !p->rows && (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)64 << 20;
   if (p->splits > 1) p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
   return AIO_OK;
 }

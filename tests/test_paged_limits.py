@@ -35,3 +35,15 @@ def test_a_pass_of_any_number_of_idle_sequences(L):
     c = B.make_config(synth.CONFIGS["7b"])
     assert L.aio_paged_forward_bytes(R(c), 1 << 20, 2048, 1) > 0
     assert L.aio_paged_forward_bytes(R(c), (1 << 20) + 1, 2048, 1) == 0
+
+
+def test_the_largest_sizes_of_a_plan(L):
+    big = 0x7fffffff
+    for n_rows, H, Hkv, hd in ((big, 1 << 30, 1 << 30, 128), (big, 16, 1, 64)):
+        for cu_q in (None, 16):
+            s = B.aio_seqs(big, n_rows, 1 << 30, cu_q, None, None, 0, None)
+            out = (ctypes.c_int32 * 3)()
+            assert L.aio_attention_plan(R(s), H, Hkv, hd, B.AIO_BF16, out) == B.AIO_ERANGE
+    # the largest that one launch covers
+    s = B.aio_seqs((1 << 24) - 1, (1 << 24) - 1, 1 << 30, None, None, None, 0, None)
+    assert L.aio_attention_plan(R(s), 1, 1, 128, B.AIO_F32, out) == B.AIO_OK and out[2] == 1
