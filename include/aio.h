@@ -559,11 +559,11 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
  * page_bytes bytes from page src[i] to page dst[i] of each of n_planes planes,
  * which are plane_bytes apart, pages page_stride_bytes apart (all three whole
  * numbers of 16, page_stride_bytes >= page_bytes).  src and dst are host
- * arrays of n entries, read before the call returns.  AIO_ERANGE: n < 0,
- * n_planes < 1 or a page id outside [0, n_pages).  AIO_EINVAL: a page that is
- * the destination of two copies or both source and destination (the copies
- * run at once, so their order would matter), or a null or misaligned
- * argument. */
+ * arrays of n entries, read before the call returns.  AIO_ERANGE: n
+ * outside [0, 2^31 - 2^16], n_planes outside [1, 2^31 - 2^16] or a page id
+ * outside [0, n_pages).  AIO_EINVAL: a page that is the destination of two
+ * copies or both source and destination (the copies run at once, so their
+ * order would matter), or a null or misaligned argument. */
 int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t n_pages,
                   int64_t page_stride_bytes, int64_t page_bytes, const int32_t* src,
                   const int32_t* dst, int32_t n, void* hip_stream);
@@ -598,8 +598,8 @@ typedef struct aio_paged_pool {
  * memory).
  * AIO_EINVAL: a null or misaligned pointer, a pool whose shape is not the
  * model's, a scratch too small, or two sequences that would write the same page.
- * AIO_ERANGE: counts, lengths (up to max_ctx and the table's width), tokens,
- * pages or out_rows out of range. */
+ * AIO_ERANGE: counts (n_out up to 2^31 - 2^16), lengths (up to max_ctx and the
+ * table's width), tokens, pages or out_rows out of range. */
 int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
                       const int32_t* rows, const int32_t* lens, const int32_t* table,
                       int32_t table_stride, const int32_t* tokens, const int32_t* out_rows,
@@ -621,9 +621,9 @@ size_t aio_paged_forward_bytes(const aio_config* cfg, int32_t n_seqs, int32_t n_
  * top_ids_dev (int32 [rows][top]) and top_logprobs_dev (fp32 [rows][top]) may
  * be NULL where top is 0.  -Inf logits (forbidden tokens) have probability 0;
  * a row of nothing else, or one with a NaN or +Inf, gives NaN.  ws_dev: see
- * aio_logprobs_workspace_bytes.  AIO_ERANGE: rows < 0, n outside [1, 2^30],
- * stride < n or top outside [0, min(n, AIO_MAX_TOP)]; AIO_EINVAL: null or
- * misaligned pointers, a bad type or too small a workspace. */
+ * aio_logprobs_workspace_bytes.  AIO_ERANGE: rows outside [0, 2^31 - 2^16], n
+ * outside [1, 2^30], stride < n or top outside [0, min(n, AIO_MAX_TOP)];
+ * AIO_EINVAL: null or misaligned pointers, a bad type or too small a workspace. */
 #define AIO_MAX_TOP 32
 int aio_logprobs(const void* logits_dev, int32_t dtype, int32_t rows, int32_t n, int64_t stride,
                  const int32_t* targets_dev, int32_t top, float* logprob_dev, float* entropy_dev,

@@ -240,7 +240,8 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
 int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t n_pages,
                   int64_t page_stride_bytes, int64_t page_bytes, const int32_t* src,
                   const int32_t* dst, int32_t n, void* hip_stream) {
-  if (n < 0 || n_planes < 1 || n_pages < 1) return AIO_ERANGE;
+  if (n < 0 || n > kMostSteps || n_planes < 1 || n_planes > kMostSteps || n_pages < 1)
+    return AIO_ERANGE;
   if (plane_bytes < 0 || page_bytes < 0 || page_stride_bytes < page_bytes || plane_bytes % 16 ||
       page_bytes % 16 || page_stride_bytes % 16)
     return AIO_EINVAL;
@@ -277,7 +278,8 @@ int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t
 }
 
 size_t aio_logprobs_workspace_bytes(int32_t rows, int32_t n, int32_t top) {
-  if (rows < 1 || n < 1 || n > (1 << 30) || top < 0 || top > AIO_MAX_TOP) return 0;
+  if (rows < 1 || rows > kMostSteps || n < 1 || n > (1 << 30) || top < 0 || top > AIO_MAX_TOP)
+    return 0;
   return aio_logprob_plan(rows, n, top).ws;
 }
 
@@ -285,7 +287,7 @@ int aio_logprobs(const void* logits_dev, int32_t dtype, int32_t rows, int32_t n,
                  const int32_t* targets_dev, int32_t top, float* logprob_dev, float* entropy_dev,
                  int32_t* top_ids_dev, float* top_logprobs_dev, void* ws_dev, size_t ws_bytes,
                  void* hip_stream) {
-  if (rows < 0 || n < 1 || n > (1 << 30) || stride < n || top < 0 ||
+  if (rows < 0 || rows > kMostSteps || n < 1 || n > (1 << 30) || stride < n || top < 0 ||
       top > std::min(n, (int32_t)AIO_MAX_TOP))
     return AIO_ERANGE;
   if (dtype != AIO_F32 && dtype != AIO_BF16) return AIO_EINVAL;

@@ -19,6 +19,9 @@ constexpr int kMaxGroup = 16;
 constexpr int kCUs = 256;
 // A grid's axis holds fewer than 2^32 threads: workgroups of 256 or 512 of them.
 constexpr int64_t kMostGroups = 0xffffffffll / 256, kMostGroups512 = 0xffffffffll / 512;
+// Counts that go out in several launches, each of at most 65535: up to here 32 bits hold the
+// step past the last.
+constexpr int32_t kMostSteps = 0x7fff0000;
 
 // AIO_OK, or what the entry points return for this pool.
 int aio_check_paged(const aio_paged_kv& kv);

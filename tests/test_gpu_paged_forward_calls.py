@@ -1,4 +1,6 @@
 """Calls of aio_paged_forward at its limits (needs an MI355X)."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -37,4 +39,24 @@ def test_many_idle_sequences(n):
     # differ by roundings)
     assert (logits - want).abs().max() <= LOGIT_TOL
     assert torch.equal(pool[0, :, 0], pool[0, :, 1]) and pool[0, :, 0].any()
+    dm.close()
+
+
+def test_more_output_rows_than_32_bits_step_over():
+    dm = model(name="outs")
+    with torch.cuda.stream(dm.stream):
+        pool, logits = dm.new_pool(2), dm.new_logits(1)
+    kv = B.aio_paged_kv(pool.data_ptr(), pool[0, 1].data_ptr(), pool.stride(2), pool.stride(3), 2,
+                        16, dm.c.n_kv_heads, dm.c.head_dim)
+    p = B.aio_paged_pool(kv, pool.stride(0), dm.c.n_layers)
+    n = B.lib().aio_paged_forward_bytes(ctypes.byref(dm.c), 1, 1, 1)
+    scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+    one, zero = np.ones(1, np.int32), np.zeros(1, np.int32)
+    for n_out in (0x7fff0001, 0x7fffffff):  # (refused before out_rows is read)
+        assert B.lib().aio_paged_forward(
+            dm.handle, ctypes.byref(p), 1, one.ctypes.data, one.ctypes.data, zero.ctypes.data, 1,
+            one.ctypes.data, zero.ctypes.data, n_out, logits.data_ptr(), scratch.data_ptr(),
+            n) == B.AIO_ERANGE
+    dm.sync()
+    assert not pool.any()
     dm.close()

@@ -37,6 +37,19 @@ def test_a_pass_of_any_number_of_idle_sequences(L):
     assert L.aio_paged_forward_bytes(R(c), (1 << 20) + 1, 2048, 1) == 0
 
 
+def test_counts_whose_last_step_passes_32_bits(L):
+    """Rows, planes and copies go out in launches of at most 65535: past 2^31 - 2^16 the
+    counter would wrap and never reach the end."""
+    most, p = 0x7fff0000, 16
+    for rows in (most + 1, 0x7fffffff):
+        assert L.aio_logprobs_workspace_bytes(rows, 8, 2) == 0
+        assert L.aio_logprobs(p, B.AIO_F32, rows, 8, 8, None, 0, None, p, None, None, None, 0,
+                              None) == B.AIO_ERANGE
+    one, two = (ctypes.c_int32 * 1)(0), (ctypes.c_int32 * 1)(1)
+    assert L.aio_page_copy(p, most + 1, 1024, 2, 512, 512, one, two, 1, None) == B.AIO_ERANGE
+    assert L.aio_page_copy(p, 1, 1024, 2, 512, 512, one, two, most + 1, None) == B.AIO_ERANGE
+
+
 def test_the_largest_sizes_of_a_plan(L):
     big = 0x7fffffff
     for n_rows, H, Hkv, hd in ((big, 1 << 30, 1 << 30, 128), (big, 16, 1, 64)):
