@@ -549,8 +549,9 @@ int aio_packed_attention(const aio_packed_kv* kv, const aio_seqs* s, const aio_a
  * fp32 is rounded to the nearest bf16, ties to even, as everywhere in a cache.
  * A row that falls before key 0, past max_len or the table's width, or into a hole
  * is not written.  Two sequences of one call must not write the same slot
- * (aio_pages_extend sees to that), nor may pages or heads of the pool overlap
- * (AIO_EINVAL where the strides show it).  Errors as aio_paged_attention. */
+ * (aio_pages_extend sees to that), nor may pages or heads of the pool, or its K
+ * and V, overlap (AIO_EINVAL where two strides show it).  Errors as
+ * aio_paged_attention. */
 int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_rows_dev,
                     const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                     int64_t head_stride, void* hip_stream);
@@ -563,7 +564,8 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
  * outside [0, 2^31 - 2^16], n_planes outside [1, 2^31 - 2^16] or a page id
  * outside [0, n_pages).  AIO_EINVAL: a page that is the destination of two
  * copies or both source and destination (the copies run at once, so their
- * order would matter), or a null or misaligned argument. */
+ * order would matter), planes or pages that overlap, or a null or misaligned
+ * argument. */
 int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t n_pages,
                   int64_t page_stride_bytes, int64_t page_bytes, const int32_t* src,
                   const int32_t* dst, int32_t n, void* hip_stream);
@@ -597,7 +599,8 @@ typedef struct aio_paged_pool {
  * read before the call returns.  Not for graph capture (it copies from host
  * memory).
  * AIO_EINVAL: a null or misaligned pointer, a pool whose shape is not the
- * model's, a scratch too small, or two sequences that would write the same page.
+ * model's or whose layers, K and V, pages or heads overlap (where two strides
+ * show it), a scratch too small, or two sequences that would write the same page.
  * AIO_ERANGE: counts (n_out up to 2^31 - 2^16), lengths (up to max_ctx and the
  * table's width), tokens, pages or out_rows out of range. */
 int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,

@@ -846,7 +846,8 @@ int check_paged_forward(const aio_model* m, const aio_paged_pool& p, int32_t n_s
   const int rc = aio_check_paged(kv);
   if (rc) return rc;
   if (kv.n_kv_heads != c.n_kv_heads || kv.head_dim != c.head_dim || p.n_layers != c.n_layers ||
-      p.layer_stride < 0 || p.layer_stride % 8 || aio_pages_overlap(kv))
+      p.layer_stride < 0 || p.layer_stride % 8 ||
+      aio_pool_overlaps(kv, p.layer_stride, p.n_layers))
     return AIO_EINVAL;
   if (n_seqs < 1 || n_seqs > (1 << 20) || n_out < 0 || n_out > kMostSteps) return AIO_ERANGE;
   int64_t total = 0;

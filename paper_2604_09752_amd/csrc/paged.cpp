@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <functional>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "aio_internal.h"
@@ -96,9 +97,43 @@ int aio_check_paged(const aio_paged_kv& kv) {
   return AIO_OK;
 }
 
+bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t size) {
+  typedef __int128 wide;  // (strides are any 63-bit numbers)
+  if ((n1 > 1 && s1 < size) || (n2 > 1 && s2 < size)) return true;
+  if (n1 == 1 || n2 == 1) return false;
+  // one dimension within a step of the other
+  if ((wide)(n1 - 1) * s1 + size <= s2 || (wide)(n2 - 1) * s2 + size <= s1) return false;
+  if (n1 > n2) {
+    std::swap(n1, n2);
+    std::swap(s1, s2);
+  }
+  // i steps of one against the nearest two counts j of the other
+  for (int64_t i = 1; i < n1; ++i) {
+    const wide at = (wide)i * s1;
+    if (at - (wide)(n2 - 1) * s2 >= size) return false;
+    const wide j = at / s2;
+    if ((j < n2 && at - j * s2 < size) || (j + 1 < n2 && (j + 1) * s2 - at < size)) return true;
+  }
+  return false;
+}
+
 bool aio_pages_overlap(const aio_paged_kv& kv) {
+  return aio_grid_overlaps(kv.n_pages, kv.page_stride, kv.n_kv_heads, kv.head_stride,
+                           (int64_t)kv.page_size * kv.head_dim);
+}
+
+bool aio_pool_overlaps(const aio_paged_kv& kv, int64_t layer_stride, int32_t n_layers) {
   const int64_t one = (int64_t)kv.page_size * kv.head_dim;
-  return (kv.n_pages > 1 && kv.page_stride < one) || (kv.n_kv_heads > 1 && kv.head_stride < one);
+  const intptr_t k = (intptr_t)kv.k_dev, v = (intptr_t)kv.v_dev;
+  const int64_t apart = (int64_t)(k < v ? v - k : k - v) / 2;  // K and V: a dimension of two
+  const struct {
+    int64_t n, stride;
+  } dim[] = {{n_layers, layer_stride}, {2, apart}, {kv.n_pages, kv.page_stride},
+             {kv.n_kv_heads, kv.head_stride}};
+  for (int a = 0; a < 4; ++a)
+    for (int b = a + 1; b < 4; ++b)
+      if (aio_grid_overlaps(dim[a].n, dim[a].stride, dim[b].n, dim[b].stride, one)) return true;
+  return false;
 }
 
 // ------------------------------------------------------------- page tables
@@ -221,6 +256,9 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
     return AIO_EINVAL;
   if (s->n_rows == 0 || s->n_seqs == 0) return AIO_OK;
   if (!good(k_rows_dev, 16) || !good(v_rows_dev, 16)) return AIO_EINVAL;
+  // (the same rows to one place for K and V are written twice, but alike)
+  if ((kv->k_dev != kv->v_dev || k_rows_dev != v_rows_dev) && aio_pool_overlaps(*kv, 0, 1))
+    return AIO_EINVAL;
   AppendArgs t{};
   t.kv = paged_keys(*kv, *s);
   t.k = (uint16_t*)kv->k_dev;
@@ -248,6 +286,8 @@ int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t
   if (n == 0) return AIO_OK;
   if (!good(pool_dev, 16) || !src || !dst) return AIO_EINVAL;
   if (page_bytes > ((int64_t)1 << 37)) return AIO_ERANGE;  // (below kMostGroups chunks of 16 KB)
+  if (aio_grid_overlaps(n_planes, plane_bytes, n_pages, page_stride_bytes, page_bytes))
+    return AIO_EINVAL;
   for (int32_t i = 0; i < n; ++i)
     if (src[i] < 0 || src[i] >= n_pages || dst[i] < 0 || dst[i] >= n_pages) return AIO_ERANGE;
   const int rc = guarded([&] {

@@ -25,8 +25,13 @@ constexpr int32_t kMostSteps = 0x7fff0000;
 
 // AIO_OK, or what the entry points return for this pool.
 int aio_check_paged(const aio_paged_kv& kv);
-// Pages or heads that would take each other's rows: not to be written.
+// Blocks of `size` in a grid of n1 x n2, s1 and s2 apart (none negative): whether two of them
+// share an element.
+bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t size);
+// Pages or heads that would take each other's rows, or K those of V, in n_layers layers
+// (one: layer_stride 0): not to be written.
 bool aio_pages_overlap(const aio_paged_kv& kv);
+bool aio_pool_overlaps(const aio_paged_kv& kv, int64_t layer_stride, int32_t n_layers);
 
 // A pure host description of one attention's launch.
 struct AttnPlan {

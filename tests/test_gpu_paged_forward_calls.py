@@ -60,3 +60,35 @@ def test_more_output_rows_than_32_bits_step_over():
     dm.sync()
     assert not pool.any()
     dm.close()
+
+
+@pytest.mark.parametrize("change", [
+    dict(layer_stride=0), dict(layer_stride=1), dict(v=0), dict(v=1), dict(v=2),
+    dict(page_stride=1), dict(head_stride=1)])
+def test_pools_whose_parts_overlap(change):
+    """Strides and the distance of V are given in parts: 1 is a layer's K, a page or a
+    head too short."""
+    dm = model(name="overlap")
+    with torch.cuda.stream(dm.stream):
+        pool, logits = dm.new_pool(4), dm.new_logits(1)
+    c, one = dm.c, 16 * dm.c.head_dim
+    v = {0: pool[0, 0], 1: pool[0, 0, 1], 2: pool[1, 0]}
+    kv = B.aio_paged_kv(pool.data_ptr(), v[change["v"]].data_ptr() if "v" in change else
+                        pool[0, 1].data_ptr(), pool.stride(2), pool.stride(3), 4, 16,
+                        c.n_kv_heads, c.head_dim)
+    if "page_stride" in change:
+        kv.page_stride = one  # its second head is the next page's first
+    if "head_stride" in change:
+        kv.head_stride = pool.stride(2)  # the next page's first head
+    p = B.aio_paged_pool(kv, change["layer_stride"] * pool.stride(1)  # (1: on the V before)
+                         if "layer_stride" in change else pool.stride(0), c.n_layers)
+    n = B.lib().aio_paged_forward_bytes(ctypes.byref(c), 1, 1, 1)
+    scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+    one_, zero = np.ones(1, np.int32), np.zeros(1, np.int32)
+    assert B.lib().aio_paged_forward(
+        dm.handle, ctypes.byref(p), 1, one_.ctypes.data, one_.ctypes.data, zero.ctypes.data, 1,
+        one_.ctypes.data, zero.ctypes.data, 1, logits.data_ptr(), scratch.data_ptr(),
+        n) == B.AIO_EINVAL
+    dm.sync()
+    assert not pool.any()
+    dm.close()
