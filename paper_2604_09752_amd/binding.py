@@ -857,8 +857,11 @@ class DeviceModel:
         receives those of the packed rows out_rows.  On the model's stream."""
         c = self.c
         _need(pool.dim() == 6 and pool.dtype == torch.bfloat16 and pool.is_contiguous() and
-              pool.device == self.device and pool.shape[:2] == (c.n_layers, 2),
+              pool.shape[:2] == (c.n_layers, 2),
               "pool: a contiguous bf16 [layers, 2, n_pages, kv_heads, page_size, head_dim]")
+        device = self.kv.device  # (which "cuda" alone does not name)
+        _need(pool.device == device and logits.device == device,
+              "pool and logits: on the model's device")
         a = [np.ascontiguousarray(x, dtype=np.int32) for x in (rows, lens, table, tokens, out_rows)]
         n = a[0].size
         _need(a[1].size == n and a[2].ndim == 2 and a[2].shape[0] == n and
@@ -870,11 +873,11 @@ class DeviceModel:
         p = aio_paged_pool(kv, pool.stride(0), pool.shape[0])
         need = int(lib().aio_paged_forward_bytes(ctypes.byref(c), n, int(a[3].size),
                                                  a[2].shape[1]))
-        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+        with torch.cuda.device(device), torch.cuda.stream(self.stream):
             if getattr(self, "_paged_scratch", None) is None or \
                     self._paged_scratch.numel() < need:
                 self._paged_scratch = torch.empty(max(need, 256), dtype=torch.uint8,
-                                                  device=self.device)
+                                                  device=device)
             s = self._paged_scratch
             _check(lib().aio_paged_forward(self.handle, ctypes.byref(p), n, a[0].ctypes.data,
                                            a[1].ctypes.data, a[2].ctypes.data, a[2].shape[1],
