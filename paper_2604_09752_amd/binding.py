@@ -393,6 +393,21 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _int32(*values) -> None:
+    """ctypes cuts an integer to the argument's 32 bits without a word."""
+    for v in values:
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError("%d does not fit 32 bits" % v)
+
+
+def _host_int32(x, what: str) -> np.ndarray:
+    """A host array of integers as contiguous int32, none of them cut."""
+    a = np.asarray(x)
+    if a.size and (a.dtype.kind not in "iu" or a.min() < -(1 << 31) or a.max() >= 1 << 31):
+        raise ValueError(what + ": integers of 32 bits are needed")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
 # (A decode step's calls are as short as their launches: the checks below look
 # at each tensor once, and a stream is asked for as a number.)
 _raw_stream = torch._C._cuda_getCurrentRawStream
@@ -524,6 +539,7 @@ def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: in
                              n_kv_heads: int, head_dim: int, prompts: bool = False) -> int:
     """Workspace of an attention over n_seqs sequences with n_rows rows (prompts:
     several rows per sequence, i.e. a call with cu_q)."""
+    _int32(n_seqs, n_rows, max_len, n_heads, n_kv_heads, head_dim)
     s = aio_seqs(n_seqs, n_rows, max_len, 16 if prompts else None, None, None, 0, None)
     return int(lib().aio_attn_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
 
@@ -611,7 +627,8 @@ def aio_page_copy(pool: torch.Tensor, src, dst) -> None:
     for n, st in zip(shape[:1:-1], stride[:1:-1]):
         _need(n == 1 or st == inner, "pool: pages have to be contiguous")
         inner *= n
-    a, b = np.ascontiguousarray(src, dtype=np.int32), np.ascontiguousarray(dst, dtype=np.int32)
+    a, b = _host_int32(src, "src"), _host_int32(dst, "dst")
+    _int32(shape[0], shape[1], a.size)
     _need(a.ndim == 1 and a.shape == b.shape, "src and dst differ in length")
     size = pool.element_size()
     rc = _launch(at, lib().aio_page_copy, pool.data_ptr(), shape[0], stride[0] * size, shape[1],
@@ -622,6 +639,7 @@ def aio_page_copy(pool: torch.Tensor, src, dst) -> None:
 
 
 def aio_logprobs_workspace_bytes(rows: int, n: int, top: int) -> int:
+    _int32(rows, n, top)
     return int(lib().aio_logprobs_workspace_bytes(rows, n, top))
 
 
@@ -635,6 +653,7 @@ def aio_logprobs(logits: torch.Tensor, targets: torch.Tensor | None,
     dtype = logits.dtype
     _need(logits.dim() == 2 and dtype in _DTYPES, "logits: fp32 or bf16 [rows, n]")
     rows, n = logits.shape
+    _int32(rows, n)
     _need(n <= 1 or rows == 0 or logits.stride(1) == 1, "logits: rows have to be contiguous")
     if targets is not None:
         _i32(targets, 1, "targets")
@@ -667,6 +686,7 @@ class Pages:
     ``extend`` and ``compact`` return the copies (src, dst) to enqueue."""
 
     def __init__(self, n_pages: int, page_size: int, max_seqs: int):
+        _int32(n_pages, page_size, max_seqs)
         h = ctypes.c_void_p()
         _check(lib().aio_pages_create(n_pages, page_size, max_seqs, ctypes.byref(h)),
                "aio_pages_create")
@@ -678,20 +698,24 @@ class Pages:
         return s.value
 
     def close(self, seq: int) -> None:
+        _int32(seq)
         _check(lib().aio_pages_close(self.handle, seq), "aio_pages_close")
 
     def fork(self, seq: int) -> int:
+        _int32(seq)
         s = ctypes.c_int32(-1)
         _check(lib().aio_pages_fork(self.handle, seq, ctypes.byref(s)), "aio_pages_fork")
         return s.value
 
     def extend(self, seq: int, n: int):
+        _int32(seq, n)
         a, b, c = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int32(0)
         _check(lib().aio_pages_extend(self.handle, seq, n, ctypes.byref(a), ctypes.byref(b),
                                       ctypes.byref(c)), "aio_pages_extend")
         return ([a.value], [b.value]) if c.value else ([], [])
 
     def truncate(self, seq: int, length: int) -> None:
+        _int32(seq, length)
         _check(lib().aio_pages_truncate(self.handle, seq, length), "aio_pages_truncate")
 
     def compact(self):
@@ -702,12 +726,14 @@ class Pages:
         return a[: n.value].copy(), b[: n.value].copy()
 
     def length(self, seq: int) -> int:
+        _int32(seq)
         n = ctypes.c_int32(0)
         _check(lib().aio_pages_row(self.handle, seq, None, 0, ctypes.byref(n)), "aio_pages_row")
         return n.value
 
     def rows(self, seqs, width: int):
         """(lens [n], table [n, width]) of the sequences, host int32."""
+        _int32(width, *seqs)
         lens, table = np.zeros(len(seqs), np.int32), np.full((len(seqs), width), -1, np.int32)
         n = ctypes.c_int32(0)
         for i, s in enumerate(seqs):
@@ -862,7 +888,9 @@ class DeviceModel:
         device = self.kv.device  # (which "cuda" alone does not name)
         _need(pool.device == device and logits.device == device,
               "pool and logits: on the model's device")
-        a = [np.ascontiguousarray(x, dtype=np.int32) for x in (rows, lens, table, tokens, out_rows)]
+        a = [_host_int32(x, what) for x, what in (
+            (rows, "rows"), (lens, "lens"), (table, "table"), (tokens, "tokens"),
+            (out_rows, "out_rows"))]
         n = a[0].size
         _need(a[1].size == n and a[2].ndim == 2 and a[2].shape[0] == n and
               a[3].size == a[0].sum(dtype=np.int64), "rows, lens, table and tokens do not match")

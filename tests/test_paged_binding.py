@@ -53,3 +53,49 @@ def test_a_model_on_the_current_device(no_device):
     """A model made on "cuda" has its tensors on "cuda:0"."""
     with pytest.raises(B.AioError):
         forward(standing_in(device=torch.device("cuda")), pool(), torch.zeros((1, TINY.vocab)))
+
+
+BIG = (1 << 32) + 1  # cut to 32 bits, 1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=np.array([BIG])), dict(lens=np.array([BIG])), dict(table=np.array([[BIG]])),
+    dict(tokens=np.array([BIG])), dict(out_rows=np.array([BIG - 1])), dict(tokens=[1.5]),
+    dict(tokens=torch.tensor([BIG])), dict(lens=np.array([BIG], np.uint64))])
+def test_a_pass_over_integers_that_do_not_fit(no_device, kw):
+    with pytest.raises(ValueError, match="32 bits"):
+        forward(standing_in(), pool(), torch.zeros((1, TINY.vocab)), **kw)
+
+
+def test_a_pass_over_integers_that_fit(no_device):
+    """Any integer type, and no rows asked for."""
+    for kind in (np.int64, np.uint8, np.int16):
+        with pytest.raises(B.AioError):
+            forward(standing_in(), pool(), torch.zeros((1, TINY.vocab)), rows=np.ones(1, kind),
+                    lens=np.ones(1, kind), tokens=np.ones(1, kind), out_rows=[])
+
+
+def test_copies_whose_pages_do_not_fit(monkeypatch):
+    monkeypatch.setattr(B, "_device_of", lambda *t: 0)
+    p = torch.zeros((2, 4, 16), dtype=torch.bfloat16)
+    for src, dst in ((np.array([BIG]), [0]), ([1], np.array([BIG - 1])), ([0.5], [1])):
+        with pytest.raises(ValueError, match="32 bits"):
+            B.aio_page_copy(p, src, dst)
+
+
+def test_sizes_that_do_not_fit():
+    with pytest.raises(ValueError, match="32 bits"):
+        B.aio_logprobs_workspace_bytes(BIG, 32000, 5)
+    with pytest.raises(ValueError, match="32 bits"):
+        B.aio_attn_workspace_bytes(1, BIG, 4096, 32, 32, 128, prompts=True)
+    with pytest.raises(ValueError, match="32 bits"):
+        B.Pages(BIG, 16, 1)
+    p = B.Pages(4, 16, 2)
+    s = p.open()
+    for call in (lambda: p.extend(s, BIG), lambda: p.extend(BIG - 1, 1), lambda: p.truncate(s, BIG - 1),
+                 lambda: p.close((1 << 32) + s), lambda: p.fork((1 << 32) + s),
+                 lambda: p.length((1 << 32) + s), lambda: p.rows([(1 << 32) + s], 4),
+                 lambda: p.rows([s], BIG + 3)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert p.length(s) == 0 and p.free == 4
