@@ -528,7 +528,7 @@ size_t aio_attn_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv
  * an earlier turn).  The rows' own keys have to be in the pages
  * (aio_page_append).  An idle place in a padded batch has lens 0.
  * AIO_EINVAL: a null or misaligned pointer or stride, a bad shape or type, a
- * scale that is not positive and finite, or a workspace smaller than
+ * scale that is not positive and below 2.3e38, or a workspace smaller than
  * aio_attn_workspace_bytes says.  AIO_ERANGE: negative counts, cu_q_dev NULL with n_rows !=
  * n_seqs, or more work than one launch covers.  AIO_EUNSUPPORTED: a page
  * size, head dimension or number of heads per kv head not listed above. */

@@ -52,7 +52,9 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   const int64_t unit = a.dtype == AIO_F32 ? 4 : 8;  // elements in 16 bytes
   if (a.q_stride < 0 || a.q_stride % unit || a.out_stride < 0 || a.out_stride % unit)
     return AIO_EINVAL;
-  if (!(a.scale > 0.f) || !isfinite(a.scale)) return AIO_EINVAL;
+  // (times log2 e: an infinite factor would make every score of 0 a NaN)
+  const float scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
+  if (!(a.scale > 0.f) || !isfinite(scale_log2)) return AIO_EINVAL;
   if (s.n_rows > 1 && a.out_stride < (int64_t)a.n_heads * hd) return AIO_EINVAL;  // (rows overlap)
   if (s.n_rows == 0 || s.n_seqs == 0) return AIO_OK;
   if (!good(a.q_dev, 16) || !good(a.out_dev, 16) || !aligned(a.lse_dev, 4)) return AIO_EINVAL;
@@ -74,7 +76,7 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   t.lse = a.lse_dev;
   t.ldq = a.q_stride;
   t.ldo = a.out_stride;
-  t.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
+  t.scale_log2 = scale_log2;
   t.S = p.splits;
   t.chunk = p.chunk;
   t.tiles = (int)p.tiles;

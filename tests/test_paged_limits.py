@@ -60,3 +60,12 @@ def test_the_largest_sizes_of_a_plan(L):
     # the largest that one launch covers
     s = B.aio_seqs((1 << 24) - 1, (1 << 24) - 1, 1 << 30, None, None, None, 0, None)
     assert L.aio_attention_plan(R(s), 1, 1, 128, B.AIO_F32, out) == B.AIO_OK and out[2] == 1
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_scales_that_overflow_in_units_of_log2(L, scale):
+    """Finite, but not times log2 e: a score of 0 would come out NaN."""
+    kv = B.aio_paged_kv(1 << 20, 1 << 30, 8 * 16 * 64, 16 * 64, 10, 16, 8, 64)
+    s = B.aio_seqs(4, 4, 100, None, 16, 16, 8, None)
+    a = B.aio_attn(16, 16, None, 16 * 64, 16 * 64, B.AIO_F32, 16, scale)
+    assert L.aio_paged_attention(R(kv), R(s), R(a), 16, 1 << 30, None) == B.AIO_EINVAL
