@@ -597,7 +597,7 @@ typedef struct aio_paged_pool {
  * rounding.  scratch_dev: aio_paged_forward_bytes bytes, 256-byte aligned, its
  * contents of no matter.  Enqueued on the model's stream; the host arrays are
  * read before the call returns.  Not for graph capture (it copies from host
- * memory).
+ * memory): AIO_EINVAL where the stream is captured.
  * AIO_EINVAL: a null or misaligned pointer, a pool whose shape is not the
  * model's or whose layers, K and V, pages or heads overlap (where two strides
  * show it), a scratch too small, or two sequences that would write the same page.

@@ -905,6 +905,11 @@ int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
     const aio_config& c = m->cfg;
     PagedScratch s = paged_scratch(c, (char*)scratch_dev, n_seqs, R, table_stride);
     if (s.bytes > scratch_bytes) return AIO_EINVAL;
+    // (a graph would keep the address of the host arrays, and read it at each replay)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t e = hipStreamIsCapturing(m->stream, &capture);
+    if (e != hipSuccess) return hip_fail(e);
+    if (capture != hipStreamCaptureStatusNone) return AIO_EINVAL;
     PagedPass pass{};
     pass.pool = *pool;
     pass.rope = s.rope;
@@ -938,8 +943,7 @@ int aio_paged_forward(aio_model* m, const aio_paged_pool* pool, int32_t n_seqs,
     pass.seqs.table_dev = cu_q + n_seqs + 1;
     pass.seqs.table_stride = table_stride;
     int32_t* out_dev = (int32_t*)pass.seqs.table_dev + (size_t)n_seqs * table_stride;
-    hipError_t e = hipMemcpyAsync(s.ints, host.data(), host.size() * 4, hipMemcpyHostToDevice,
-                                  m->stream);
+    e = hipMemcpyAsync(s.ints, host.data(), host.size() * 4, hipMemcpyHostToDevice, m->stream);
     if (e == hipSuccess) e = aio_launch_paged_pass(*m, s.pf, R, pass);
     // (their places in turn: where rows are asked for more than once, n_out is larger than R)
     for (int32_t at = 0; at < n_out && e == hipSuccess; at += R) {

@@ -92,3 +92,32 @@ def test_pools_whose_parts_overlap(change):
     dm.sync()
     assert not pool.any()
     dm.close()
+
+
+def test_a_captured_pass():
+    """Refused: the graph would read the call's host arrays when it is replayed.  The capture
+    goes on without it."""
+    dm = model(name="captured")
+    with torch.cuda.stream(dm.stream):
+        pool, logits, seen = dm.new_pool(2), dm.new_logits(1), torch.zeros(4, device="cuda")
+    call = (pool, [1], [1], [[0]], [3], [0], logits)
+    dm.paged_forward(*call)  # (its scratch is there)
+    dm.sync()
+    want = logits.clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=dm.stream):
+        with pytest.raises(B.AioError) as e:
+            dm.paged_forward(*call)
+        seen += 1
+    assert e.value.code == B.AIO_EINVAL
+    for i in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert (seen == i + 1).all() and torch.equal(logits, want)
+    logits.zero_()
+    torch.cuda.synchronize()
+    dm.paged_forward(*call)
+    dm.sync()
+    assert torch.equal(logits, want)
+    dm.close()
