@@ -121,3 +121,45 @@ def test_a_captured_pass():
     dm.sync()
     assert torch.equal(logits, want)
     dm.close()
+
+
+def test_the_call_returns_before_its_work():
+    """Enqueued behind 15 ms of products, which are not done when it returns."""
+    dm = model(name="behind")
+    with torch.cuda.stream(dm.stream):
+        pool, logits = dm.new_pool(8), dm.new_logits(40)
+        a = torch.zeros((8192, 8192), dtype=torch.bfloat16, device="cuda")
+        a @ a
+    call = (pool, [20, 20], [20, 20], [[0, 1], [2, 3]], [5] * 40, list(range(40)), logits)
+    dm.paged_forward(*call)
+    dm.sync()
+    want = logits.clone()
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    with torch.cuda.stream(dm.stream):
+        for _ in range(20):
+            a @ a
+        done.record()
+    dm.paged_forward(*call)
+    assert not done.query()
+    dm.sync()
+    assert torch.equal(logits, want)
+    dm.close()
+
+
+@pytest.mark.parametrize("vocab,rows", [(997, 2), (1001, 3), (515, 10)])
+def test_rows_of_an_odd_vocabulary(vocab, rows):
+    """Groups of the LM head whose logits start at any multiple of 4 bytes: every row as in
+    one group, nothing behind the last."""
+    outs = []
+    for most in (rows, 1):
+        dm = model(name="odd", vocab=vocab, max_verify=most)
+        with torch.cuda.stream(dm.stream):
+            pool, logits = dm.new_pool(2), torch.full((24, vocab), 7.0, device="cuda")
+        dm.paged_forward(pool, [21], [21], [[0, 1]], [i % 500 for i in range(21)],
+                         list(range(21)) + [4, 4], logits[:23])
+        dm.sync()
+        assert (logits[23] == 7).all() and torch.equal(logits[21], logits[4])
+        outs.append(logits[:23].clone())
+        dm.close()
+    assert torch.isfinite(outs[0]).all() and (outs[0] - outs[1]).abs().max() <= LOGIT_TOL
