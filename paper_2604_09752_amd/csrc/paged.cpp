@@ -79,7 +79,6 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   t.scale_log2 = scale_log2;
   t.S = p.splits;
   t.chunk = p.chunk;
-  t.tiles = (int)p.tiles;
   if (p.ws) {
     t.part_o = (float*)ws;
     t.part_ml = t.part_o + (size_t)p.splits * s.n_rows * t.H * hd;

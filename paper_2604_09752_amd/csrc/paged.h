@@ -81,7 +81,6 @@ struct AttnArgs {
   int64_t ldq, ldo;
   float scale_log2;  // scores in units of log2
   int S, chunk;
-  int tiles;         // k_attn_rows: row tiles of the launch
   float* part_o;     // [S][n_rows][H][hd]
   float* part_ml;    // [S][n_rows][H][2]: maximum (log2 units), sum
 };
