@@ -530,7 +530,9 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   const int32_t* table = PAGED ? a.kv.table + (int64_t)seq * a.kv.tstride : nullptr;
   const int pmask = (1 << a.kv.shift) - 1;
 
-  // Plain tiles t0 .. tp - 1: every row sees every key of them.
+  // Plain tiles t0 .. tp - 1: every row sees every key of them.  (One hole among them sends them
+  // all through the loop below: 2048 rows of the 1B behind 2000 keys, bf16, 90 us without a hole,
+  // 263 with one.)
   int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
   if constexpr (PAGED) {
     // (not with holes among them)
@@ -1023,9 +1025,14 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
   p->splits = 1;
   if (!p->rows) {
     // Splits of at least 128 keys (a block of 32 per wave), up to the workgroups that the
-    // GPU holds at once, or twice as many for many sequences, whose lengths differ (two of
-    // 32768 keys: 169 against 173 us; 24 of 37 to 4096: 55.6 against 51.4).  None up to
-    // 512 keys: a launch that joins them costs more than four blocks per wave.
+    // GPU holds at once, or twice as many for many sequences, whose lengths differ.  Up to 7
+    // sequences the smaller limit never lost (7 of 37 to 4096 keys, 8 kv heads: 23.6
+    // against 28.7 us; 2 of 32768, 32 kv heads: 169 against 173).  Beyond, it depends on how
+    // evenly the smaller one fills the CUs and how far the lengths lie apart, which
+    // the host does not know: 8 of 37 to 4096 keys 25.0 with the smaller one, 30.0 with the larger;
+    // 16: 38.5, 48.5; 24: 55.1, 50.6; 14 of 1000 to 20000: 124, 109; 24: 232, 192; 24 of 30000 to
+    // 32768: 493, 511; 10 of 8192, 32 kv heads: 234, 217.  None up to 512 keys: a launch that joins
+    // them costs more than four blocks per wave.
     const int64_t units = std::max<int64_t>(1, ((int64_t)s.max_len + 127) / 128);
     const int64_t base = std::max<int64_t>(1, (int64_t)s.n_seqs * Hkv);
     const int64_t most = s.n_seqs < 8 ? kStepGroups / 2 : kStepGroups;
