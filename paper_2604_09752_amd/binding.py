@@ -403,7 +403,8 @@ def _int32(*values) -> None:
 def _host_int32(x, what: str) -> np.ndarray:
     """A host array of integers as contiguous int32, none of them cut."""
     a = np.asarray(x)
-    if a.size and (a.dtype.kind not in "iu" or a.min() < -(1 << 31) or a.max() >= 1 << 31):
+    if a.dtype != np.int32 and a.size and (  # (the search takes as long as a short call)
+            a.dtype.kind not in "iu" or a.min() < -(1 << 31) or a.max() >= 1 << 31):
         raise ValueError(what + ": integers of 32 bits are needed")
     return np.ascontiguousarray(a, dtype=np.int32)
 
