@@ -531,7 +531,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   const int pmask = (1 << a.kv.shift) - 1;
 
   // Plain tiles t0 .. tp - 1: every row sees every key of them.  (One hole among them sends them
-  // all through the loop below: 2048 rows of the 1B behind 2000 keys, bf16, 90 us without a hole,
+  // all through the loop below: 2048 rows of the 1B behind 1637 keys, bf16, 90 us without a hole,
   // 263 with one.)
   int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
   if constexpr (PAGED) {
