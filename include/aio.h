@@ -556,6 +556,109 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
                     const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                     int64_t head_stride, void* hip_stream);
 
+/* Keys and values of one layer in pages of 8-bit codes: slot s of kv head h of
+ * page p is the head_dim int8 codes at byte p page_stride + h head_stride +
+ * s head_dim and one unsigned byte b at p exp_page_stride + h exp_head_stride +
+ * s of k_exp_dev or v_exp_dev; its elements are code 2^(b - 127), half the bytes
+ * of a bf16 page.  b lies from 8 to 248; b = 255 with codes of 0 stands for a
+ * row that held something not finite, and reads as NaN. */
+typedef struct aio_q8_kv {
+  void* k_dev;
+  void* v_dev;
+  void* k_exp_dev;         /* 8-byte aligned                                 */
+  void* v_exp_dev;         /* 8-byte aligned                                 */
+  int64_t page_stride;     /* bytes, a multiple of 16                        */
+  int64_t head_stride;     /* bytes, a multiple of 16                        */
+  int64_t exp_page_stride; /* bytes, a multiple of 8                         */
+  int64_t exp_head_stride; /* bytes, a multiple of 8                         */
+  int32_t n_pages;
+  int32_t page_size;       /* positions per page: a power of two, 8 .. 256   */
+  int32_t n_kv_heads;
+  int32_t head_dim;        /* 64 or 128                                      */
+} aio_q8_kv;
+
+/* aio_page_append into pages of 8-bit codes.  For a head's row of K or V with
+ * the largest magnitude A, b is the least from 8 to 248 for which A / 2^(b - 127),
+ * rounded to the nearest integer, ties to even, is at most 127 (248 where none is),
+ * and the codes are the elements over 2^(b - 127), rounded alike and held to 127: an
+ * element is off by at most A / 127, or by 2^-120 where that is more.  A row with an infinity
+ * or NaN gets b = 255 and codes of 0.  Which rows are written, and the errors, as
+ * aio_page_append; pages, heads, K and V, codes and bytes must not overlap. */
+int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev,
+                  const void* v_rows_dev, int32_t dtype, int64_t row_stride,
+                  int64_t head_stride, void* hip_stream);
+
+/* aio_paged_attention over pages of 8-bit codes (an element is exactly a bf16,
+ * so nothing is rounded on the way to the products), with the workspace of
+ * aio_attn_workspace_bytes.  Errors as aio_paged_attention. */
+int aio_q8_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_attn* a, void* ws_dev,
+                     size_t ws_bytes, void* hip_stream);
+
+/* Groups of sequences that begin with the same keys (requests behind one
+ * template): group g is the sequences cu_seqs[g] .. cu_seqs[g + 1] - 1, whose
+ * first prefix_lens[g] keys are alike.  Sequences of no group share nothing. */
+typedef struct aio_prefixes {
+  int32_t n_groups;                /* at most 2^30                           */
+  int32_t max_prefix;              /* more keys than that are not shared     */
+  const int32_t* cu_seqs_dev;      /* [n_groups + 1], ascending              */
+  const int32_t* prefix_lens_dev;  /* [n_groups]                             */
+} aio_prefixes;
+
+/* aio_paged_attention that reads a group's first keys once for all of its
+ * rows instead of once for each sequence: the same results up to rounding.
+ * They are read through the table of the group's first sequence, up to its
+ * own length, in whole multiples of 64; the others' tables have to list pages of the
+ * same contents (a fork's are the same pages).  A sequence that is not
+ * to share (an idle place with lens 0, new rows that begin within the prefix)
+ * computes all of its keys by itself.  Its workspace is
+ * aio_prefix_workspace_bytes's.  Errors as aio_paged_attention; AIO_EINVAL: a null
+ * or misaligned array of the groups; AIO_ERANGE: negative counts, or more groups than 2^30. */
+int aio_prefix_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_prefixes* x,
+                         const aio_attn* a, void* ws_dev, size_t ws_bytes, void* hip_stream);
+
+/* The same over pages of 8-bit codes. */
+int aio_q8_prefix_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_prefixes* x,
+                            const aio_attn* a, void* ws_dev, size_t ws_bytes, void* hip_stream);
+
+/* Bytes of workspace that an attention with these groups takes, as
+ * aio_attn_workspace_bytes; of the groups only the two numbers are read. */
+size_t aio_prefix_workspace_bytes(const aio_seqs* s, const aio_prefixes* x, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t head_dim);
+
+/* Query and key rows to be normalised and rotated: [n_rows][heads][head_dim],
+ * all fp32 or all bf16, rows the strides apart (whole numbers of 16 bytes; rows
+ * of outputs must not overlap). */
+typedef struct aio_qk_rows {
+  const void* q_dev;
+  const void* k_dev;
+  void* q_out_dev;
+  void* k_out_dev;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t q_out_stride;
+  int64_t k_out_stride;
+  int32_t dtype;       /* AIO_F32 or AIO_BF16 */
+  int32_t n_rows;
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128           */
+} aio_qk_rows;
+
+/* RMS norm of each head of the query and key rows, then the rotation by the
+ * row's position, in one pass: y = w x / sqrt(mean x^2 + eps), and for i below
+ * head_dim / 2 with t = position base^(-2i / head_dim) the pair (y_i,
+ * y_(i + head_dim / 2)) turned by t.  positions_dev: int32 [n_rows], any value;
+ * q_weight_dev and k_weight_dev: bf16 [head_dim], or NULL for 1.  Angles are
+ * computed in 64 bits, the rest in 32, rounded once to the outputs' type.  An output
+ * may take its input's place (the same pointer and stride); otherwise outputs
+ * overlap nothing.  AIO_EINVAL: a null or misaligned pointer or stride, a bad
+ * type, outputs that overlap, eps not positive and finite, base not above 1 and
+ * finite; AIO_ERANGE: n_rows outside [0, 2^24) or heads outside [1, 2^16];
+ * AIO_EUNSUPPORTED: another head dimension. */
+int aio_qk_norm_rope(const aio_qk_rows* r, const int32_t* positions_dev,
+                     const void* q_weight_dev, const void* k_weight_dev, float eps, float base,
+                     void* hip_stream);
+
 /* Copies pages in every plane of a pool (a plane: K or V of one layer):
  * page_bytes bytes from page src[i] to page dst[i] of each of n_planes planes,
  * which are plane_bytes apart, pages page_stride_bytes apart (all three whole

@@ -77,6 +77,26 @@ class aio_seqs(ctypes.Structure):
                 ("table_stride", ctypes.c_int32), ("cu_k_dev", ctypes.c_void_p)]
 
 
+class aio_q8_kv(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_dev", "v_dev", "k_exp_dev", "v_exp_dev")] + \
+               [(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "exp_page_stride",
+                                              "exp_head_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim")]
+
+
+class aio_prefixes(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("max_prefix", ctypes.c_int32),
+                ("cu_seqs_dev", ctypes.c_void_p), ("prefix_lens_dev", ctypes.c_void_p)]
+
+
+class aio_qk_rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_dev", "k_dev", "q_out_dev", "k_out_dev")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "q_out_stride",
+                                              "k_out_stride")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "n_rows", "n_heads", "n_kv_heads",
+                                              "head_dim")]
+
+
 class aio_attn(ctypes.Structure):
     _fields_ = [("q_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
                 ("lse_dev", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
@@ -146,6 +166,13 @@ def lib():
         L.aio_paged_attention.argtypes = [vp, vp, vp, vp, sz, vp]
         L.aio_packed_attention.argtypes = [vp, vp, vp, vp, sz, vp]
         L.aio_page_append.argtypes = [vp, vp, vp, vp, i32, i64, i64, vp]
+        L.aio_q8_append.argtypes = [vp, vp, vp, vp, i32, i64, i64, vp]
+        L.aio_q8_attention.argtypes = [vp, vp, vp, vp, sz, vp]
+        L.aio_prefix_attention.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.aio_q8_prefix_attention.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.aio_prefix_workspace_bytes.argtypes = [vp, vp, i32, i32, i32]
+        L.aio_prefix_workspace_bytes.restype = sz
+        L.aio_qk_norm_rope.argtypes = [vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp]
         L.aio_page_copy.argtypes = [vp, i32, i64, i32, i64, i64, vp, vp, i32, vp]
         L.aio_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.aio_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
@@ -430,8 +457,9 @@ def _packer(cls):
     return pack
 
 
-_pack_paged, _pack_packed, _pack_seqs, _pack_attn = map(
-    _packer, (aio_paged_kv, aio_packed_kv, aio_seqs, aio_attn))
+(_pack_paged, _pack_packed, _pack_seqs, _pack_attn, _pack_q8, _pack_prefixes, _pack_qk) = map(
+    _packer, (aio_paged_kv, aio_packed_kv, aio_seqs, aio_attn, aio_q8_kv, aio_prefixes,
+              aio_qk_rows))
 
 
 def _device_of(first: torch.Tensor, *others) -> int:
@@ -479,6 +507,39 @@ def _paged(k: torch.Tensor, v: torch.Tensor):
     # (the stride of a single head or page says nothing)
     return _pack_paged(k.data_ptr(), v.data_ptr(), page_stride if pages > 1 else 0,
                        head_stride if heads > 1 else 0, pages, size, heads, hd), heads, size, hd
+
+
+def _paged8(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
+    """(aio_q8_kv's bytes, kv heads, page size, head_dim)"""
+    shape, stride = k.shape, k.stride()
+    if (len(shape) != 4 or v.shape != shape or k.dtype is not torch.int8 or
+            v.dtype is not torch.int8):
+        raise ValueError("pages: two int8 [n_pages, kv_heads, page_size, head_dim]")
+    pages, heads, size, hd = shape
+    page_stride, head_stride, slot, one = stride
+    if v.stride() != stride or one != 1 or slot != hd:
+        raise ValueError("pages: K and V of the same strides, slots and dimensions contiguous")
+    exp_stride = k_exp.stride()
+    if (k_exp.shape != shape[:3] or v_exp.shape != shape[:3] or k_exp.dtype is not torch.uint8 or
+            v_exp.dtype is not torch.uint8 or v_exp.stride() != exp_stride or exp_stride[2] != 1):
+        raise ValueError("k_exp, v_exp: two uint8 [n_pages, kv_heads, page_size] of the same "
+                         "strides, slots contiguous")
+    return _pack_q8(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+                    page_stride if pages > 1 else 0, head_stride if heads > 1 else 0,
+                    exp_stride[0] if pages > 1 else 0, exp_stride[1] if heads > 1 else 0,
+                    pages, size, heads, hd), heads, size, hd
+
+
+def _prefixes(cu_seqs, prefix_lens, max_prefix, most: int) -> bytes:
+    if (cu_seqs.dtype is not torch.int32 or prefix_lens.dtype is not torch.int32 or
+            cu_seqs.dim() != 1 or prefix_lens.dim() != 1 or
+            cu_seqs.shape[0] != prefix_lens.shape[0] + 1):
+        raise ValueError("cu_seqs and prefix_lens: int32 [groups + 1] and [groups]")
+    n = prefix_lens.shape[0]
+    _need((n == 0 or cu_seqs.stride(0) == 1) and (n <= 1 or prefix_lens.stride(0) == 1),
+          "cu_seqs and prefix_lens have to be contiguous")
+    return _pack_prefixes(n, most if max_prefix is None else max_prefix, cu_seqs.data_ptr(),
+                          prefix_lens.data_ptr() if n else 0)
 
 
 def _paged_seqs(lens, table, cu_q, n_rows: int, max_len, page_size: int) -> bytes:
@@ -574,6 +635,87 @@ def aio_paged_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens:
     _attend(lib().aio_paged_attention, at, kv, s, a, heads, kv_heads, hd, q.device, ws)
 
 
+def _check_heads(q, hd: int) -> None:
+    if q.shape[2] != hd:
+        raise ValueError("q and k differ in head_dim")
+
+
+def aio_q8_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor,
+                     v_exp: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
+                     out: torch.Tensor, cu_q: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, scale: float | None = None,
+                     max_len: int | None = None, ws: torch.Tensor | None = None) -> None:
+    """aio_paged_attention over 8-bit pages: codes k, v (int8 [n_pages, kv_heads,
+    page_size, head_dim]) and a byte for each row (uint8 [n_pages, kv_heads,
+    page_size]), as aio_q8_append writes them."""
+    at = _device_of(q, k, v, k_exp, v_exp, lens, table, out, cu_q, lse, ws)
+    kv, kv_heads, page_size, hd = _paged8(k, v, k_exp, v_exp)
+    a = _attn(q, out, lse, scale)
+    _check_heads(q, hd)
+    s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, page_size)
+    _attend(lib().aio_q8_attention, at, kv, s, a, q.shape[1], kv_heads, hd, q.device, ws)
+
+
+def aio_prefix_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_groups: int,
+                               max_prefix: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                               prompts: bool = False) -> int:
+    """Workspace of an attention with n_groups groups of up to max_prefix shared
+    keys, otherwise as aio_attn_workspace_bytes."""
+    _int32(n_seqs, n_rows, max_len, n_groups, max_prefix, n_heads, n_kv_heads, head_dim)
+    s = aio_seqs(n_seqs, n_rows, max_len, 16 if prompts else None, None, None, 0, None)
+    x = aio_prefixes(n_groups, max_prefix, None, None)
+    return int(lib().aio_prefix_workspace_bytes(ctypes.byref(s), ctypes.byref(x), n_heads,
+                                                n_kv_heads, head_dim))
+
+
+def _attend_groups(call, at, kv, s, x, a, n_heads, n_kv_heads, head_dim, device, ws):
+    n = lib().aio_prefix_workspace_bytes(s, x, n_heads, n_kv_heads, head_dim)
+    w = None
+    if n:
+        ws, w = _workspace(n, ws, device)
+    rc = _launch(at, call, kv, s, x, a, w, n)
+    if rc:
+        raise AioError(rc, call.__name__)
+
+
+def aio_prefix_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
+                         table: torch.Tensor, cu_seqs: torch.Tensor, prefix_lens: torch.Tensor,
+                         out: torch.Tensor, cu_q: torch.Tensor | None = None,
+                         lse: torch.Tensor | None = None, scale: float | None = None,
+                         max_len: int | None = None, max_prefix: int | None = None,
+                         ws: torch.Tensor | None = None) -> None:
+    """aio_paged_attention of sequences in groups: those from cu_seqs[g] up to
+    cu_seqs[g + 1] begin with the same prefix_lens[g] keys, which are read once for all
+    of them.  max_prefix: no prefix is longer (default: max_len)."""
+    at = _device_of(q, k, v, lens, table, cu_seqs, prefix_lens, out, cu_q, lse, ws)
+    kv, kv_heads, page_size, hd = _paged(k, v)
+    a = _attn(q, out, lse, scale)
+    _check_heads(q, hd)
+    s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, page_size)
+    x = _prefixes(cu_seqs, prefix_lens, max_prefix, 1 << 30)
+    _attend_groups(lib().aio_prefix_attention, at, kv, s, x, a, q.shape[1], kv_heads, hd,
+                   q.device, ws)
+
+
+def aio_q8_prefix_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                            k_exp: torch.Tensor, v_exp: torch.Tensor, lens: torch.Tensor,
+                            table: torch.Tensor, cu_seqs: torch.Tensor,
+                            prefix_lens: torch.Tensor, out: torch.Tensor,
+                            cu_q: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                            scale: float | None = None, max_len: int | None = None,
+                            max_prefix: int | None = None,
+                            ws: torch.Tensor | None = None) -> None:
+    """aio_prefix_attention over the 8-bit pages of aio_q8_attention."""
+    at = _device_of(q, k, v, k_exp, v_exp, lens, table, cu_seqs, prefix_lens, out, cu_q, lse, ws)
+    kv, kv_heads, page_size, hd = _paged8(k, v, k_exp, v_exp)
+    a = _attn(q, out, lse, scale)
+    _check_heads(q, hd)
+    s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, page_size)
+    x = _prefixes(cu_seqs, prefix_lens, max_prefix, 1 << 30)
+    _attend_groups(lib().aio_q8_prefix_attention, at, kv, s, x, a, q.shape[1], kv_heads, hd,
+                   q.device, ws)
+
+
 def aio_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
                          cu_k: torch.Tensor, out: torch.Tensor, lse: torch.Tensor | None = None,
                          scale: float | None = None, max_len: int | None = None,
@@ -605,6 +747,23 @@ def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor,
     bf16) into their pages; lens counts them already."""
     at = _device_of(k, v, k_rows, v_rows, lens, table, cu_q)
     kv, kv_heads, page_size, hd = _paged(k, v)
+    _append(lib().aio_page_append, at, kv, kv_heads, page_size, hd, k_rows, v_rows, lens, table,
+            cu_q, max_len)
+
+
+def aio_q8_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                  k_exp: torch.Tensor, v_exp: torch.Tensor, lens: torch.Tensor,
+                  table: torch.Tensor, cu_q: torch.Tensor | None = None,
+                  max_len: int | None = None) -> None:
+    """aio_page_append into the 8-bit pages of aio_q8_attention: each head's row
+    becomes int8 codes and the byte of their power of two."""
+    at = _device_of(k, v, k_exp, v_exp, k_rows, v_rows, lens, table, cu_q)
+    kv, kv_heads, page_size, hd = _paged8(k, v, k_exp, v_exp)
+    _append(lib().aio_q8_append, at, kv, kv_heads, page_size, hd, k_rows, v_rows, lens, table,
+            cu_q, max_len)
+
+
+def _append(call, at, kv, kv_heads, page_size, hd, k_rows, v_rows, lens, table, cu_q, max_len):
     shape, stride, dtype = k_rows.shape, k_rows.stride(), k_rows.dtype
     if (len(shape) != 3 or v_rows.shape != shape or v_rows.dtype is not dtype or
             dtype not in _DTYPES or shape[1] != kv_heads or shape[2] != hd):
@@ -612,11 +771,40 @@ def aio_page_append(k_rows: torch.Tensor, v_rows: torch.Tensor, k: torch.Tensor,
     if v_rows.stride() != stride or stride[2] != 1:
         _need(k_rows.numel() == 0, "rows: the same strides, dimensions contiguous")
     s = _paged_seqs(lens, table, cu_q, shape[0], max_len, page_size)
-    rc = _launch(at, lib().aio_page_append, kv, s, k_rows.data_ptr(),
-                 v_rows.data_ptr(), _DTYPES[dtype], stride[0] if shape[0] > 1 else 0,
-                 stride[1] if shape[1] > 1 else 0)
+    rc = _launch(at, call, kv, s, k_rows.data_ptr(), v_rows.data_ptr(), _DTYPES[dtype],
+                 stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0)
     if rc:
-        raise AioError(rc, "aio_page_append")
+        raise AioError(rc, call.__name__)
+
+
+def aio_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+                     q_out: torch.Tensor, k_out: torch.Tensor,
+                     q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                     eps: float = 1e-5, base: float = 10000.0) -> None:
+    """RMS norm of each head of q [rows, heads, head_dim] and k [rows, kv_heads,
+    head_dim] (both fp32 or bf16), times the weights (bf16 [head_dim], None: 1), and the
+    rotation of its halves by the row's position (int32).  An output may be its input."""
+    at = _device_of(q, k, positions, q_out, k_out, q_weight, k_weight)
+    shape, k_shape, dtype = q.shape, k.shape, q.dtype
+    if (len(shape) != 3 or len(k_shape) != 3 or k_shape[0] != shape[0] or
+            k_shape[2] != shape[2] or dtype not in _DTYPES or k.dtype is not dtype or
+            q_out.shape != shape or k_out.shape != k_shape or q_out.dtype is not dtype or
+            k_out.dtype is not dtype):
+        raise ValueError("q, k and their outputs: all fp32 or all bf16 [rows, heads, head_dim]")
+    rows, heads, hd = shape
+    _i32(positions, 1, "positions")
+    _need(positions.shape[0] == rows, "one position per row")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype is not torch.bfloat16 or w.shape != (hd,) or
+                              not w.is_contiguous()):
+            raise ValueError("q_weight, k_weight: contiguous bf16 [head_dim]")
+    r = _pack_qk(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
+                 _rows3(q, shape, "q"), _rows3(k, k_shape, "k"), _rows3(q_out, shape, "q_out"),
+                 _rows3(k_out, k_shape, "k_out"), _DTYPES[dtype], rows, heads, k_shape[1], hd)
+    rc = _launch(at, lib().aio_qk_norm_rope, r, positions.data_ptr(), _ptr(q_weight),
+                 _ptr(k_weight), eps, base)
+    if rc:
+        raise AioError(rc, "aio_qk_norm_rope")
 
 
 def aio_page_copy(pool: torch.Tensor, src, dst) -> None:

@@ -17,8 +17,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libaio.so")
 SOURCES = ["api.cpp", "decode_kernels.hip", "verify_kernels.hip", "step_kernel.hip",
-           "prefill_kernels.hip", "paged.cpp", "attn_kernels.hip", "page_kernels.hip",
-           "logprob_kernels.hip"]
+           "prefill_kernels.hip", "paged.cpp", "attn_kernels.hip", "attn8_kernels.hip",
+           "attn_groups_kernels.hip", "attn8_groups_kernels.hip", "page_kernels.hip",
+           "qk_kernels.hip", "logprob_kernels.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -89,6 +89,35 @@ AIO_DEV void load_query(const AttnArgs& a, int row, int head, int hd, int d0, bo
   }
 }
 
+// Eight elements of a cache row: bf16 as they lie in memory, or eight codes and their row's
+// byte b, which stand for code 2^(b - 127): at most seven bits and a sign, so exactly a bf16.
+// (b = 255 gives a factor of infinity, and with codes of 0 NaN.)
+struct Codes8 {
+  uint2 code;
+  uint32_t exp;
+};
+template <bool Q8>
+using Row8 = std::conditional_t<Q8, Codes8, u32x4>;
+
+AIO_DEV u32x4 widen(u32x4 w) { return w; }
+AIO_DEV u32x4 widen(const Codes8& r) {
+  const float scale = __uint_as_float(r.exp << 23);
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i < 2 ? r.code.x : r.code.y;
+    const float x = i8_at(w, 2 * (i & 1)) * scale, y = i8_at(w, 2 * (i & 1) + 1) * scale;
+    o[i] = __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u);
+  }
+  return o;
+}
+
+// Where the keys of an attention lie.
+enum Keys { kPaged, kPacked, kPaged8 };
+
+template <bool Q8, bool SHARED>
+using ArgsOf = std::conditional_t<Q8 || SHARED, AttnMoreArgs, AttnArgs>;
+
 AIO_DEV void store_out(const AttnArgs& a, bool f32, int64_t at, float v) {
   if (f32) ((float*)a.out)[at] = v;
   else ((uint16_t*)a.out)[at] = f32_to_bf16(v);
@@ -116,7 +145,167 @@ AIO_DEV void carry(T& hi, T& lo) {
 // 1457 us.  (bf16 outputs round to 2^-9, which no such chain comes near.)
 constexpr int kStepCarry = 32, kRowsCarry = 32;
 
+// --------------------------------------------------------- shared prefixes
+
+// The sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 of group g share their first keys.  The rows
+// of a group lie behind one another, so for those keys a group is one sequence whose
+// rows all see all of them: its rows and heads are packed into tiles that read each key
+// once, and every sequence's own workgroups begin behind them.  Both write partial
+// results, the shared part into the first px.S places of a row and its own into the others,
+// and k_attn_join joins them.  A sequence whose rows do not all see the whole prefix (an idle
+// place, say) takes no part: its own workgroups read all of its keys and mark the first
+// places as empty.
+//
+// Shared keys are counted in whole tiles, so that a sequence's own keys start at one.
+constexpr int kSharedUnit = 64;
+
+AIO_DEV int bounded(int v, int most) { return min(max(v, 0), most); }
+
+// First row of group g, or the end of the last one.
+AIO_DEV int group_row(const AttnMoreArgs& a, int g) {
+  const int s = bounded(a.px.cu_seqs[g], a.n_seqs);
+  return a.cu_q ? bounded(a.cu_q[s], a.n_rows) : min(s, a.n_rows);
+}
+
+// How many keys the group whose first sequence is s0 shares: no more than that one has.
+AIO_DEV int shared_keys(const AttnMoreArgs& a, int g, int s0) {
+  const int p = min(bounded(a.px.lens[g], a.px.max), paged_len(a.kv, s0, a.max_len));
+  return p & ~(kSharedUnit - 1);
+}
+
+// The last i of [0, n) for which at(i) <= v, of an ascending at (-1: none), searched for
+// 64 places at a time.
+template <class F>
+AIO_DEV int last_at_most(int n, int v, F at) {
+  const int lane = threadIdx.x & (AIO_WAVE - 1);
+  int lo = 0, hi = n;
+  bool any = false;
+  while (hi - lo > (any ? 1 : 0)) {
+    const int step = (hi - lo + AIO_WAVE - 1) / AIO_WAVE;
+    const int64_t p = lo + (int64_t)lane * step;
+    const int c = __popcll(__ballot(p < hi && at((int)min(p, (int64_t)hi - 1)) <= v));
+    if (c == 0) return -1;
+    any = true;
+    lo += (c - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return any ? lo : -1;
+}
+
+// How many keys sequence i shares with its group (0: it is in none).
+AIO_DEV int shared_keys_of(const AttnMoreArgs& a, int i) {
+  const int g = last_at_most(a.px.n, i, [&](int j) { return a.px.cu_seqs[j]; });
+  if (g < 0 || i >= a.px.cu_seqs[g + 1]) return 0;
+  return shared_keys(a, g, bounded(a.px.cu_seqs[g], a.n_seqs - 1));
+}
+
+// Tile t of the groups' tiles of ROWS packed rows, which come one group after the
+// other: group g's from place first(g) G / ROWS + min(g, first(g)) on, which leaves room for
+// its last, partly filled tile.  False where there is none.
+struct GroupTile {
+  int group, seq, end;  // its sequences: seq .. end - 1
+  int first, count;     // its rows
+  int tile;
+};
+template <int ROWS>
+AIO_DEV bool find_group_tile(const AttnMoreArgs& a, int t, GroupTile& r) {
+  auto place = [&](int i) {
+    const int first = group_row(a, i);
+    return (int)((int64_t)first * a.G / ROWS) + min(i, first);
+  };
+  r.group = last_at_most(a.px.n, t, place);
+  if (r.group < 0) return false;
+  r.first = group_row(a, r.group);
+  r.count = group_row(a, r.group + 1) - r.first;
+  r.tile = t - place(r.group);
+  r.seq = bounded(a.px.cu_seqs[r.group], a.n_seqs - 1);
+  r.end = bounded(a.px.cu_seqs[r.group + 1], a.n_seqs);
+  return r.count > 0 && r.tile >= 0 && (int64_t)r.tile * ROWS < (int64_t)r.count * a.G;
+}
+
 // ------------------------------------------------ one new token per sequence
+
+// What a workgroup of k_attn_step computes: keys c0 .. c1 - 1 of kv head kvh in the pages of
+// sequence seq, for ncol columns, the packed rows p0 .. (packed row r G + g is head g of the kv
+// head's, of row first + r), into place `slot` of the partial results.
+struct StepUnit {
+  int seq, kvh, slot, c0, c1, first, p0, ncol;
+  int need;  // rows of fewer keys take no part
+};
+
+// False where there is nothing to compute (and what others read is written).
+AIO_DEV bool step_unit(const AttnArgs& a, StepUnit& u) {
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int sh = udiv(b, a.by_s), split = b - sh * a.S;
+  u.seq = udiv(sh, a.by_hkv);
+  u.kvh = sh - u.seq * a.kv.Hkv;
+  const int len = paged_len(a.kv, u.seq, a.max_len);
+  u.slot = split;
+  u.c0 = split * a.chunk;
+  u.c1 = min(len, u.c0 + a.chunk);
+  u.first = u.seq;
+  u.p0 = 0;
+  u.ncol = a.G;
+  u.need = 0;
+  if (split > 0 && u.c0 >= len) {  // a split without keys
+    if (tid < a.G)
+      a.part_ml[(((int64_t)split * a.n_rows + u.seq) * a.H + u.kvh * a.G + tid) * 2] = -INFINITY;
+    return false;
+  }
+  return true;
+}
+
+// The same with groups: shared keys first, then every sequence's own.
+AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
+  const int b = blockIdx.x, tid = threadIdx.x;
+  // (per split of n keys: whole blocks for each of the four waves)
+  auto chunk_of = [](int n, int splits) { return ((n + splits - 1) / splits + 127) & ~127; };
+  if (b < a.px.groups) {
+    const int split = udiv(b, a.px.by_s), lin = b - split * a.px.by_s.d;
+    const int t = udiv(lin, a.by_hkv);
+    u.kvh = lin - t * a.kv.Hkv;
+    GroupTile r;
+    if (!find_group_tile<kMaxGroup>(a, t, r)) return false;
+    const int n = shared_keys(a, r.group, r.seq);
+    if (n == 0) return false;
+    const int chunk = chunk_of(n, a.px.S);
+    u.seq = r.seq;
+    u.slot = split;
+    u.c0 = split * chunk;
+    u.c1 = min(n, u.c0 + chunk);
+    u.first = r.first;
+    u.p0 = r.tile * kMaxGroup;
+    u.ncol = min(kMaxGroup, r.count * a.G - u.p0);
+    u.need = n;
+    if (u.c0 < n) return true;
+    if (tid < u.ncol) {
+      const int r0 = udiv(u.p0 + tid, a.by_g), row = u.first + r0;
+      if (paged_len(a.kv, row, a.max_len) >= n)
+        a.part_ml[(((int64_t)split * a.n_rows + row) * a.H + u.kvh * a.G + u.p0 + tid - r0 * a.G) * 2] =
+            -INFINITY;
+    }
+    return false;
+  }
+  const int o = b - a.px.groups, sh = udiv(o, a.by_s), split = o - sh * a.px.own;
+  u.seq = udiv(sh, a.by_hkv);
+  u.kvh = sh - u.seq * a.kv.Hkv;
+  const int len = paged_len(a.kv, u.seq, a.max_len), n = shared_keys_of(a, u.seq);
+  const int start = len >= n ? n : 0, chunk = chunk_of(len - start, a.px.own);
+  u.slot = a.px.S + split;
+  u.c0 = start + split * chunk;
+  u.c1 = min(len, u.c0 + chunk);
+  u.first = u.seq;
+  u.p0 = 0;
+  u.ncol = a.G;
+  u.need = 0;
+  const int64_t at = ((int64_t)u.seq * a.H + u.kvh * a.G + tid) * 2, plane = (int64_t)a.n_rows * a.H * 2;
+  if (tid < a.G) {
+    if (start == 0 && split == 0)
+      for (int i = 0; i < a.px.S; ++i) a.part_ml[i * plane + at] = -INFINITY;
+    if (split > 0 && u.c0 >= len) a.part_ml[u.slot * plane + at] = -INFINITY;
+  }
+  return split == 0 || u.c0 < len;
+}
 
 // Workgroup (sequence, kv head, split): the G query heads of the kv head are
 // columns of one 16-wide tile; each wave takes every fourth block of 32 keys of
@@ -138,8 +327,8 @@ struct StepLds {
   static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
 };
 
-template <int HD, int NT, bool STREAM>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(AttnArgs a) {
+template <int HD, int NT, bool STREAM, bool Q8 = false, bool SHARED = false>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(ArgsOf<Q8, SHARED> a) {
   using L = StepLds<HD>;
   extern __shared__ __align__(16) char smem[];
   __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
@@ -151,24 +340,45 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
   const int col = lane & 15, grp = lane >> 4;
-  const int b = blockIdx.x, sh = udiv(b, a.by_s), split = b - sh * a.S;
-  const int seq = udiv(sh, a.by_hkv), kvh = sh - seq * a.kv.Hkv;
-  const int len = paged_len(a.kv, seq, a.max_len);
-  const int c0 = split * a.chunk, c1 = min(len, c0 + a.chunk);
-  const int h0 = kvh * a.G;
-  if (split > 0 && c0 >= len) {  // a split without keys
-    if (tid < a.G) a.part_ml[(((int64_t)split * a.n_rows + seq) * a.H + h0 + tid) * 2] = -INFINITY;
-    return;
+  StepUnit u;
+  if constexpr (SHARED) {
+    if (!shared_step_unit(a, u)) return;
+  } else {
+    if (!step_unit(a, u)) return;
   }
+  const int seq = u.seq, kvh = u.kvh, c0 = u.c0, c1 = u.c1, h0 = kvh * a.G;
+  // row and head of a column
+  auto place = [&](int c, int& row, int& head) {
+    row = seq;
+    head = h0 + c;
+    if constexpr (SHARED) {
+      const int r = udiv(u.p0 + c, a.by_g);
+      row = u.first + r;
+      head = h0 + u.p0 + c - r * a.G;
+    }
+  };
   bf16x8 q[NC][NT];
+  int row, head;
+  place(min(col, u.ncol - 1), row, head);
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    load_query<NT>(a, seq, h0 + col, HD, c * 32 + 8 * grp, col < a.G, q[c]);
+    load_query<NT>(a, row, head, HD, c * 32 + 8 * grp, col < u.ncol, q[c]);
+  // (in the shared part: the rows that see all of it)
+  __shared__ bool use[kMaxGroup];
+  if constexpr (SHARED) {
+    if (tid < kMaxGroup) use[tid] = paged_len(a.kv, row, a.max_len) >= u.need;
+  }
 
   const int32_t* table = a.kv.table + (int64_t)seq * a.kv.tstride;
   const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
-  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride;
-  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride;
+  using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
+  const Elem* kb = (const Elem*)a.kv.k + kvh * a.kv.head_stride;
+  const Elem* vb = (const Elem*)a.kv.v + kvh * a.kv.head_stride;
+  const uint8_t *ke = nullptr, *ve = nullptr;
+  if constexpr (Q8) {
+    ke = a.exp.k + kvh * a.exp.head_stride;
+    ve = a.exp.v + kvh * a.exp.head_stride;
+  }
   // Lane l holds the page of key l mod 32 of a block (-1: not visible).
   auto load_page = [&](int t) {
     const int key = c0 + t * 32 + (lane & 31);
@@ -180,15 +390,22 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   // would take half a 128-byte line of 16 rows); the 8 keys of an aligned group share
   // a page, so pages are wave uniform.  Keys that are not visible read page 0.
   const int lr = lane / TPR, ld = lane % TPR * 8;
-  u32x4 kr[NV], vr[NV];
-  auto load_block = [&](u32x4 (&r)[NV], const uint16_t* from, int t, int page) {
+  Row8<Q8> kr[NV], vr[NV];
+  auto load_block = [&](Row8<Q8> (&r)[NV], const Elem* from, const uint8_t* exps, int t, int page) {
     const int j0 = c0 + t * 32;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
-                         ((j0 + i * RPL) & pm) * HD;
-      const u32x4* p = (const u32x4*)(from + at + (uint32_t)(lr * HD + ld));
-      r[i] = STREAM ? __builtin_nontemporal_load(p) : *p;
+      const int pg = max(__builtin_amdgcn_readlane(page, i * RPL), 0);
+      const int slot = (j0 + i * RPL) & pm;
+      const Elem* p = from + (pg * a.kv.stride + slot * HD) + (uint32_t)(lr * HD + ld);
+      if constexpr (Q8) {
+        const u32x2* c = (const u32x2*)p;
+        const u32x2 w = STREAM ? __builtin_nontemporal_load(c) : *c;
+        r[i].code = make_uint2(w.x, w.y);
+        r[i].exp = exps[pg * a.exp.stride + slot + (uint32_t)lr];
+      } else {
+        r[i] = STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
+      }
     }
   };
   f32x4 o[ND];
@@ -209,8 +426,8 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 
   int page = load_page(wid), next = load_page(wid + kWaves);
   if (wid < nt) {
-    load_block(kr, kb, wid, page);
-    load_block(vr, vb, wid, page);
+    load_block(kr, kb, ke, wid, page);
+    load_block(vr, vb, ve, wid, page);
   }
   for (int t = wid; t < nt;) {
     const int te = NT == 3 ? min(nt, t + kStepCarry * kWaves) : nt;
@@ -220,8 +437,8 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       const bool more = t + kWaves < nt;
       const int tn = more ? t + kWaves : t, pn = more ? next : page;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = kr[i];
-      load_block(kr, kb, tn, pn);
+      for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = widen(kr[i]);
+      load_block(kr, kb, ke, tn, pn);
       wave_lds_sync();  // the keys are in LDS
       float p[8];
 #pragma unroll
@@ -240,11 +457,11 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       // (those that may not be seen are zero: 0 x NaN is not)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        u32x4 w = vr[i];
+        u32x4 w = widen(vr[i]);
         if (vis != 0xffffffffu && !(vis >> (i * RPL + lr) & 1)) w = u32x4{0, 0, 0, 0};
         *(u32x4*)(tile + (i * RPL + lr) * L::VROW + ld * 2) = w;
       }
-      load_block(vr, vb, tn, pn);
+      load_block(vr, vb, ve, tn, pn);
       page = next;
       next = load_page(t + 2 * kWaves);
       if (vis != 0xffffffffu) {
@@ -316,7 +533,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   // join the waves
   __syncthreads();
   float* om = (float*)smem;  // [wave][column][OROW]
-  if (col < a.G) {
+  if (col < u.ncol) {
 #pragma unroll
     for (int d = 0; d < ND; ++d)
       *(f32x4*)(om + (wid * kMaxGroup + col) * L::OROW + d * 16 + 4 * grp) = o[d];
@@ -326,8 +543,9 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
     }
   }
   __syncthreads();
-  for (int e = tid; e < a.G * HD; e += kBlock) {
+  for (int e = tid; e < u.ncol * HD; e += kBlock) {
     const int g = e / HD, d = e % HD;
+    if (SHARED && !use[g]) continue;
     float M = wm[0][g];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wm[w][g]);
@@ -339,13 +557,14 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       ls += c * wl[w][g];
       os += c * om[(w * kMaxGroup + g) * L::OROW + d];
     }
-    const int64_t rh = (int64_t)seq * a.H + h0 + g;
-    if (a.S == 1) {
+    place(g, row, head);
+    const int64_t rh = (int64_t)row * a.H + head;
+    if (!SHARED && a.S == 1) {
       const bool none = ls == 0.f;  // no visible key
-      store_out(a, NT == 3, (int64_t)seq * a.ldo + (int64_t)(h0 + g) * HD + d, none ? 0.f : os / ls);
+      store_out(a, NT == 3, (int64_t)row * a.ldo + (int64_t)head * HD + d, none ? 0.f : os / ls);
       if (d == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
     } else {
-      const int64_t at = (int64_t)split * a.n_rows * a.H + rh;
+      const int64_t at = (int64_t)u.slot * a.n_rows * a.H + rh;
       a.part_o[at * HD + d] = os;
       if (d == 0) {
         a.part_ml[at * 2] = ls != ls ? ls : M;
@@ -477,9 +696,10 @@ constexpr float kSlack = 8.f;
 // Products by which LDS reads run ahead of their use.
 constexpr int kAhead = 4;
 
-template <int HD, int NT, bool PAGED, int W>
-__global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
+template <int HD, int NT, Keys KEYS, int W, bool SHARED = false>
+__global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   using L = RowsLds<HD>;
+  constexpr bool PAGED = KEYS != kPacked, Q8 = KEYS == kPaged8;
   constexpr int kThreads = W * AIO_WAVE, kRows = W * 32;
   extern __shared__ __align__(16) char smem[];
   __shared__ uint8_t seen[kKeys];
@@ -492,31 +712,76 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
   const int rl = lane & 31, kh = lane >> 5;
-  const int split = udiv(blockIdx.x, a.by_s);  // by_s: workgroups per split
-  const int lin = blockIdx.x - split * a.by_s.d;
+  int b = blockIdx.x;
+  UDiv by_s = a.by_s;  // workgroups per split
+  bool shared = false;  // a group's shared keys, not a sequence's own
+  if constexpr (SHARED) {
+    shared = b < a.px.groups;
+    if (shared) by_s = a.px.by_s;
+    else b -= a.px.groups;
+  }
+  const int split = udiv(b, by_s);
+  const int lin = b - split * by_s.d;
   const int tg = udiv(lin, a.by_hkv), kvh = lin - tg * a.kv.Hkv;
-  int seq, tile;
-  if (!find_tile<kRows, PAGED>(a, tg, seq, tile)) return;
-  int first, count, key0, len, full;
-  seq_rows(a.cu_q, a.n_rows, seq, first, count);
-  seq_keys<PAGED>(a, seq, key0, len, full);
+  int seq = 0, tile = 0, first = 0, count = 0, key0 = 0, len = 0, full = 0, key_t0 = 0;
+  int slot = split, splits = a.S;
+  GroupTile of{};
+  if constexpr (SHARED) {
+    if (shared) {
+      if (!find_group_tile<kRows>(a, tg, of)) return;
+      seq = of.seq;
+      tile = of.tile;
+      first = of.first;
+      count = of.count;
+      full = len = shared_keys(a, of.group, seq);
+      if (len == 0) return;
+      splits = a.px.S;
+    }
+  }
+  if (!shared) {
+    if (!find_tile<kRows, PAGED>(a, tg, seq, tile)) return;
+    seq_rows(a.cu_q, a.n_rows, seq, first, count);
+    seq_keys<PAGED>(a, seq, key0, len, full);
+    if constexpr (SHARED) {
+      const int n = shared_keys_of(a, seq);
+      if (len >= n && full - count >= n - 1) key_t0 = n / kKeys;
+      slot = a.px.S + split;
+      splits = a.px.own;
+    }
+  }
   const int packed = count * a.G, p0 = tile * kRows;
   const int h0 = kvh * a.G;
   // this lane's query
   const int pr = p0 + wid * 32 + rl;
   const bool live = pr < packed;
   const int row = udiv(min(pr, packed - 1), a.by_g), g = min(pr, packed - 1) - row * a.G;
-  auto sees = [&](int r) { return min(full - count + r, len - 1); };  // row r's last key
+  // row r's last key
+  auto sees = [&](int r) { return shared ? len - 1 : min(full - count + r, len - 1); };
   const int lim = sees(row);
   // the last key that any row of the wave, of the workgroup sees, and the last
   // that all rows of the workgroup see
   const int wave_lim = sees(udiv(min(p0 + wid * 32 + 31, packed - 1), a.by_g));
   const int wg_lim = sees(udiv(min(p0 + kRows, packed) - 1, a.by_g));
   const int all_lim = sees(udiv(p0, a.by_g));
-  const int nkt = wg_lim < 0 ? 0 : wg_lim / kKeys + 1;
+  const int nkt = (wg_lim < 0 ? 0 : wg_lim / kKeys + 1) - key_t0;
   // this split's key tiles
-  const int each = nkt / a.S, rest = nkt - each * a.S;
-  const int t0 = split * each + min(split, rest), t1 = t0 + each + (split < rest ? 1 : 0);
+  const int each = nkt / splits, rest = nkt - each * splits;
+  const int t0 = key_t0 + split * each + min(split, rest);
+  const int t1 = t0 + each + (split < rest ? 1 : 0);
+  // the rows that see all of the shared keys (the others' own workgroups read them)
+  bool takes_part = true;
+  if (shared && live) {
+    int lo = of.seq, hi = of.end;  // this row's sequence
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (a.cu_q[mid] <= first + row) lo = mid;
+      else hi = mid;
+    }
+    int f, n, k, there, all;
+    seq_rows(a.cu_q, a.n_rows, lo, f, n);
+    seq_keys<true>(a, lo, k, there, all);
+    takes_part = there >= len && all - n >= len - 1;
+  }
 
   bf16x8 q[NC][NT];
 #pragma unroll
@@ -526,8 +791,14 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   // staging: pass p of this wave is rows p RPP + wid RPW .. + RPW - 1, of a lane 16
   // bytes of one
   const int wr = wid * RPW, lr = lane / TPR, sd = lane % TPR * 8;
-  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride;
-  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride;
+  using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
+  const Elem* kb = (const Elem*)a.kv.k + kvh * a.kv.head_stride;
+  const Elem* vb = (const Elem*)a.kv.v + kvh * a.kv.head_stride;
+  const uint8_t *ke = nullptr, *ve = nullptr;
+  if constexpr (Q8) {
+    ke = a.exp.k + kvh * a.exp.head_stride;
+    ve = a.exp.v + kvh * a.exp.head_stride;
+  }
   const int64_t lane_at = PAGED ? lr * HD + sd : lr * a.kv.stride + sd;
   const int32_t* table = PAGED ? a.kv.table + (int64_t)seq * a.kv.tstride : nullptr;
   const int pmask = (1 << a.kv.shift) - 1;
@@ -630,11 +901,17 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
       }
       return pg;
     };
-    auto load_tile = [&](u32x4 (&r)[NP], const uint16_t* from, int t, const PageIds& pg) {
+    auto load_tile = [&](Row8<Q8> (&r)[NP], const Elem* from, const uint8_t* exps, int t,
+                         const PageIds& pg) {
       const int key = min(t, tp - 1) * kKeys + wr;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        if constexpr (PAGED) {
+        if constexpr (Q8) {
+          const int in_page = (key + p * RPP) & pmask;
+          r[p].code = *(const uint2*)(from + (pg.id[p] * a.kv.stride + (int64_t)in_page * HD) +
+                                      (uint32_t)lane_at);
+          r[p].exp = exps[pg.id[p] * a.exp.stride + in_page + (uint32_t)lr];
+        } else if constexpr (PAGED) {
           const int64_t at = pg.id[p] * a.kv.stride + (int64_t)((key + p * RPP) & pmask) * HD;
           r[p] = *(const u32x4*)(from + at + (uint32_t)lane_at);
         } else {
@@ -642,17 +919,17 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         }
       }
     };
-    auto store_keys = [&](const u32x4 (&r)[NP], int buf) {
+    auto store_keys = [&](const Row8<Q8> (&r)[NP], int buf) {
 #pragma unroll
       for (int p = 0; p < NP; ++p)
-        *(u32x4*)(smem + buf * L::KBYTES + st_at + p * RPP * L::KROW) = r[p];
+        *(u32x4*)(smem + buf * L::KBYTES + st_at + p * RPP * L::KROW) = widen(r[p]);
     };
-    auto store_values = [&](const u32x4 (&r)[NP], int buf) {
+    auto store_values = [&](const Row8<Q8> (&r)[NP], int buf) {
 #pragma unroll
       for (int p = 0; p < NP; ++p)
-        *(u32x4*)(smem + 2 * L::KBYTES + buf * L::VBYTES + sv_at + p * RPP * L::VROW) = r[p];
+        *(u32x4*)(smem + 2 * L::KBYTES + buf * L::VBYTES + sv_at + p * RPP * L::VROW) = widen(r[p]);
     };
-    u32x4 kr[NP], vr[NP];
+    Row8<Q8> kr[NP], vr[NP];
     PageIds pg2 = pages_of(t0 + 2), pg3 = pages_of(t0 + 3), pg4 = pages_of(t0 + 4);
     float mx;
     // One tile: its softmax while the next tile's scores (sn) are multiplied, then
@@ -700,8 +977,8 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      load_tile(kr, kb, t + 3, pg3);
-      load_tile(vr, vb, t + 2, pg2);
+      load_tile(kr, kb, ke, t + 3, pg3);
+      load_tile(vr, vb, ve, t + 2, pg2);
       pg2 = pg3;
       pg3 = pg4;
       pg4 = pages_of(t + 5);
@@ -726,14 +1003,14 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
     f32x16 sa[2], sb[2];
     {
       const PageIds pg0 = pages_of(t0), pg1 = pages_of(t0 + 1);
-      load_tile(kr, kb, t0, pg0);
-      load_tile(vr, vb, t0, pg0);
+      load_tile(kr, kb, ke, t0, pg0);
+      load_tile(vr, vb, ve, t0, pg0);
       store_keys(kr, 0);
       store_values(vr, 0);
-      load_tile(kr, kb, t0 + 1, pg1);
+      load_tile(kr, kb, ke, t0 + 1, pg1);
       store_keys(kr, 1);
-      load_tile(kr, kb, t0 + 2, pg2);
-      load_tile(vr, vb, t0 + 1, pg1);
+      load_tile(kr, kb, ke, t0 + 2, pg2);
+      load_tile(vr, vb, ve, t0 + 1, pg1);
     }
     __syncthreads();
 #pragma unroll
@@ -765,22 +1042,28 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   // holes.
   for (int t = tp; t < t1; ++t) {
     const int j0 = t * kKeys;
-    u32x4 kr[NP], vr[NP];
+    Row8<Q8> kr[NP], vr[NP];
     uint32_t ok = 0;  // bit p: the row of pass p is there
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int key = j0 + p * RPP + wr;
       bool there = key + lr < len;
-      int64_t at = (int64_t)(key0 + key) * a.kv.stride;
+      int64_t at = (int64_t)(key0 + key) * a.kv.stride, exp_at = 0;
       if constexpr (PAGED) {
         const int page = key < len ? table[key >> a.kv.shift] : -1;
         there &= (unsigned)page < (unsigned)a.kv.limit;
         at = page * a.kv.stride + (int64_t)(key & pmask) * HD;
+        if constexpr (Q8) exp_at = page * a.exp.stride + (key & pmask) + lr;
       }
-      kr[p] = vr[p] = u32x4{0, 0, 0, 0};
+      kr[p] = vr[p] = Row8<Q8>{};
       if (there) {
-        kr[p] = *(const u32x4*)(kb + at + lane_at);
-        vr[p] = *(const u32x4*)(vb + at + lane_at);
+        if constexpr (Q8) {
+          kr[p] = {*(const uint2*)(kb + at + lane_at), ke[exp_at]};
+          vr[p] = {*(const uint2*)(vb + at + lane_at), ve[exp_at]};
+        } else {
+          kr[p] = *(const u32x4*)(kb + at + lane_at);
+          vr[p] = *(const u32x4*)(vb + at + lane_at);
+        }
         ok |= 1u << p;
       }
     }
@@ -788,10 +1071,11 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
     bool odd = false;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      *(u32x4*)(smem + st_at + p * RPP * L::KROW) = kr[p];
-      *(u32x4*)(smem + 2 * L::KBYTES + sv_at + p * RPP * L::VROW) = vr[p];
+      const u32x4 value = widen(vr[p]);
+      *(u32x4*)(smem + st_at + p * RPP * L::KROW) = widen(kr[p]);
+      *(u32x4*)(smem + 2 * L::KBYTES + sv_at + p * RPP * L::VROW) = value;
       if (sd == 0) seen[p * RPP + wr + lr] = ok >> p & 1;
-      odd |= not_finite(vr[p]);
+      odd |= not_finite(value);
     }
     if (__syncthreads_or(odd)) {
       // Values that are not finite must not meet a weight of 0 in a product: they go
@@ -871,8 +1155,15 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Att
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
   const int64_t rh = (int64_t)(first + row) * a.H + h0 + g;
-  if (a.S > 1) {
-    const int64_t at = (int64_t)split * a.n_rows * a.H + rh;
+  if (SHARED || a.S > 1) {
+    if constexpr (SHARED) {
+      if (!takes_part) return;
+      if (!shared && split == 0 && key_t0 == 0 && kh == 0) {
+        for (int i = 0; i < a.px.S; ++i)
+          a.part_ml[((int64_t)i * a.n_rows * a.H + rh) * 2] = -INFINITY;
+      }
+    }
+    const int64_t at = (int64_t)slot * a.n_rows * a.H + rh;
     if (kh == 0) {
       a.part_ml[at * 2] = m;
       a.part_ml[at * 2 + 1] = l;
@@ -971,10 +1262,10 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
 }
 
-template <int HD, int NT, bool PAGED, int W>
-hipError_t launch_rows_w(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+template <int HD, int NT, Keys KEYS, bool SHARED, int W>
+hipError_t launch_rows_w(const ArgsOf<KEYS == kPaged8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
   constexpr int lds = RowsLds<HD>::BYTES(NT, W);
-  const auto fn = k_attn_rows<HD, NT, PAGED, W>;
+  const auto fn = k_attn_rows<HD, NT, KEYS, W, SHARED>;
   const hipError_t e =
       hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
@@ -982,32 +1273,54 @@ hipError_t launch_rows_w(const AttnArgs& a, const AttnPlan& p, hipStream_t strea
   return hipGetLastError();
 }
 
-template <int HD, int NT, bool PAGED>
-hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+template <int HD, int NT, Keys KEYS, bool SHARED>
+hipError_t launch_rows(const ArgsOf<KEYS == kPaged8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
   if constexpr (NT == 1) {
-    if (p.waves == 8) return launch_rows_w<HD, NT, PAGED, 8>(a, p, stream);
+    if (p.waves == 8) return launch_rows_w<HD, NT, KEYS, SHARED, 8>(a, p, stream);
   }
-  return launch_rows_w<HD, NT, PAGED, 4>(a, p, stream);
+  return launch_rows_w<HD, NT, KEYS, SHARED, 4>(a, p, stream);
 }
 
-template <int HD, int NT>
-hipError_t launch(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+template <int HD, int NT, bool Q8, bool SHARED, bool STREAM>
+hipError_t launch_step(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
+  constexpr int lds = StepLds<HD>::BYTES(NT);
+  const auto fn = k_attn_step<HD, NT, STREAM, Q8, SHARED>;
+  const hipError_t e =
+      hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fn, dim3((unsigned)p.groups), dim3(kBlock), lds, stream, a);
+  return hipGetLastError();
+}
+
+template <int HD, int NT, bool Q8, bool SHARED>
+hipError_t launch(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
   hipError_t e;
   if (!p.rows) {
-    constexpr int lds = StepLds<HD>::BYTES(NT);
-    const auto fn = p.stream ? k_attn_step<HD, NT, true> : k_attn_step<HD, NT, false>;
-    e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(fn, dim3((unsigned)p.groups), dim3(kBlock), lds, stream, a);
-    e = hipGetLastError();
+    // (shared keys are read by several workgroups)
+    e = !SHARED && p.stream ? launch_step<HD, NT, Q8, SHARED, !SHARED>(a, p, stream)
+                            : launch_step<HD, NT, Q8, SHARED, false>(a, p, stream);
+  } else if constexpr (Q8) {
+    e = launch_rows<HD, NT, kPaged8, SHARED>(a, p, stream);
+  } else if (SHARED || a.kv.table) {
+    e = launch_rows<HD, NT, kPaged, SHARED>(a, p, stream);
   } else {
-    e = a.kv.table ? launch_rows<HD, NT, true>(a, p, stream) : launch_rows<HD, NT, false>(a, p, stream);
+    e = launch_rows<HD, NT, SHARED ? kPaged : kPacked, SHARED>(a, p, stream);
   }
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t rh = (int64_t)a.n_rows * a.H;
   hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
                      dim3(kBlock), 0, stream, a);
   return hipGetLastError();
+}
+
+template <bool Q8, bool SHARED>
+hipError_t launch_any(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, int hd, int dtype,
+                      hipStream_t stream) {
+  if (hd == 128)
+    return dtype == AIO_F32 ? launch<128, 3, Q8, SHARED>(a, p, stream)
+                            : launch<128, 1, Q8, SHARED>(a, p, stream);
+  return dtype == AIO_F32 ? launch<64, 3, Q8, SHARED>(a, p, stream)
+                          : launch<64, 1, Q8, SHARED>(a, p, stream);
 }
 
 }  // namespace

@@ -5,7 +5,8 @@
 // Workgroups up to which the keys are split.
 constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
 
-int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p) {
+int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p,
+                  int key_bytes) {
   *p = AttnPlan{};
   if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0 || s.max_len > (1 << 30)) return AIO_ERANGE;
   if (Hkv < 1 || H < 1 || H % Hkv) return AIO_EINVAL;
@@ -56,8 +57,41 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
   // read again (217 MB of at most 403: 59.3 against 55.6 us, 1.07 GB: 188 against 172).  A
   // small one's may stay in the 256 MB in front of memory.  (Below 2^24 sequences x heads
   // are left here, so the product stays in 64 bits.)
-  p->stream = !p->rows && (int64_t)s.n_seqs * s.max_len * Hkv * hd * 4 > (int64_t)64 << 20;
+  p->stream = !p->rows && (int64_t)s.n_seqs * s.max_len * Hkv * hd * 2 * key_bytes > (int64_t)64 << 20;
   if (p->splits > 1) p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
+  return AIO_OK;
+}
+
+int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, int hd, int dtype,
+                    AttnPlan* p, PrefixArgs* px, int key_bytes) {
+  *px = PrefixArgs{};
+  if (x.n_groups < 0 || x.n_groups > (1 << 30) || x.max_prefix < 0) return AIO_ERANGE;
+  const int rc = aio_attn_plan(s, H, Hkv, hd, dtype, p, key_bytes);
+  const int most_shared = std::min(x.max_prefix, s.max_len);
+  if (rc || x.n_groups == 0 || most_shared < kSharedUnit || s.n_rows == 0 || s.n_seqs == 0) return rc;
+  const int64_t G = H / Hkv;
+  px->n = x.n_groups;
+  px->max = most_shared;
+  // A place for every full tile of the groups' rows, and one more for each group with rows.
+  const int64_t width = p->rows ? 32 * p->waves : kMaxGroup;
+  const int64_t tiles = (int64_t)s.n_rows * G / width + std::min(x.n_groups, s.n_rows);
+  auto splits = [](int64_t most, int64_t base, int64_t units) {
+    return (int)std::max<int64_t>(1, std::min(units, most / std::max<int64_t>(1, base)));
+  };
+  // Both parts fill the GPU by themselves: the shared one starts first, and how much is left to
+  // the others is not known here.
+  const int64_t most = !p->rows ? kStepGroups : dtype == AIO_F32 ? kRowsGroups / 2 : kRowsGroups;
+  const int64_t unit = p->rows ? kKeys : 128, own = p->rows ? p->tiles : s.n_seqs;
+  px->S = splits(most, tiles * Hkv, (most_shared + unit - 1) / unit);
+  px->own = splits(most, own * Hkv, ((int64_t)s.max_len + unit - 1) / unit);
+  const int64_t shared = tiles * Hkv * px->S;
+  p->groups = shared + own * Hkv * px->own;
+  if (p->groups > (p->waves == 8 ? kMostGroups512 : kMostGroups)) return AIO_ERANGE;
+  px->groups = (int)shared;
+  px->by_s = make_udiv((unsigned)(tiles * Hkv), (unsigned)p->groups);
+  p->splits = px->S + px->own;
+  p->stream = false;
+  p->ws = (size_t)p->splits * s.n_rows * H * (hd + 2) * 4;
   return AIO_OK;
 }
 
@@ -81,7 +115,5 @@ size_t aio_attn_workspace_bound(int H, int Hkv, int hd) {
 
 hipError_t aio_launch_attention(const AttnArgs& a, const AttnPlan& p, int hd, int dtype,
                                 hipStream_t stream) {
-  if (hd == 128)
-    return dtype == AIO_F32 ? launch<128, 3>(a, p, stream) : launch<128, 1>(a, p, stream);
-  return dtype == AIO_F32 ? launch<64, 3>(a, p, stream) : launch<64, 1>(a, p, stream);
+  return launch_any<false, false>(a, p, hd, dtype, stream);
 }

@@ -42,12 +42,100 @@ KeysArgs paged_keys(const aio_paged_kv& kv, const aio_seqs& s) {
   return k;
 }
 
-// What both attentions check of the rows, and their launch.
-int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const aio_attn& a,
-              void* ws, size_t ws_bytes, void* stream) {
+KeysArgs paged_keys(const aio_q8_kv& kv, const aio_seqs& s) {
+  const aio_paged_kv as = {kv.k_dev,   kv.v_dev,     kv.page_stride, kv.head_stride,
+                           kv.n_pages, kv.page_size, kv.n_kv_heads,  kv.head_dim};
+  return paged_keys(as, s);
+}
+
+int check_q8(const aio_q8_kv& kv) {
+  if (!good(kv.k_dev, 16) || !good(kv.v_dev, 16) || !good(kv.k_exp_dev, 8) ||
+      !good(kv.v_exp_dev, 8))
+    return AIO_EINVAL;
+  if (kv.n_pages < 1 || kv.n_kv_heads < 1 || kv.page_stride < 0 || kv.page_stride % 16 ||
+      kv.head_stride < 0 || kv.head_stride % 16 || kv.exp_page_stride < 0 ||
+      kv.exp_page_stride % 8 || kv.exp_head_stride < 0 || kv.exp_head_stride % 8)
+    return AIO_EINVAL;
+  if (!page_size_ok(kv.page_size) || (kv.head_dim != 64 && kv.head_dim != 128))
+    return AIO_EUNSUPPORTED;
+  return AIO_OK;
+}
+
+// Codes, bytes, K or V that would take each other's place: pages and heads by their strides,
+// K against V and codes against bytes by their first rows too.
+bool q8_overlaps(const aio_q8_kv& kv) {
+  const int64_t codes = (int64_t)kv.page_size * kv.head_dim, exps = kv.page_size;
+  auto apart = [](const void* a, const void* b) {
+    const intptr_t x = (intptr_t)a, y = (intptr_t)b;
+    return (int64_t)(x < y ? y - x : x - y);
+  };
+  auto overlaps = [&](int64_t between, int64_t page, int64_t head, int64_t size) {
+    return aio_grid_overlaps(2, between, kv.n_pages, page, size) ||
+           aio_grid_overlaps(2, between, kv.n_kv_heads, head, size) ||
+           aio_grid_overlaps(kv.n_pages, page, kv.n_kv_heads, head, size);
+  };
+  if (overlaps(apart(kv.k_dev, kv.v_dev), kv.page_stride, kv.head_stride, codes) ||
+      overlaps(apart(kv.k_exp_dev, kv.v_exp_dev), kv.exp_page_stride, kv.exp_head_stride, exps))
+    return true;
+  for (const void* c : {kv.k_dev, kv.v_dev})
+    for (const void* e : {kv.k_exp_dev, kv.v_exp_dev})
+      if (apart(c, e) < ((uintptr_t)c < (uintptr_t)e ? codes : exps)) return true;
+  return false;
+}
+
+ExpArgs q8_exps(const aio_q8_kv& kv) {
+  return {(const uint8_t*)kv.k_exp_dev, (const uint8_t*)kv.v_exp_dev, kv.exp_page_stride,
+          kv.exp_head_stride};
+}
+
+// What both appends check of their sequences and rows: AIO_OK, kNothing where there are no
+// rows, or an error.
+constexpr int kNothing = 1;
+int check_append(const aio_seqs& s, const void* k_rows, const void* v_rows, int32_t dtype,
+                 int64_t row_stride, int64_t head_stride) {
+  if (s.n_seqs < 0 || s.n_rows < 0 || s.max_len < 0) return AIO_ERANGE;
+  if (!s.cu_q_dev && s.n_rows != s.n_seqs) return AIO_ERANGE;
+  if (s.n_rows > kMostGroups) return AIO_ERANGE;
+  if (dtype != AIO_F32 && dtype != AIO_BF16) return AIO_EINVAL;
+  const int64_t unit = dtype == AIO_F32 ? 4 : 8;
+  if (row_stride < 0 || row_stride % unit || head_stride < 0 || head_stride % unit)
+    return AIO_EINVAL;
+  if (s.n_rows == 0 || s.n_seqs == 0) return kNothing;
+  return good(k_rows, 16) && good(v_rows, 16) ? AIO_OK : AIO_EINVAL;
+}
+
+template <class KV>
+void set_append(AppendArgs& t, const KV& kv, const aio_seqs& s, const void* k_rows,
+                const void* v_rows, int64_t row_stride, int64_t head_stride) {
+  t.kv = paged_keys(kv, s);
+  t.k = (uint16_t*)kv.k_dev;
+  t.v = (uint16_t*)kv.v_dev;
+  t.cu_q = s.cu_q_dev;
+  t.n_seqs = s.n_seqs;
+  t.n_rows = s.n_rows;
+  t.max_len = s.max_len;
+  t.hd = kv.head_dim;
+  t.k_rows = k_rows;
+  t.v_rows = v_rows;
+  t.row_stride = row_stride;
+  t.head_stride = head_stride;
+}
+
+// What all attentions check of the rows, and their launch: over 8-bit keys with exps, with
+// groups that share keys with groups.
+int attention(const KeysArgs& keys, const ExpArgs* exps, int Hkv, int hd, const aio_seqs& s,
+              const aio_prefixes* groups_of, const aio_attn& a, void* ws, size_t ws_bytes,
+              void* stream) {
   AttnPlan p;
-  const int rc = aio_attn_plan(s, a.n_heads, Hkv, hd, a.dtype, &p);
+  PrefixArgs px{};
+  const int key_bytes = exps ? 1 : 2;
+  const int rc = groups_of ? aio_groups_plan(s, *groups_of, a.n_heads, Hkv, hd, a.dtype, &p, &px,
+                                             key_bytes)
+                           : aio_attn_plan(s, a.n_heads, Hkv, hd, a.dtype, &p, key_bytes);
   if (rc) return rc;
+  if (groups_of && groups_of->n_groups > 0 &&
+      (!good(groups_of->cu_seqs_dev, 4) || !good(groups_of->prefix_lens_dev, 4)))
+    return AIO_EINVAL;
   if (a.dtype != AIO_F32 && a.dtype != AIO_BF16) return AIO_EINVAL;
   const int64_t unit = a.dtype == AIO_F32 ? 4 : 8;  // elements in 16 bytes
   if (a.q_stride < 0 || a.q_stride % unit || a.out_stride < 0 || a.out_stride % unit)
@@ -59,7 +147,7 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   if (s.n_rows == 0 || s.n_seqs == 0) return AIO_OK;
   if (!good(a.q_dev, 16) || !good(a.out_dev, 16) || !aligned(a.lse_dev, 4)) return AIO_EINVAL;
   if (p.ws && (!good(ws, 16) || ws_bytes < p.ws)) return AIO_EINVAL;
-  AttnArgs t{};
+  AttnMoreArgs t{};
   t.kv = keys;
   t.cu_q = s.cu_q_dev;
   t.n_seqs = s.n_seqs;
@@ -70,7 +158,8 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
   const unsigned groups = (unsigned)p.groups;
   t.by_g = make_udiv((unsigned)t.G, (unsigned)std::min<int64_t>((int64_t)s.n_rows * t.G, 0x7fffffff));
   t.by_hkv = make_udiv((unsigned)Hkv, groups);
-  t.by_s = make_udiv(p.rows ? (unsigned)(p.tiles * Hkv) : (unsigned)p.splits, groups);
+  const int own = px.S ? px.own : p.splits;  // splits of a sequence's own keys
+  t.by_s = make_udiv(p.rows ? (unsigned)(p.tiles * Hkv) : (unsigned)own, groups);
   t.q = a.q_dev;
   t.out = a.out_dev;
   t.lse = a.lse_dev;
@@ -83,7 +172,16 @@ int attention(const KeysArgs& keys, int Hkv, int hd, const aio_seqs& s, const ai
     t.part_o = (float*)ws;
     t.part_ml = t.part_o + (size_t)p.splits * s.n_rows * t.H * hd;
   }
-  return done(aio_launch_attention(t, p, hd, a.dtype, (hipStream_t)stream));
+  if (exps) t.exp = *exps;
+  if (px.S) {
+    t.px = px;
+    t.px.cu_seqs = groups_of->cu_seqs_dev;
+    t.px.lens = groups_of->prefix_lens_dev;
+  }
+  const auto launch = px.S ? (exps ? aio_launch_attention8_groups : aio_launch_attention_groups)
+                           : aio_launch_attention8;
+  return done(px.S || exps ? launch(t, p, hd, a.dtype, (hipStream_t)stream)
+                           : aio_launch_attention(t, p, hd, a.dtype, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -116,6 +214,17 @@ bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t s
     if ((j < n2 && at - j * s2 < size) || (j + 1 < n2 && (j + 1) * s2 - at < size)) return true;
   }
   return false;
+}
+
+bool aio_rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb,
+                      int64_t n) {
+  typedef __int128 wide;
+  const wide x = (uintptr_t)a, y = (uintptr_t)b;
+  if (x + (wide)(n - 1) * sa + wa <= y || y + (wide)(n - 1) * sb + wb <= x) return false;
+  if (sa != sb || n == 1 || sa == 0) return true;
+  // rows of one stride: the one's place within the other's
+  const wide d = x < y ? (y - x) % sa : (sa - (x - y) % sa) % sa;
+  return d < wa || d + wb > sa;
 }
 
 bool aio_pages_overlap(const aio_paged_kv& kv) {
@@ -200,6 +309,11 @@ int guarded(F f) {
 
 extern "C" {
 
+int aio_rows_overlap_test(int64_t a, int64_t sa, int64_t wa, int64_t b, int64_t sb, int64_t wb,
+                          int64_t n) {
+  return aio_rows_overlap((const void*)a, sa, wa, (const void*)b, sb, wb, n);
+}
+
 size_t aio_attn_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
                                 int32_t head_dim) {
   if (!s) return 0;
@@ -214,8 +328,56 @@ int aio_paged_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_att
   int rc = aio_check_paged(*kv);
   if (rc == AIO_OK) rc = check_table(*s);
   if (rc) return rc;
-  return attention(paged_keys(*kv, *s), kv->n_kv_heads, kv->head_dim, *s, *a, ws_dev, ws_bytes,
-                   hip_stream);
+  return attention(paged_keys(*kv, *s), nullptr, kv->n_kv_heads, kv->head_dim, *s, nullptr, *a,
+                   ws_dev, ws_bytes, hip_stream);
+}
+
+int aio_q8_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_attn* a, void* ws_dev,
+                     size_t ws_bytes, void* hip_stream) {
+  if (!kv || !s || !a) return AIO_EINVAL;
+  if (s->cu_k_dev) return AIO_EINVAL;
+  int rc = check_q8(*kv);
+  if (rc == AIO_OK) rc = check_table(*s);
+  if (rc) return rc;
+  const ExpArgs e = q8_exps(*kv);
+  return attention(paged_keys(*kv, *s), &e, kv->n_kv_heads, kv->head_dim, *s, nullptr, *a, ws_dev,
+                   ws_bytes, hip_stream);
+}
+
+size_t aio_prefix_workspace_bytes(const aio_seqs* s, const aio_prefixes* x, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t head_dim) {
+  if (!s || !x) return 0;
+  size_t most = 0;
+  for (const int dtype : {AIO_F32, AIO_BF16}) {
+    AttnPlan p;
+    PrefixArgs px;
+    if (aio_groups_plan(*s, *x, n_heads, n_kv_heads, head_dim, dtype, &p, &px) == AIO_OK)
+      most = std::max(most, p.ws);
+  }
+  return most;
+}
+
+int aio_prefix_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_prefixes* x,
+                         const aio_attn* a, void* ws_dev, size_t ws_bytes, void* hip_stream) {
+  if (!kv || !s || !x || !a) return AIO_EINVAL;
+  if (s->cu_k_dev) return AIO_EINVAL;
+  int rc = aio_check_paged(*kv);
+  if (rc == AIO_OK) rc = check_table(*s);
+  if (rc) return rc;
+  return attention(paged_keys(*kv, *s), nullptr, kv->n_kv_heads, kv->head_dim, *s, x, *a, ws_dev,
+                   ws_bytes, hip_stream);
+}
+
+int aio_q8_prefix_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_prefixes* x,
+                            const aio_attn* a, void* ws_dev, size_t ws_bytes, void* hip_stream) {
+  if (!kv || !s || !x || !a) return AIO_EINVAL;
+  if (s->cu_k_dev) return AIO_EINVAL;
+  int rc = check_q8(*kv);
+  if (rc == AIO_OK) rc = check_table(*s);
+  if (rc) return rc;
+  const ExpArgs e = q8_exps(*kv);
+  return attention(paged_keys(*kv, *s), &e, kv->n_kv_heads, kv->head_dim, *s, x, *a, ws_dev,
+                   ws_bytes, hip_stream);
 }
 
 int aio_packed_attention(const aio_packed_kv* kv, const aio_seqs* s, const aio_attn* a,
@@ -237,7 +399,8 @@ int aio_packed_attention(const aio_packed_kv* kv, const aio_seqs* s, const aio_a
   k.limit = kv->n_rows;
   k.Hkv = kv->n_kv_heads;
   k.cu_k = s->cu_k_dev;
-  return attention(k, kv->n_kv_heads, kv->head_dim, *s, *a, ws_dev, ws_bytes, hip_stream);
+  return attention(k, nullptr, kv->n_kv_heads, kv->head_dim, *s, nullptr, *a, ws_dev, ws_bytes,
+                   hip_stream);
 }
 
 int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_rows_dev,
@@ -247,33 +410,94 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
   int rc = aio_check_paged(*kv);
   if (rc == AIO_OK) rc = check_table(*s);
   if (rc) return rc;
-  if (s->n_seqs < 0 || s->n_rows < 0 || s->max_len < 0) return AIO_ERANGE;
-  if (!s->cu_q_dev && s->n_rows != s->n_seqs) return AIO_ERANGE;
-  if (s->n_rows > kMostGroups) return AIO_ERANGE;
+  rc = check_append(*s, k_rows_dev, v_rows_dev, dtype, row_stride, head_stride);
+  if (rc < 0) return rc;
   if (aio_pages_overlap(*kv)) return AIO_EINVAL;
-  if (dtype != AIO_F32 && dtype != AIO_BF16) return AIO_EINVAL;
-  const int64_t unit = dtype == AIO_F32 ? 4 : 8;
-  if (row_stride < 0 || row_stride % unit || head_stride < 0 || head_stride % unit)
-    return AIO_EINVAL;
-  if (s->n_rows == 0 || s->n_seqs == 0) return AIO_OK;
-  if (!good(k_rows_dev, 16) || !good(v_rows_dev, 16)) return AIO_EINVAL;
+  if (rc == kNothing) return AIO_OK;
   // (the same rows to one place for K and V are written twice, but alike)
   if ((kv->k_dev != kv->v_dev || k_rows_dev != v_rows_dev) && aio_pool_overlaps(*kv, 0, 1))
     return AIO_EINVAL;
   AppendArgs t{};
-  t.kv = paged_keys(*kv, *s);
-  t.k = (uint16_t*)kv->k_dev;
-  t.v = (uint16_t*)kv->v_dev;
-  t.cu_q = s->cu_q_dev;
-  t.n_seqs = s->n_seqs;
-  t.n_rows = s->n_rows;
-  t.max_len = s->max_len;
-  t.hd = kv->head_dim;
-  t.k_rows = k_rows_dev;
-  t.v_rows = v_rows_dev;
-  t.row_stride = row_stride;
-  t.head_stride = head_stride;
+  set_append(t, *kv, *s, k_rows_dev, v_rows_dev, row_stride, head_stride);
   return done(aio_launch_append(t, dtype, (hipStream_t)hip_stream));
+}
+
+int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev,
+                  const void* v_rows_dev, int32_t dtype, int64_t row_stride,
+                  int64_t head_stride, void* hip_stream) {
+  if (!kv || !s) return AIO_EINVAL;
+  int rc = check_q8(*kv);
+  if (rc == AIO_OK) rc = check_table(*s);
+  if (rc) return rc;
+  rc = check_append(*s, k_rows_dev, v_rows_dev, dtype, row_stride, head_stride);
+  if (rc < 0) return rc;
+  if (q8_overlaps(*kv)) return AIO_EINVAL;
+  if (rc == kNothing) return AIO_OK;
+  Append8Args t{};
+  set_append(t, *kv, *s, k_rows_dev, v_rows_dev, row_stride, head_stride);
+  t.k_exp = (uint8_t*)kv->k_exp_dev;
+  t.v_exp = (uint8_t*)kv->v_exp_dev;
+  t.exp_stride = kv->exp_page_stride;
+  t.exp_head_stride = kv->exp_head_stride;
+  return done(aio_launch_append8(t, dtype, (hipStream_t)hip_stream));
+}
+
+int aio_qk_norm_rope(const aio_qk_rows* r, const int32_t* positions_dev,
+                     const void* q_weight_dev, const void* k_weight_dev, float eps, float base,
+                     void* hip_stream) {
+  if (!r) return AIO_EINVAL;
+  if (r->n_rows < 0 || r->n_rows > kMostGroups || r->n_heads < 1 || r->n_heads > (1 << 16) ||
+      r->n_kv_heads < 1 || r->n_kv_heads > (1 << 16))
+    return AIO_ERANGE;
+  if (r->head_dim != 64 && r->head_dim != 128) return AIO_EUNSUPPORTED;
+  if (r->dtype != AIO_F32 && r->dtype != AIO_BF16) return AIO_EINVAL;
+  if (!(eps > 0.f) || !isfinite(eps) || !(base > 1.f) || !isfinite(base)) return AIO_EINVAL;
+  const int64_t size = r->dtype == AIO_F32 ? 4 : 2;
+  struct Rows {
+    const void* p;
+    int64_t stride, width;  // bytes
+  } rows[4] = {{r->q_dev, r->q_stride * size, r->n_heads * r->head_dim * size},
+               {r->k_dev, r->k_stride * size, r->n_kv_heads * r->head_dim * size},
+               {r->q_out_dev, r->q_out_stride * size, r->n_heads * r->head_dim * size},
+               {r->k_out_dev, r->k_out_stride * size, r->n_kv_heads * r->head_dim * size}};
+  const int64_t strides[4] = {r->q_stride, r->k_stride, r->q_out_stride, r->k_out_stride};
+  for (int i = 0; i < 4; ++i) {
+    if (strides[i] < 0 || strides[i] > ((int64_t)1 << 56) || rows[i].stride % 16) return AIO_EINVAL;
+    if (i >= 2 && r->n_rows > 1 && rows[i].stride < rows[i].width) return AIO_EINVAL;
+  }
+  if (r->n_rows == 0) return AIO_OK;
+  for (const Rows& x : rows)
+    if (!good(x.p, 16)) return AIO_EINVAL;
+  if (!good(positions_dev, 4) || !aligned(q_weight_dev, 16) || !aligned(k_weight_dev, 16))
+    return AIO_EINVAL;
+  // every output against the other and against what is read, but for its own place
+  for (int o = 2; o < 4; ++o)
+    for (int i = 0; i < 4; ++i) {
+      if (i == o || (i == o - 2 && rows[i].p == rows[o].p &&
+                     (r->n_rows == 1 || rows[i].stride == rows[o].stride)))
+        continue;
+      if (aio_rows_overlap(rows[o].p, rows[o].stride, rows[o].width, rows[i].p, rows[i].stride,
+                           rows[i].width, r->n_rows))
+        return AIO_EINVAL;
+    }
+  QkArgs t{};
+  for (int i = 0; i < 2; ++i) {
+    t.in[i] = rows[i].p;
+    t.out[i] = (void*)rows[2 + i].p;
+    t.ldi[i] = strides[i];
+    t.ldo[i] = strides[2 + i];
+  }
+  t.w[0] = (const uint16_t*)q_weight_dev;
+  t.w[1] = (const uint16_t*)k_weight_dev;
+  t.n_rows = r->n_rows;
+  t.H = r->n_heads;
+  t.Hkv = r->n_kv_heads;
+  t.pos = positions_dev;
+  t.eps = eps;
+  const double pi = 3.14159265358979323846;
+  for (int i = 0; i < r->head_dim / 2; ++i)
+    t.turns[i] = pow((double)base, -2.0 * i / r->head_dim) / (2 * pi);
+  return done(aio_launch_qk(t, r->head_dim, r->dtype, (hipStream_t)hip_stream));
 }
 
 int aio_page_copy(void* pool_dev, int32_t n_planes, int64_t plane_bytes, int32_t n_pages,

@@ -28,6 +28,13 @@ int aio_check_paged(const aio_paged_kv& kv);
 // Blocks of `size` in a grid of n1 x n2, s1 and s2 apart (none negative): whether two of them
 // share an element.
 bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t size);
+// Two lists of n rows, of wa and wb bytes: whether any rows share a byte (also true where ranges
+// of different strides mingle).
+bool aio_rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb,
+                      int64_t n);
+// The same for the tests (not part of the ABI; pure host), by addresses.
+extern "C" int aio_rows_overlap_test(int64_t a, int64_t sa, int64_t wa, int64_t b, int64_t sb,
+                                     int64_t wb, int64_t n);
 // Pages or heads that would take each other's rows, or K those of V, in n_layers layers
 // (one: layer_stride 0): not to be written.
 bool aio_pages_overlap(const aio_paged_kv& kv);
@@ -45,7 +52,14 @@ struct AttnPlan {
   size_t ws;       // bytes of partial results
 };
 // AIO_OK, or the error that the entry points return for these sizes.
-int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p);
+// (key_bytes: of an element of the keys)
+int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p,
+                  int key_bytes = 2);
+// The same with groups (PrefixArgs's sizes); without any that can share, as without groups
+// (px->S: 0).
+struct PrefixArgs;
+int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, int hd, int dtype,
+                    AttnPlan* p, PrefixArgs* px, int key_bytes = 2);
 // What an attention takes, for the tests (not part of the ABI; pure host): out[3] = waves of
 // a workgroup of prompt rows (0: one new token per sequence), splits of the keys, and
 // whether the keys pass the caches by.
@@ -56,7 +70,7 @@ size_t aio_attn_workspace_bound(int H, int Hkv, int hd);
 
 // Where an attention's keys lie: pages, or (table null) packed rows.
 struct KeysArgs {
-  const uint16_t* k;
+  const uint16_t* k;    // (8-bit pages: their codes)
   const uint16_t* v;
   int64_t stride;       // elements between pages, packed: between rows
   int64_t head_stride;
@@ -85,12 +99,42 @@ struct AttnArgs {
   float* part_ml;    // [S][n_rows][H][2]: maximum (log2 units), sum
 };
 
+// The bytes of 8-bit rows.
+struct ExpArgs {
+  const uint8_t* k;
+  const uint8_t* v;
+  int64_t stride, head_stride;
+};
+
+// Groups of sequences that share their first keys (the shared part's workgroups come first).
+struct PrefixArgs {
+  const int32_t* cu_seqs;  // [n + 1]
+  const int32_t* lens;     // [n]
+  int n, max;
+  int S, own;              // splits of a group's shared keys and of a sequence's own
+  int groups;              // workgroups of the shared part
+  UDiv by_s;               // ... of one split of it
+};
+
+// What 8-bit keys and groups take besides.
+struct AttnMoreArgs : AttnArgs {
+  ExpArgs exp;
+  PrefixArgs px;  // S = px.S + px.own
+};
+
+// Over bf16 keys; over 8-bit ones; the same with groups of shared keys.
 hipError_t aio_launch_attention(const AttnArgs& a, const AttnPlan& p, int hd, int dtype,
                                 hipStream_t stream);
+hipError_t aio_launch_attention8(const AttnMoreArgs& a, const AttnPlan& p, int hd, int dtype,
+                                 hipStream_t stream);
+hipError_t aio_launch_attention_groups(const AttnMoreArgs& a, const AttnPlan& p, int hd, int dtype,
+                                       hipStream_t stream);
+hipError_t aio_launch_attention8_groups(const AttnMoreArgs& a, const AttnPlan& p, int hd, int dtype,
+                                        hipStream_t stream);
 
 struct AppendArgs {
   KeysArgs kv;          // pages
-  uint16_t* k;
+  uint16_t* k;          // (8-bit pages: their codes)
   uint16_t* v;
   const int32_t* cu_q;
   int n_seqs, n_rows, max_len, hd;
@@ -99,6 +143,24 @@ struct AppendArgs {
   int64_t row_stride, head_stride;
 };
 hipError_t aio_launch_append(const AppendArgs& a, int dtype, hipStream_t stream);
+struct Append8Args : AppendArgs {
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  int64_t exp_stride, exp_head_stride;
+};
+hipError_t aio_launch_append8(const Append8Args& a, int dtype, hipStream_t stream);
+
+struct QkArgs {
+  const void* in[2];     // queries, keys
+  void* out[2];
+  int64_t ldi[2], ldo[2];
+  const uint16_t* w[2];  // null: 1
+  int n_rows, H, Hkv;
+  const int32_t* pos;
+  float eps;
+  double turns[64];      // of pair i per position: base^(-2i / hd) / 2 pi
+};
+hipError_t aio_launch_qk(const QkArgs& a, int hd, int dtype, hipStream_t stream);
 
 // One launch's copies travel in the kernel's arguments (4 KB at most): no
 // memory that has to outlive the call, or to be kept apart per stream.
