@@ -112,6 +112,18 @@ AIO_DEV u32x4 widen(const Codes8& r) {
   return o;
 }
 
+// Eight codes as bf16.
+AIO_DEV bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i < 2 ? lo : hi;
+    o[i] = __float_as_uint(i8_at(w, 2 * (i & 1))) >> 16 |
+           (__float_as_uint(i8_at(w, 2 * (i & 1) + 1)) & 0xffff0000u);
+  }
+  return as_bf16x8(o);
+}
+
 // Where the keys of an attention lie.
 enum Keys { kPaged, kPacked, kPaged8 };
 
@@ -307,6 +319,72 @@ AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
   return split == 0 || u.c0 < len;
 }
 
+// Row and head of a column.
+template <bool SHARED>
+AIO_DEV void step_place(const AttnArgs& a, const StepUnit& u, int c, int& row, int& head) {
+  row = u.seq;
+  head = u.kvh * a.G + c;
+  if constexpr (SHARED) {
+    const int r = udiv(u.p0 + c, a.by_g);
+    row = u.first + r;
+    head += u.p0 - r * a.G;
+  }
+}
+
+// Joins the waves' states (o and l as sums, m as a score) in LDS ([wave][column][HD + 4] floats),
+// and writes the workgroup's result.
+template <int HD, int NT, bool SHARED>
+AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, char* smem, const bool* use,
+                         const f32x4 (&o)[HD / 16], float m, float l) {
+  __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
+  constexpr int OROW = HD + 4;
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
+  const int col = lane & 15, grp = lane >> 4;
+  __syncthreads();
+  float* om = (float*)smem;
+  if (col < u.ncol) {
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d)
+      *(f32x4*)(om + (wid * kMaxGroup + col) * OROW + d * 16 + 4 * grp) = o[d];
+    if (grp == 0) {
+      wm[wid][col] = m * a.scale_log2;
+      wl[wid][col] = l;
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < u.ncol * HD; e += kBlock) {
+    const int g = e / HD, d = e % HD;
+    if (SHARED && !use[g]) continue;
+    float M = wm[0][g];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wm[w][g]);
+    float ls = 0.f, os = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float x = wm[w][g];
+      const float c = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M);
+      ls += c * wl[w][g];
+      os += c * om[(w * kMaxGroup + g) * OROW + d];
+    }
+    int row, head;
+    step_place<SHARED>(a, u, g, row, head);
+    const int64_t rh = (int64_t)row * a.H + head;
+    if (!SHARED && a.S == 1) {
+      const bool none = ls == 0.f;  // no visible key
+      store_out(a, NT == 3, (int64_t)row * a.ldo + (int64_t)head * HD + d, none ? 0.f : os / ls);
+      if (d == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
+    } else {
+      const int64_t at = (int64_t)u.slot * a.n_rows * a.H + rh;
+      a.part_o[at * HD + d] = os;
+      if (d == 0) {
+        a.part_ml[at * 2] = ls != ls ? ls : M;
+        a.part_ml[at * 2 + 1] = ls;
+      }
+    }
+  }
+}
+
 // Workgroup (sequence, kv head, split): the G query heads of the kv head are
 // columns of one 16-wide tile; each wave takes every fourth block of 32 keys of
 // the split, and the waves' states join in LDS.  What bounds it is the reading of
@@ -327,8 +405,9 @@ struct StepLds {
   static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
 };
 
-template <int HD, int NT, bool STREAM, bool Q8 = false, bool SHARED = false>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(ArgsOf<Q8, SHARED> a) {
+template <int HD, int NT, bool STREAM, bool SHARED = false>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(
+    ArgsOf<false, SHARED> a) {
   using L = StepLds<HD>;
   extern __shared__ __align__(16) char smem[];
   __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
@@ -346,20 +425,10 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   } else {
     if (!step_unit(a, u)) return;
   }
-  const int seq = u.seq, kvh = u.kvh, c0 = u.c0, c1 = u.c1, h0 = kvh * a.G;
-  // row and head of a column
-  auto place = [&](int c, int& row, int& head) {
-    row = seq;
-    head = h0 + c;
-    if constexpr (SHARED) {
-      const int r = udiv(u.p0 + c, a.by_g);
-      row = u.first + r;
-      head = h0 + u.p0 + c - r * a.G;
-    }
-  };
+  const int seq = u.seq, kvh = u.kvh, c0 = u.c0, c1 = u.c1;
   bf16x8 q[NC][NT];
   int row, head;
-  place(min(col, u.ncol - 1), row, head);
+  step_place<SHARED>(a, u, min(col, u.ncol - 1), row, head);
 #pragma unroll
   for (int c = 0; c < NC; ++c)
     load_query<NT>(a, row, head, HD, c * 32 + 8 * grp, col < u.ncol, q[c]);
@@ -371,14 +440,8 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 
   const int32_t* table = a.kv.table + (int64_t)seq * a.kv.tstride;
   const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
-  using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
-  const Elem* kb = (const Elem*)a.kv.k + kvh * a.kv.head_stride;
-  const Elem* vb = (const Elem*)a.kv.v + kvh * a.kv.head_stride;
-  const uint8_t *ke = nullptr, *ve = nullptr;
-  if constexpr (Q8) {
-    ke = a.exp.k + kvh * a.exp.head_stride;
-    ve = a.exp.v + kvh * a.exp.head_stride;
-  }
+  const uint16_t* kb = a.kv.k + kvh * a.kv.head_stride;
+  const uint16_t* vb = a.kv.v + kvh * a.kv.head_stride;
   // Lane l holds the page of key l mod 32 of a block (-1: not visible).
   auto load_page = [&](int t) {
     const int key = c0 + t * 32 + (lane & 31);
@@ -390,22 +453,15 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   // would take half a 128-byte line of 16 rows); the 8 keys of an aligned group share
   // a page, so pages are wave uniform.  Keys that are not visible read page 0.
   const int lr = lane / TPR, ld = lane % TPR * 8;
-  Row8<Q8> kr[NV], vr[NV];
-  auto load_block = [&](Row8<Q8> (&r)[NV], const Elem* from, const uint8_t* exps, int t, int page) {
+  u32x4 kr[NV], vr[NV];
+  auto load_block = [&](u32x4 (&r)[NV], const uint16_t* from, int t, int page) {
     const int j0 = c0 + t * 32;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int pg = max(__builtin_amdgcn_readlane(page, i * RPL), 0);
-      const int slot = (j0 + i * RPL) & pm;
-      const Elem* p = from + (pg * a.kv.stride + slot * HD) + (uint32_t)(lr * HD + ld);
-      if constexpr (Q8) {
-        const u32x2* c = (const u32x2*)p;
-        const u32x2 w = STREAM ? __builtin_nontemporal_load(c) : *c;
-        r[i].code = make_uint2(w.x, w.y);
-        r[i].exp = exps[pg * a.exp.stride + slot + (uint32_t)lr];
-      } else {
-        r[i] = STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
-      }
+      const int64_t at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
+                         ((j0 + i * RPL) & pm) * HD;
+      const u32x4* p = (const u32x4*)(from + at + (uint32_t)(lr * HD + ld));
+      r[i] = STREAM ? __builtin_nontemporal_load(p) : *p;
     }
   };
   f32x4 o[ND];
@@ -426,8 +482,8 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 
   int page = load_page(wid), next = load_page(wid + kWaves);
   if (wid < nt) {
-    load_block(kr, kb, ke, wid, page);
-    load_block(vr, vb, ve, wid, page);
+    load_block(kr, kb, wid, page);
+    load_block(vr, vb, wid, page);
   }
   for (int t = wid; t < nt;) {
     const int te = NT == 3 ? min(nt, t + kStepCarry * kWaves) : nt;
@@ -437,8 +493,8 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       const bool more = t + kWaves < nt;
       const int tn = more ? t + kWaves : t, pn = more ? next : page;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = widen(kr[i]);
-      load_block(kr, kb, ke, tn, pn);
+      for (int i = 0; i < NV; ++i) *(u32x4*)(tile + (i * RPL + lr) * L::KROW + ld * 2) = kr[i];
+      load_block(kr, kb, tn, pn);
       wave_lds_sync();  // the keys are in LDS
       float p[8];
 #pragma unroll
@@ -457,11 +513,11 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       // (those that may not be seen are zero: 0 x NaN is not)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        u32x4 w = widen(vr[i]);
+        u32x4 w = vr[i];
         if (vis != 0xffffffffu && !(vis >> (i * RPL + lr) & 1)) w = u32x4{0, 0, 0, 0};
         *(u32x4*)(tile + (i * RPL + lr) * L::VROW + ld * 2) = w;
       }
-      load_block(vr, vb, ve, tn, pn);
+      load_block(vr, vb, tn, pn);
       page = next;
       next = load_page(t + 2 * kWaves);
       if (vis != 0xffffffffu) {
@@ -557,7 +613,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       ls += c * wl[w][g];
       os += c * om[(w * kMaxGroup + g) * L::OROW + d];
     }
-    place(g, row, head);
+    step_place<SHARED>(a, u, g, row, head);
     const int64_t rh = (int64_t)row * a.H + head;
     if (!SHARED && a.S == 1) {
       const bool none = ls == 0.f;  // no visible key
@@ -572,6 +628,220 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
       }
     }
   }
+}
+
+// The same over pages of 8-bit codes.  Codes stay codes as far as LDS: a wave stores a block's
+// rows and the rows' powers of two, reads the keys as operands (a lane's eight codes of
+// a k chunk are eight neighbours of its row: the queries' chunks are taken alike) and the values
+// transposed, and makes bf16 of both in registers, where codes are exact.  A power of two goes
+// to the key's score and to the value's weight, 16 products instead of 128.
+template <int HD>
+struct Step8Lds {
+  // bytes of a row, and of the second 16 rows from the first: the 16 rows of an operand, and
+  // the rows 0 .. 7 and 16 .. 23 of a transposing read, lie in distinct banks
+  static constexpr int ROW = HD + 16, HALF = 16 * ROW + 128;
+  static constexpr int TBYTES = HALF + 16 * ROW;  // of a key or value tile
+  static constexpr int WBYTES = 2 * TBYTES + 64 * 4;
+  static constexpr int OBYTES = kWaves * kMaxGroup * (HD + 4) * 4;
+  static constexpr int TILES = kWaves * WBYTES > OBYTES ? kWaves * WBYTES : OBYTES;
+  static constexpr int HBYTES = HD * 16 * 4 + AIO_WAVE * 4;
+  static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
+};
+
+template <int HD, int NT, bool STREAM, bool SHARED = false>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMoreArgs a) {
+  using L = Step8Lds<HD>;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ bool use[kMaxGroup];
+  constexpr int NC = HD / 32;              // k chunks of a score product
+  constexpr int TPR = HD / 16;             // lanes of a row
+  constexpr int RPL = AIO_WAVE / TPR;      // rows per load: 8 or 16, of one page or two
+  constexpr int NV = 32 / RPL;             // loads of a tile
+  constexpr int ND = HD / 16;              // output tiles
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
+  const int col = lane & 15, grp = lane >> 4;
+  StepUnit u;
+  if constexpr (SHARED) {
+    if (!shared_step_unit(a, u)) return;
+  } else {
+    if (!step_unit(a, u)) return;
+  }
+  const int seq = u.seq, kvh = u.kvh, c0 = u.c0, c1 = u.c1;
+  bf16x8 q[NC][NT];
+  int row, head;
+  step_place<SHARED>(a, u, min(col, u.ncol - 1), row, head);
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    load_query<NT>(a, row, head, HD, c / 2 * 64 + 16 * grp + c % 2 * 8, col < u.ncol, q[c]);
+  if constexpr (SHARED) {
+    if (tid < kMaxGroup) use[tid] = paged_len(a.kv, row, a.max_len) >= u.need;
+  }
+
+  const int32_t* table = a.kv.table + (int64_t)seq * a.kv.tstride;
+  const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
+  const uint8_t* kb = (const uint8_t*)a.kv.k + kvh * a.kv.head_stride;
+  const uint8_t* vb = (const uint8_t*)a.kv.v + kvh * a.kv.head_stride;
+  const uint8_t* exps = (lane < 32 ? a.exp.k : a.exp.v) + kvh * a.exp.head_stride;
+  // Lane l holds the page of key l mod 32 of a block (-1: not visible).
+  auto load_page = [&](int t) {
+    const int key = c0 + t * 32 + (lane & 31);
+    int p = -1;
+    if (key < c1) p = table[key >> a.kv.shift];
+    return (unsigned)p < (unsigned)a.kv.limit ? p : -1;
+  };
+  // Rows as they lie in memory; the 8 keys of an aligned group share a page.  Keys that are not
+  // visible read page 0.
+  const int lr = lane / TPR, ld = lane % TPR * 16;
+  u32x4 kr[NV], vr[NV];
+  uint32_t er;  // the byte of key (lane mod 32), of the values in lanes 32 to 63
+  auto load_block = [&](int t, int page) {
+    const int j0 = c0 + t * 32;
+    const int64_t ep = max(page, 0);
+    er = exps[ep * a.exp.stride + ((j0 + (lane & 31)) & pm)];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      int64_t at;
+      if constexpr (RPL == 8) {
+        at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
+             ((j0 + i * RPL) & pm) * HD + (uint32_t)(lr * HD + ld);
+      } else {
+        const int64_t p0 = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride;
+        const int64_t p1 = max(__builtin_amdgcn_readlane(page, i * RPL + 8), 0) * a.kv.stride;
+        at = (lr < 8 ? p0 : p1) + ((j0 + i * RPL + lr) & pm) * HD + ld;
+      }
+      const u32x4 *kp = (const u32x4*)(kb + at), *vp = (const u32x4*)(vb + at);
+      kr[i] = STREAM ? __builtin_nontemporal_load(kp) : *kp;
+      vr[i] = STREAM ? __builtin_nontemporal_load(vp) : *vp;
+    }
+  };
+  f32x4 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f, lh = 0.f;
+  // The upper parts of o wait in LDS, with the maximum of then.
+  f32x4* park = (f32x4*)(smem + L::TILES + wid * L::HBYTES) + lane;
+  float* park_m = (float*)(smem + L::TILES + wid * L::HBYTES + HD * 16 * 4) + lane;
+  auto parked_scale = [&] {
+    const float mh = *park_m;
+    return mh == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mh - m) * a.scale_log2);
+  };
+  char* ktile = smem + wid * L::WBYTES;
+  char* vtile = ktile + L::TBYTES;
+  float* scales = (float*)(vtile + L::TBYTES);  // of the 32 keys, of the 32 values
+  auto row_at = [&](int r) { return r * L::ROW + (r >= 16 ? 128 : 0); };
+  const char* kop = ktile + col * L::ROW + 16 * grp;
+  const int vrow = 4 * grp + (col >> 1 & 3) + (col >= 8 ? 16 : 0);
+  const char* vop = vtile + row_at(vrow) + (col & 1) * 8;
+
+  int page = load_page(wid), next = load_page(wid + kWaves);
+  if (wid < nt) load_block(wid, page);
+  for (int t = wid; t < nt;) {
+    const int te = NT == 3 ? min(nt, t + kStepCarry * kWaves) : nt;
+    for (; t < te; t += kWaves) {
+      const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
+      // (keys that may not be seen weigh 0 x 0, whatever their bytes say)
+      scales[lane] = page >= 0 ? __uint_as_float(er << 23) : 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int at = row_at(i * RPL) + lr * L::ROW + ld;
+        *(u32x4*)(ktile + at) = kr[i];
+        *(u32x4*)(vtile + at) = vr[i];
+      }
+      // the wave's next block (its last one is read again: no branch)
+      const bool more = t + kWaves < nt;
+      const int tn = more ? t + kWaves : t;
+      page = more ? next : page;
+      load_block(tn, page);
+      next = load_page(t + 2 * kWaves);
+      wave_lds_sync();  // the block is in LDS
+      float p[8];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) {
+          const u32x4 w = *(const u32x4*)(kop + kt * L::HALF + c * 32);
+          const bf16x8 k0 = codes_bf16(w[0], w[1]), k1 = codes_bf16(w[2], w[3]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s = mfma16(k0, q[c][n], s);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s = mfma16(k1, q[c + 1][n], s);
+        }
+        const f32x4 by = *(const f32x4*)(scales + kt * 16 + 4 * grp);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[4 * kt + v] = s[v] * by[v];
+      }
+      if (vis != 0xffffffffu) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+          if (!(vis >> (v / 4 * 16 + 4 * grp + v % 4) & 1)) p[v] = -INFINITY;
+      }
+      float mx = p[0];
+#pragma unroll
+      for (int v = 1; v < 8; ++v) mx = fmaxf(mx, p[v]);
+      float other = mx;
+      swap32(mx, other);
+      mx = fmaxf(mx, other);
+      other = mx;
+      swap16(mx, other);
+      mx = fmaxf(mx, other);
+      const float mnew = fmaxf(m, mx);
+      const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+      if (__any(mnew > m)) {
+        const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+        l *= c;
+        lh *= c;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= c;
+      }
+      m = mnew;
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], a.scale_log2, -mref));
+        l += p[v];
+      }
+      carry(lh, l);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const f32x4 by = *(const f32x4*)(scales + 32 + kt * 16 + 4 * grp);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[4 * kt + v] *= by[v];
+      }
+      bf16x8 pt[NT];
+      terms<NT>(p, pt);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const uint2 w = lds_read_tr8(vop + d * 16);
+        const bf16x8 av = codes_bf16(w.x, w.y);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[d] = mfma16(av, pt[n], o[d]);
+      }
+      wave_lds_sync();  // every read of the block is done before the next is written
+    }
+    if (NT == 3 && t < nt) {
+      const bool first = t == wid + kStepCarry * kWaves;
+      const float c = first ? 0.f : parked_scale();
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        f32x4 h = {0.f, 0.f, 0.f, 0.f};
+        if (!first) h = park[d * AIO_WAVE] * c;
+        carry(h, o[d]);
+        park[d * AIO_WAVE] = h;
+      }
+      *park_m = m;
+    }
+  }
+  if (NT == 3 && wid + kStepCarry * kWaves < nt) {
+    const float c = parked_scale();
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] += park[d * AIO_WAVE] * c;
+  }
+  l += lh;
+  l += __shfl_xor(l, 16, AIO_WAVE);
+  l += __shfl_xor(l, 32, AIO_WAVE);
+  if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
+  step_finish<HD, NT, SHARED>(a, u, smem, use, o, m, l);
 }
 
 // ------------------------------------------------------- the rows of prompts
@@ -1283,13 +1553,19 @@ hipError_t launch_rows(const ArgsOf<KEYS == kPaged8, SHARED>& a, const AttnPlan&
 
 template <int HD, int NT, bool Q8, bool SHARED, bool STREAM>
 hipError_t launch_step(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
-  constexpr int lds = StepLds<HD>::BYTES(NT);
-  const auto fn = k_attn_step<HD, NT, STREAM, Q8, SHARED>;
-  const hipError_t e =
-      hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const void* fn;
+  int lds;
+  if constexpr (Q8) {
+    fn = (const void*)k_attn_step8<HD, NT, STREAM, SHARED>;
+    lds = Step8Lds<HD>::BYTES(NT);
+  } else {
+    fn = (const void*)k_attn_step<HD, NT, STREAM, SHARED>;
+    lds = StepLds<HD>::BYTES(NT);
+  }
+  const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fn, dim3((unsigned)p.groups), dim3(kBlock), lds, stream, a);
-  return hipGetLastError();
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel(fn, dim3((unsigned)p.groups), dim3(kBlock), args, (size_t)lds, stream);
 }
 
 template <int HD, int NT, bool Q8, bool SHARED>

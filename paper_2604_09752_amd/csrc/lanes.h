@@ -44,6 +44,15 @@ AIO_DEV uint2 lds_read_tr16(const void* p) {
   return __builtin_bit_cast(uint2, v);
 }
 
+// The same of 8-bit values: lanes 2 e and 2 e + 1 of a group give the addresses of the two
+// halves (8 values each) of row e, and lane i receives column i of the eight rows.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+AIO_DEV uint2 lds_read_tr8(const void* p) {
+  const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+      (__attribute__((address_space(3))) i32x2*)p);
+  return __builtin_bit_cast(uint2, v);
+}
+
 // Device-coherent access for sums that workgroups hand to one another (K slices,
 // attention splits): written through to memory and read past the (per-XCD) L2, so
 // the hand-over needs no fence that writes back or drops a whole L2 (with fences, it

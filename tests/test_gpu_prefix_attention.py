@@ -174,7 +174,7 @@ def test_wide_tiles(q8):
 def test_holes(ql, q8, dtype):
     """Evicted pages in the prefix and behind it."""
     k_len = [400, 420, 390]
-    holes = [(0, 1), (0, 7), (1, 24), (2, 23)]
+    holes = [(0, 1), (0, 7), (1, 24), (2, 24)]  # (the last two behind it)
     p = Grouped(k_len, [(0, 3, 380)], 2, 64, q8=q8, holes=holes)
     q = rows(sum(ql) if ql else 3, 4, 64, dtype)
     out, l = p.run(q, ql)
