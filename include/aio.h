@@ -589,10 +589,15 @@ int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev
                   int64_t head_stride, void* hip_stream);
 
 /* aio_paged_attention over pages of 8-bit codes (an element is exactly a bf16,
- * so nothing is rounded on the way to the products), with the workspace of
- * aio_attn_workspace_bytes.  Errors as aio_paged_attention. */
+ * so nothing is rounded on the way to the products).  Its workspace is
+ * aio_q8_workspace_bytes's.  Errors as aio_paged_attention. */
 int aio_q8_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_attn* a, void* ws_dev,
                      size_t ws_bytes, void* hip_stream);
+
+/* Bytes of workspace that an attention over 8-bit pages takes, as
+ * aio_attn_workspace_bytes. */
+size_t aio_q8_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
+                              int32_t head_dim);
 
 /* Groups of sequences that begin with the same keys (requests behind one
  * template): group g is the sequences cu_seqs[g] .. cu_seqs[g + 1] - 1, whose

@@ -170,6 +170,8 @@ def lib():
         L.aio_q8_attention.argtypes = [vp, vp, vp, vp, sz, vp]
         L.aio_prefix_attention.argtypes = [vp, vp, vp, vp, vp, sz, vp]
         L.aio_q8_prefix_attention.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.aio_q8_workspace_bytes.argtypes = [vp, i32, i32, i32]
+        L.aio_q8_workspace_bytes.restype = sz
         L.aio_prefix_workspace_bytes.argtypes = [vp, vp, i32, i32, i32]
         L.aio_prefix_workspace_bytes.restype = sz
         L.aio_qk_norm_rope.argtypes = [vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp]
@@ -606,8 +608,8 @@ def aio_attn_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: in
     return int(lib().aio_attn_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
 
 
-def _attend(call, at, kv, s, a, n_heads, n_kv_heads, head_dim, device, ws):
-    n = lib().aio_attn_workspace_bytes(s, n_heads, n_kv_heads, head_dim)
+def _attend(call, at, kv, s, a, n_heads, n_kv_heads, head_dim, device, ws, need=None):
+    n = (need or lib().aio_attn_workspace_bytes)(s, n_heads, n_kv_heads, head_dim)
     w = None
     if n:
         ws, w = _workspace(n, ws, device)
@@ -653,7 +655,17 @@ def aio_q8_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_exp: t
     a = _attn(q, out, lse, scale)
     _check_heads(q, hd)
     s = _paged_seqs(lens, table, cu_q, q.shape[0], max_len, page_size)
-    _attend(lib().aio_q8_attention, at, kv, s, a, q.shape[1], kv_heads, hd, q.device, ws)
+    L = lib()
+    _attend(L.aio_q8_attention, at, kv, s, a, q.shape[1], kv_heads, hd, q.device, ws,
+            L.aio_q8_workspace_bytes)
+
+
+def aio_q8_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_heads: int,
+                           n_kv_heads: int, head_dim: int, prompts: bool = False) -> int:
+    """Workspace of an attention over 8-bit pages, as aio_attn_workspace_bytes."""
+    _int32(n_seqs, n_rows, max_len, n_heads, n_kv_heads, head_dim)
+    s = aio_seqs(n_seqs, n_rows, max_len, 16 if prompts else None, None, None, 0, None)
+    return int(lib().aio_q8_workspace_bytes(ctypes.byref(s), n_heads, n_kv_heads, head_dim))
 
 
 def aio_prefix_workspace_bytes(n_seqs: int, n_rows: int, max_len: int, n_groups: int,

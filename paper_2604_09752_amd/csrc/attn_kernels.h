@@ -170,6 +170,8 @@ constexpr int kStepCarry = 32, kRowsCarry = 32;
 //
 // Shared keys are counted in whole tiles, so that a sequence's own keys start at one.
 constexpr int kSharedUnit = 64;
+// Key tiles of prompt rows that a split of a sequence's own keys takes at least.
+constexpr int kOwnPer = 8;
 
 AIO_DEV int bounded(int v, int most) { return min(max(v, 0), most); }
 
@@ -267,7 +269,9 @@ AIO_DEV bool step_unit(const AttnArgs& a, StepUnit& u) {
   return true;
 }
 
-// The same with groups: shared keys first, then every sequence's own.
+// The same with groups, whose rows are taken COLS columns at a time: shared keys first, then every
+// sequence's own.
+template <int COLS>
 AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
   const int b = blockIdx.x, tid = threadIdx.x;
   // (per split of n keys: whole blocks for each of the four waves)
@@ -277,7 +281,7 @@ AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
     const int t = udiv(lin, a.by_hkv);
     u.kvh = lin - t * a.kv.Hkv;
     GroupTile r;
-    if (!find_group_tile<kMaxGroup>(a, t, r)) return false;
+    if (!find_group_tile<COLS>(a, t, r)) return false;
     const int n = shared_keys(a, r.group, r.seq);
     if (n == 0) return false;
     const int chunk = chunk_of(n, a.px.S);
@@ -286,8 +290,8 @@ AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
     u.c0 = split * chunk;
     u.c1 = min(n, u.c0 + chunk);
     u.first = r.first;
-    u.p0 = r.tile * kMaxGroup;
-    u.ncol = min(kMaxGroup, r.count * a.G - u.p0);
+    u.p0 = r.tile * COLS;
+    u.ncol = min(COLS, r.count * a.G - u.p0);
     u.need = n;
     if (u.c0 < n) return true;
     if (tid < u.ncol) {
@@ -331,41 +335,39 @@ AIO_DEV void step_place(const AttnArgs& a, const StepUnit& u, int c, int& row, i
   }
 }
 
-// Joins the waves' states (o and l as sums, m as a score) in LDS ([wave][column][HD + 4] floats),
-// and writes the workgroup's result.
-template <int HD, int NT, bool SHARED>
-AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, char* smem, const bool* use,
-                         const f32x4 (&o)[HD / 16], float m, float l) {
-  __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
-  constexpr int OROW = HD + 4;
-  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
-  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
-  const int col = lane & 15, grp = lane >> 4;
-  __syncthreads();
-  float* om = (float*)smem;
-  if (col < u.ncol) {
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d)
-      *(f32x4*)(om + (wid * kMaxGroup + col) * OROW + d * 16 + 4 * grp) = o[d];
-    if (grp == 0) {
-      wm[wid][col] = m * a.scale_log2;
-      wl[wid][col] = l;
-    }
+// The waves' states of a workgroup in LDS, to be joined: o and l as sums, m in log2 units.
+template <int HD, int COLS>
+struct StepStates {
+  static constexpr int OROW = HD + 4;  // floats of an output row
+  static constexpr int BYTES = kWaves * COLS * (OROW + 2) * 4;
+  float* om;
+  AIO_DEV float* out(int wave, int col) { return om + (wave * COLS + col) * OROW; }
+  AIO_DEV float2& ml(int wave, int col) {
+    return ((float2*)(om + kWaves * COLS * OROW))[wave * COLS + col];
   }
+};
+
+// Joins them and writes the workgroup's result.
+template <int HD, int NT, bool SHARED, int COLS>
+AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, StepStates<HD, COLS> st,
+                         const bool* use) {
   __syncthreads();
-  for (int e = tid; e < u.ncol * HD; e += kBlock) {
+  for (int e = threadIdx.x; e < u.ncol * HD; e += kBlock) {
     const int g = e / HD, d = e % HD;
     if (SHARED && !use[g]) continue;
-    float M = wm[0][g];
+    float2 ml[kWaves];
+    float M = -INFINITY;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wm[w][g]);
+    for (int w = 0; w < kWaves; ++w) {
+      ml[w] = st.ml(w, g);
+      M = fmaxf(M, ml[w].x);
+    }
     float ls = 0.f, os = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float x = wm[w][g];
-      const float c = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M);
-      ls += c * wl[w][g];
-      os += c * om[(w * kMaxGroup + g) * OROW + d];
+      const float c = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
+      ls += c * ml[w].y;
+      os += c * st.out(w, g)[d];
     }
     int row, head;
     step_place<SHARED>(a, u, g, row, head);
@@ -421,7 +423,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   const int col = lane & 15, grp = lane >> 4;
   StepUnit u;
   if constexpr (SHARED) {
-    if (!shared_step_unit(a, u)) return;
+    if (!shared_step_unit<kMaxGroup>(a, u)) return;
   } else {
     if (!step_unit(a, u)) return;
   }
@@ -642,7 +644,7 @@ struct Step8Lds {
   static constexpr int ROW = HD + 16, HALF = 16 * ROW + 128;
   static constexpr int TBYTES = HALF + 16 * ROW;  // of a key or value tile
   static constexpr int WBYTES = 2 * TBYTES + 64 * 4;
-  static constexpr int OBYTES = kWaves * kMaxGroup * (HD + 4) * 4;
+  static constexpr int OBYTES = StepStates<HD, kMaxGroup>::BYTES;
   static constexpr int TILES = kWaves * WBYTES > OBYTES ? kWaves * WBYTES : OBYTES;
   static constexpr int HBYTES = HD * 16 * 4 + AIO_WAVE * 4;
   static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
@@ -663,7 +665,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMore
   const int col = lane & 15, grp = lane >> 4;
   StepUnit u;
   if constexpr (SHARED) {
-    if (!shared_step_unit(a, u)) return;
+    if (!shared_step_unit<kMaxGroup>(a, u)) return;
   } else {
     if (!step_unit(a, u)) return;
   }
@@ -841,7 +843,225 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMore
   l += __shfl_xor(l, 16, AIO_WAVE);
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
-  step_finish<HD, NT, SHARED>(a, u, smem, use, o, m, l);
+  __syncthreads();
+  StepStates<HD, kMaxGroup> st{(float*)smem};
+  if (col < u.ncol) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) *(f32x4*)(st.out(wid, col) + d * 16 + 4 * grp) = o[d];
+    if (grp == 0) st.ml(wid, col) = make_float2(m * a.scale_log2, l);
+  }
+  step_finish<HD, NT, SHARED>(a, u, st, use);
+}
+
+// Groups of more than 16 columns, bf16 queries: 32 columns as 32 x 32 x 16 products, so that a
+// key that a wave has read and stored serves twice as many.  (48 rows of 32 heads on 8 behind 8192
+// keys are 192 columns: at 16 columns, LDS and the caches' lines were two thirds busy.)
+template <int HD, bool Q8>
+struct Step32Lds {
+  // row pitches and tiles as in Step8Lds and RowsLds
+  static constexpr int KROW = Q8 ? HD + 16 : HD * 2 + 16, VROW = Q8 ? HD + 16 : HD * 2 + 64;
+  static constexpr int GAP = Q8 ? 128 : 0;  // between a tile's halves
+  static constexpr int KBYTES = 32 * KROW + GAP, VBYTES = 32 * VROW + GAP;
+  static constexpr int WBYTES = KBYTES + VBYTES + 64 * 4;
+  static constexpr int OBYTES = StepStates<HD, 32>::BYTES;
+  static constexpr int BYTES = kWaves * WBYTES > OBYTES ? kWaves * WBYTES : OBYTES;
+};
+
+template <int HD, bool Q8>
+__global__ __launch_bounds__(kBlock, 2) void k_attn_step32(AttnMoreArgs a) {
+  using L = Step32Lds<HD, Q8>;
+  using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ bool use[32];
+  constexpr int NC = HD / 16;              // k chunks of a score product
+  constexpr int NHB = HD / 32;             // output tiles
+  constexpr int PER = 16 / sizeof(Elem);   // elements of a load
+  constexpr int TPR = HD / PER;            // lanes of a row
+  constexpr int RPL = AIO_WAVE / TPR;      // rows per load: 4 or 8 of one page, 16 of two
+  constexpr int NV = 32 / RPL;             // loads of a tile
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
+  const int col = lane & 31, kh = lane >> 5;
+  StepUnit u;
+  if (!shared_step_unit<32>(a, u)) return;
+  const int c0 = u.c0, c1 = u.c1;
+  bf16x8 q[NC][1];
+  int row, head;
+  step_place<true>(a, u, min(col, u.ncol - 1), row, head);
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    load_query<1>(a, row, head, HD, Q8 ? c / 2 * 32 + 16 * kh + c % 2 * 8 : c * 16 + 8 * kh,
+                  col < u.ncol, q[c]);
+  if (tid < 32) use[tid] = paged_len(a.kv, row, a.max_len) >= u.need;
+
+  const int32_t* table = a.kv.table + (int64_t)u.seq * a.kv.tstride;
+  const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
+  const Elem* kb = (const Elem*)a.kv.k + u.kvh * a.kv.head_stride;
+  const Elem* vb = (const Elem*)a.kv.v + u.kvh * a.kv.head_stride;
+  const uint8_t* exps = nullptr;
+  if constexpr (Q8) exps = (lane < 32 ? a.exp.k : a.exp.v) + u.kvh * a.exp.head_stride;
+  // Lane l holds the page of key l mod 32 of a block (-1: not visible).
+  auto load_page = [&](int t) {
+    const int key = c0 + t * 32 + (lane & 31);
+    int p = -1;
+    if (key < c1) p = table[key >> a.kv.shift];
+    return (unsigned)p < (unsigned)a.kv.limit ? p : -1;
+  };
+  const int lr = lane / TPR, ld = lane % TPR * PER;
+  u32x4 kr[NV], vr[NV];
+  uint32_t er = 0;  // the byte of key (lane mod 32), of the values in lanes 32 to 63
+  auto load_block = [&](int t, int page) {
+    const int j0 = c0 + t * 32;
+    if constexpr (Q8) er = exps[(int64_t)max(page, 0) * a.exp.stride + ((j0 + (lane & 31)) & pm)];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      int64_t at;
+      if constexpr (RPL <= 8) {
+        at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
+             ((j0 + i * RPL) & pm) * HD + (uint32_t)(lr * HD + ld);
+      } else {
+        const int64_t p0 = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride;
+        const int64_t p1 = max(__builtin_amdgcn_readlane(page, i * RPL + 8), 0) * a.kv.stride;
+        at = (lr < 8 ? p0 : p1) + ((j0 + i * RPL + lr) & pm) * HD + ld;
+      }
+      kr[i] = *(const u32x4*)(kb + at);
+      vr[i] = *(const u32x4*)(vb + at);
+    }
+  };
+  f32x16 o[NHB];
+#pragma unroll
+  for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[hb][i] = 0.f;
+  float m = -INFINITY, l = 0.f, lh = 0.f;
+  char* ktile = smem + wid * L::WBYTES;
+  char* vtile = ktile + L::KBYTES;
+  float* scales = (float*)(vtile + L::VBYTES);  // of the 32 keys, of the 32 values
+  const char* kop = ktile + col * L::KROW + (col >= 16 ? L::GAP : 0) + 16 * kh;
+  const char* vop;
+  if constexpr (Q8) {
+    const int r = 4 * kh + (lane >> 1 & 3) + (lane & 8);
+    vop = vtile + r * L::VROW + (lane >> 4 & 1) * 16 + (lane & 1) * 8;
+  } else {
+    vop = vtile + (4 * kh + (lane & 15) / 4) * L::VROW +
+          ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+  }
+  auto value_frag = [&](int c, int hb) {  // chunk of 16 keys, tile of 32 dims
+    if constexpr (Q8) {
+      const uint2 w = lds_read_tr8(vop + c * (16 * L::VROW + L::GAP) + hb * 32);
+      return codes_bf16(w.x, w.y);
+    } else {
+      const char* v = vop + c * 16 * L::VROW + hb * 64;
+      const uint2 v0 = lds_read_tr16(v), v1 = lds_read_tr16(v + 8 * L::VROW);
+      return as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+    }
+  };
+
+  int page = load_page(wid), next = load_page(wid + kWaves);
+  if (wid < nt) load_block(wid, page);
+  for (int t = wid; t < nt; t += kWaves) {
+    const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
+    if constexpr (Q8) scales[lane] = page >= 0 ? __uint_as_float(er << 23) : 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int r = i * RPL + lr, gap = i * RPL >= 16 ? L::GAP : 0;
+      *(u32x4*)(ktile + r * L::KROW + gap + ld * sizeof(Elem)) = kr[i];
+      u32x4 w = vr[i];
+      // (values that may not be seen are zero: 0 x NaN is not; codes are finite)
+      if (!Q8 && vis != 0xffffffffu && !(vis >> r & 1)) w = u32x4{0, 0, 0, 0};
+      *(u32x4*)(vtile + r * L::VROW + gap + ld * sizeof(Elem)) = w;
+    }
+    // the wave's next block (its last one is read again: no branch)
+    const bool more = t + kWaves < nt;
+    page = more ? next : page;
+    load_block(more ? t + kWaves : t, page);
+    next = load_page(t + 2 * kWaves);
+    wave_lds_sync();  // the block is in LDS
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+    if constexpr (Q8) {
+#pragma unroll
+      for (int c = 0; c < NC; c += 2) {
+        const u32x4 w = *(const u32x4*)(kop + c * 16);
+        s = mfma32(codes_bf16(w[0], w[1]), q[c][0], s);
+        s = mfma32(codes_bf16(w[2], w[3]), q[c + 1][0], s);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 by = *(const f32x4*)(scales + 8 * i + 4 * kh);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[4 * i + v] *= by[v];
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        s = mfma32(as_bf16x8(*(const u32x4*)(kop + c * 32)), q[c][0], s);
+    }
+    // score v is that of key 8 (v / 4) + 4 kh + v mod 4
+    if (vis != 0xffffffffu) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (!(vis >> (v / 4 * 8 + 4 * kh + v % 4) & 1)) s[v] = -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    float other = mx;
+    swap32(mx, other);
+    mx = fmaxf(mx, other);
+    const float mnew = fmaxf(m, mx);
+    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+    if (__any(mnew > m)) {
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+      l *= c;
+      lh *= c;
+#pragma unroll
+      for (int hb = 0; hb < NHB; ++hb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[hb][i] *= c;
+    }
+    m = mnew;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, -mref));
+      l += s[v];
+    }
+    carry(lh, l);
+    if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 by = *(const f32x4*)(scales + 32 + 8 * i + 4 * kh);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[4 * i + v] *= by[v];
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = s[8 * c + e];
+      bf16x8 pt[1];
+      terms<1>(p, pt);
+#pragma unroll
+      for (int hb = 0; hb < NHB; ++hb) o[hb] = mfma32(value_frag(c, hb), pt[0], o[hb]);
+    }
+    wave_lds_sync();  // every read of the block is done before the next is written
+  }
+  l += lh;
+  l += __shfl_xor(l, 32, AIO_WAVE);
+  if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
+  __syncthreads();
+  StepStates<HD, 32> st{(float*)smem};
+  if (col < u.ncol) {
+#pragma unroll
+    for (int i = 0; i < 4 * NHB; ++i)
+      *(f32x4*)(st.out(wid, col) + i / 4 * 32 + i % 4 * 8 + 4 * kh) =
+          f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2],
+                o[i / 4][4 * (i % 4) + 3]};
+    if (kh == 0) st.ml(wid, col) = make_float2(m * a.scale_log2, l);
+  }
+  step_finish<HD, 1, true>(a, u, st, use);
 }
 
 // ------------------------------------------------------- the rows of prompts
@@ -970,6 +1190,7 @@ template <int HD, int NT, Keys KEYS, int W, bool SHARED = false>
 __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   using L = RowsLds<HD>;
   constexpr bool PAGED = KEYS != kPacked, Q8 = KEYS == kPaged8;
+  constexpr bool ADAPT = Q8 || SHARED;  // (with what the kernels over bf16 keys have no registers for)
   constexpr int kThreads = W * AIO_WAVE, kRows = W * 32;
   extern __shared__ __align__(16) char smem[];
   __shared__ uint8_t seen[kKeys];
@@ -1035,7 +1256,10 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
   const int all_lim = sees(udiv(p0, a.by_g));
   const int nkt = (wg_lim < 0 ? 0 : wg_lim / kKeys + 1) - key_t0;
   // this split's key tiles
-  const int each = nkt / splits, rest = nkt - each * splits;
+  int used = splits;
+  if constexpr (SHARED)  // (a sequence's own keys: kOwnPer tiles each at least)
+    used = max(1, min(splits, shared ? nkt : (nkt + kOwnPer - 1) / kOwnPer));
+  const int each = nkt / used, rest = nkt - each * used;
   const int t0 = key_t0 + split * each + min(split, rest);
   const int t1 = t0 + each + (split < rest ? 1 : 0);
   // the rows that see all of the shared keys (the others' own workgroups read them)
@@ -1052,6 +1276,14 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
     seq_keys<true>(a, lo, k, there, all);
     takes_part = there >= len && all - n >= len - 1;
   }
+  const int64_t rh = (int64_t)(first + row) * a.H + h0 + g;
+  if (SHARED && split >= used) {  // nothing is left for this split
+    if (live && takes_part && kh == 0)
+      a.part_ml[((int64_t)slot * a.n_rows * a.H + rh) * 2] = -INFINITY;
+    return;
+  }
+  // (a wave without rows only moves tiles)
+  const bool idle = ADAPT && p0 + wid * 32 >= packed;
 
   bf16x8 q[NC][NT];
 #pragma unroll
@@ -1077,14 +1309,18 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
   // all through the loop below: 2048 rows of the 1B behind 1637 keys, bf16, 90 us without a hole,
   // 263 with one.)
   int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
+  bool holes = !ADAPT;  // (of those after them: some may be)
   if constexpr (PAGED) {
     // (not with holes among them)
-    if (tp > t0) {
+    if (ADAPT ? t1 > t0 : tp > t0) {
       bool hole = false;
-      const int e1 = (tp * kKeys - 1) >> a.kv.shift;
+      const int e1 = ((ADAPT ? min(t1 * kKeys, len) : tp * kKeys) - 1) >> a.kv.shift;
       for (int e = (t0 * kKeys >> a.kv.shift) + tid; e <= e1; e += kThreads)
         hole |= (unsigned)table[e] >= (unsigned)a.kv.limit;
-      if (__syncthreads_or(hole)) tp = t0;
+      if (__syncthreads_or(hole)) {
+        tp = t0;
+        holes = true;
+      }
     }
   }
 
@@ -1283,40 +1519,53 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
       load_tile(vr, vb, ve, t0 + 1, pg1);
     }
     __syncthreads();
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sa[b][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 ak = key_frag(0, 2 * c + b);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) sa[b] = mfma32(ak, q[c][n], sa[b]);
+    if (idle) {
+      for (int t = t0; t < tp; ++t) {
+        __syncthreads();
+        store_keys(kr, (t - t0) & 1);
+        store_values(vr, (t - t0 & 1) ^ 1);
+        load_tile(kr, kb, ke, t + 3, pg3);
+        load_tile(vr, vb, ve, t + 2, pg2);
+        pg2 = pg3;
+        pg3 = pg4;
+        pg4 = pages_of(t + 5);
       }
-    }
-    mx = sa[0][0];
+    } else {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sa[b][v]);
-    int t = t0;
-    for (; t + 1 < tp; t += 2) {
-      step(t, std::integral_constant<int, 0>{}, sa, sb);
-      step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
-      carry_out(t + 2 - t0);
+        for (int i = 0; i < 16; ++i) sa[b][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const bf16x8 ak = key_frag(0, 2 * c + b);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) sa[b] = mfma32(ak, q[c][n], sa[b]);
+        }
+      }
+      mx = sa[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sa[b][v]);
+      int t = t0;
+      for (; t + 1 < tp; t += 2) {
+        step(t, std::integral_constant<int, 0>{}, sa, sb);
+        step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
+        carry_out(t + 2 - t0);
+      }
+      if (t < tp) step(t, std::integral_constant<int, 0>{}, sa, sb);
     }
-    if (t < tp) step(t, std::integral_constant<int, 0>{}, sa, sb);
   }
 
   // The other tiles, one after the other: at the causal edge or the keys' end, or with
   // holes.
-  for (int t = tp; t < t1; ++t) {
-    const int j0 = t * kKeys;
-    Row8<Q8> kr[NP], vr[NP];
-    uint32_t ok = 0;  // bit p: the row of pass p is there
+  Row8<Q8> kr[NP], vr[NP];
+  uint32_t ok;  // bit p: the row of pass p is there
+  auto fetch = [&](int t) {
+    ok = 0;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int key = j0 + p * RPP + wr;
+      const int key = t * kKeys + p * RPP + wr;
       bool there = key + lr < len;
       int64_t at = (int64_t)(key0 + key) * a.kv.stride, exp_at = 0;
       if constexpr (PAGED) {
@@ -1337,6 +1586,10 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
         ok |= 1u << p;
       }
     }
+  };
+  for (int t = tp; t < t1; ++t) {
+    const int j0 = t * kKeys;
+    if (!ADAPT || t == tp) fetch(t);
     __syncthreads();  // every wave is done with the tile before
     bool odd = false;
 #pragma unroll
@@ -1370,7 +1623,8 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
       }
       __syncthreads();
     }
-    if (j0 > wave_lim) continue;
+    if (ADAPT && t + 1 < t1) fetch(t + 1);  // (in flight meanwhile)
+    if (j0 > wave_lim || idle) continue;
     f32x16 s[2];
     float mx = -INFINITY;
 #pragma unroll
@@ -1383,12 +1637,27 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
       }
+      if constexpr (!ADAPT) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
-        if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
-        mx = fmaxf(mx, s[b][v]);
+        for (int v = 0; v < 16; ++v) {
+          const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
+          if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
+          mx = fmaxf(mx, s[b][v]);
+        }
       }
+    }
+    if constexpr (ADAPT) {
+      const int edge = lim - j0 - 4 * kh;
+#pragma unroll
+      for (int v = 0; v < 32; ++v)
+        if (v / 16 * 32 + v % 16 / 4 * 8 + v % 4 > edge) s[v / 16][v % 16] = -INFINITY;
+      if (holes) {
+#pragma unroll
+        for (int v = 0; v < 32; ++v)
+          if (!seen[v / 16 * 32 + v % 16 / 4 * 8 + 4 * kh + v % 4]) s[v / 16][v % 16] = -INFINITY;
+      }
+#pragma unroll
+      for (int v = 0; v < 32; ++v) mx = fmaxf(mx, s[v / 16][v % 16]);
     }
     const float mref = refer(mx);
 #pragma unroll
@@ -1424,7 +1693,6 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
   l += lh;
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
-  const int64_t rh = (int64_t)(first + row) * a.H + h0 + g;
   if (SHARED || a.S > 1) {
     if constexpr (SHARED) {
       if (!takes_part) return;
@@ -1553,9 +1821,14 @@ hipError_t launch_rows(const ArgsOf<KEYS == kPaged8, SHARED>& a, const AttnPlan&
 
 template <int HD, int NT, bool Q8, bool SHARED, bool STREAM>
 hipError_t launch_step(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
-  const void* fn;
-  int lds;
-  if constexpr (Q8) {
+  const void* fn = nullptr;
+  int lds = 0;
+  if (p.cols == 32) {
+    if constexpr (SHARED && NT == 1) {
+      fn = (const void*)k_attn_step32<HD, Q8>;
+      lds = Step32Lds<HD, Q8>::BYTES;
+    }
+  } else if constexpr (Q8) {
     fn = (const void*)k_attn_step8<HD, NT, STREAM, SHARED>;
     lds = Step8Lds<HD>::BYTES(NT);
   } else {

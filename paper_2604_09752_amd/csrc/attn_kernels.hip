@@ -5,6 +5,7 @@
 // Workgroups up to which the keys are split.
 constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
 
+
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p,
                   int key_bytes) {
   *p = AttnPlan{};
@@ -38,6 +39,12 @@ int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan
     // four rounds of workgroups, 128 balance better (one prompt of 8192 rows, 32 heads: 594
     // against 564 us; eight of up to 2048, 8 kv heads: 136 against 143)
     p->waves = fp32 || (int64_t)s.n_rows * G / 256 * Hkv < 4 * kCUs ? 4 : 8;
+    // 8-bit keys become bf16 once per workgroup: 256 rows as soon as sequences fill half of them
+    // (six of 600 rows behind 2000 keys, 16 heads on 8: 123 us in tiles of 128, 95 of 256; six of 64 rows
+    // 50 and 46; one of 64 rows 28 and 32).
+    if (key_bytes == 1 && !fp32 && (int64_t)s.n_rows * G >= 128 * (int64_t)s.n_seqs &&
+        (int64_t)s.n_rows * G * Hkv >= 4096)
+      p->waves = 8;
     // (full tiles, and a last one of each sequence that has rows)
     const int64_t full = (int64_t)s.n_rows * G / (32 * p->waves);
     p->tiles = full + std::min(s.n_seqs, s.n_rows);
@@ -73,17 +80,24 @@ int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, in
   px->n = x.n_groups;
   px->max = most_shared;
   // A place for every full tile of the groups' rows, and one more for each group with rows.
-  const int64_t width = p->rows ? 32 * p->waves : kMaxGroup;
+  p->cols = !p->rows && dtype == AIO_BF16 && (int64_t)s.n_rows * G > 16 * (int64_t)x.n_groups ? 32 : 16;
+  const int64_t width = p->rows ? 32 * p->waves : p->cols;
   const int64_t tiles = (int64_t)s.n_rows * G / width + std::min(x.n_groups, s.n_rows);
   auto splits = [](int64_t most, int64_t base, int64_t units) {
     return (int)std::max<int64_t>(1, std::min(units, most / std::max<int64_t>(1, base)));
   };
-  // Both parts fill the GPU by themselves: the shared one starts first, and how much is left to
-  // the others is not known here.
-  const int64_t most = !p->rows ? kStepGroups : dtype == AIO_F32 ? kRowsGroups / 2 : kRowsGroups;
+  const int64_t most = !p->rows ? (p->cols == 32 ? kRowsGroups : kStepGroups) : dtype == AIO_F32 ? kRowsGroups / 2 : kRowsGroups;
   const int64_t unit = p->rows ? kKeys : 128, own = p->rows ? p->tiles : s.n_seqs;
-  px->S = splits(most, tiles * Hkv, (most_shared + unit - 1) / unit);
-  px->own = splits(most, own * Hkv, ((int64_t)s.max_len + unit - 1) / unit);
+  if (p->rows) {
+    // One round of workgroups, the own keys' among them; a sequence's own keys are split from
+    // kOwnPer key tiles on.
+    const int64_t units = ((int64_t)s.max_len + unit - 1) / unit;
+    px->own = splits(most / 2, own * Hkv, (units + kOwnPer - 1) / kOwnPer);
+    px->S = splits(most - std::min(most / 2, own * Hkv), tiles * Hkv, (most_shared + unit - 1) / unit);
+  } else {
+    px->S = splits(most, tiles * Hkv, (most_shared + unit - 1) / unit);
+    px->own = splits(most, own * Hkv, ((int64_t)s.max_len + unit - 1) / unit);
+  }
   const int64_t shared = tiles * Hkv * px->S;
   p->groups = shared + own * Hkv * px->own;
   if (p->groups > (p->waves == 8 ? kMostGroups512 : kMostGroups)) return AIO_ERANGE;

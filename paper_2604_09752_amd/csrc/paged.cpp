@@ -344,16 +344,30 @@ int aio_q8_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_attn* a, 
                    ws_bytes, hip_stream);
 }
 
+size_t aio_q8_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_heads,
+                              int32_t head_dim) {
+  if (!s) return 0;
+  size_t most = 0;
+  for (const int dtype : {AIO_F32, AIO_BF16}) {
+    AttnPlan p;
+    if (aio_attn_plan(*s, n_heads, n_kv_heads, head_dim, dtype, &p, 1) == AIO_OK)
+      most = std::max(most, p.ws);
+  }
+  return most;
+}
+
 size_t aio_prefix_workspace_bytes(const aio_seqs* s, const aio_prefixes* x, int32_t n_heads,
                                   int32_t n_kv_heads, int32_t head_dim) {
   if (!s || !x) return 0;
   size_t most = 0;
-  for (const int dtype : {AIO_F32, AIO_BF16}) {
-    AttnPlan p;
-    PrefixArgs px;
-    if (aio_groups_plan(*s, *x, n_heads, n_kv_heads, head_dim, dtype, &p, &px) == AIO_OK)
-      most = std::max(most, p.ws);
-  }
+  for (const int dtype : {AIO_F32, AIO_BF16})
+    for (const int key_bytes : {1, 2}) {
+      AttnPlan p;
+      PrefixArgs px;
+      if (aio_groups_plan(*s, *x, n_heads, n_kv_heads, head_dim, dtype, &p, &px, key_bytes) ==
+          AIO_OK)
+        most = std::max(most, p.ws);
+    }
   return most;
 }
 

@@ -257,9 +257,9 @@ def test_captured_and_replayed():
     lens = [600, 1700]
     pool = Q8Pool(PoolCase(lens, 2, 64, 16))
     k, v, ke, ve, ln, table = pool.device()
-    need = B.aio_attn_workspace_bytes(2, 2, 1700, 4, 2, 64)
+    need = B.aio_q8_workspace_bytes(2, 2, 1700, 4, 2, 64)
     assert need > 0
-    ws = torch.full((max(need, B.aio_attn_workspace_bytes(2, 34, 1700, 4, 2, 64, prompts=True)),),
+    ws = torch.full((max(need, B.aio_q8_workspace_bytes(2, 34, 1700, 4, 2, 64, prompts=True)),),
                     255, dtype=torch.uint8, device="cuda")
     q, ql = rows(2, 4, 64, F32).cuda(), [9, 25]
     pq = rows(sum(ql), 4, 64, BF16).cuda()
