@@ -135,6 +135,16 @@ AIO_DEV void store_out(const AttnArgs& a, bool f32, int64_t at, float v) {
   else ((uint16_t*)a.out)[at] = f32_to_bf16(v);
 }
 
+AIO_DEV void store_out4(const AttnArgs& a, bool f32, int64_t at, f32x4 v) {
+  if (f32) {
+    *(f32x4*)((float*)a.out + at) = v;
+  } else {
+    const uint2 w = {f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16,
+                     f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
+    *(uint2*)((uint16_t*)a.out + at) = w;
+  }
+}
+
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // A long sum in two floats: hi becomes the rounded hi + lo, lo what that is off by (exactly
@@ -352,8 +362,8 @@ template <int HD, int NT, bool SHARED, int COLS>
 AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, StepStates<HD, COLS> st,
                          const bool* use) {
   __syncthreads();
-  for (int e = threadIdx.x; e < u.ncol * HD; e += kBlock) {
-    const int g = e / HD, d = e % HD;
+  for (int e = threadIdx.x; e < u.ncol * (HD / 4); e += kBlock) {
+    const int g = e / (HD / 4), d = e % (HD / 4) * 4;
     if (SHARED && !use[g]) continue;
     float2 ml[kWaves];
     float M = -INFINITY;
@@ -362,23 +372,25 @@ AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, StepStates<HD, CO
       ml[w] = st.ml(w, g);
       M = fmaxf(M, ml[w].x);
     }
-    float ls = 0.f, os = 0.f;
+    float ls = 0.f;
+    f32x4 os = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float c = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
       ls += c * ml[w].y;
-      os += c * st.out(w, g)[d];
+      os += c * *(const f32x4*)(st.out(w, g) + d);
     }
     int row, head;
     step_place<SHARED>(a, u, g, row, head);
     const int64_t rh = (int64_t)row * a.H + head;
     if (!SHARED && a.S == 1) {
       const bool none = ls == 0.f;  // no visible key
-      store_out(a, NT == 3, (int64_t)row * a.ldo + (int64_t)head * HD + d, none ? 0.f : os / ls);
+      store_out4(a, NT == 3, (int64_t)row * a.ldo + (int64_t)head * HD + d,
+                 none ? f32x4{0.f, 0.f, 0.f, 0.f} : os / ls);
       if (d == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
     } else {
       const int64_t at = (int64_t)u.slot * a.n_rows * a.H + rh;
-      a.part_o[at * HD + d] = os;
+      *(f32x4*)(a.part_o + at * HD + d) = os;
       if (d == 0) {
         a.part_ml[at * 2] = ls != ls ? ls : M;
         a.part_ml[at * 2 + 1] = ls;
@@ -1800,6 +1812,63 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
 }
 
+// The same with 8 elements of a row and head per lane and everything of 8 splits requested at
+// once, places without keys among it: one trip to memory where k_attn_join makes two, and
+// a quarter of the waves (400 rows of 16 heads of 128, 11 splits: 8.0 us, so XXX).
+template <int HD, bool F32>
+__global__ __launch_bounds__(kBlock) void k_attn_join8(AttnArgs a) {
+  constexpr int LANES = HD / 8, B = 8;
+  const int rh = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES, d0 = threadIdx.x % LANES * 8;
+  const int all = a.n_rows * a.H;  // (below 2^31)
+  if (rh >= all) return;
+  const int row = rh / a.H, head = rh - row * a.H;
+  // rows of no sequence are left alone
+  if (a.cu_q && (row < a.cu_q[0] || row >= a.cu_q[a.n_seqs])) return;
+  float os[8] = {}, oh[8] = {}, ls = 0.f, M = -INFINITY;
+  for (int s0 = 0; s0 < a.S; s0 += B) {
+    float2 ml[B];
+    f32x4 v[B][2];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int64_t at = (int64_t)min(s0 + b, a.S - 1) * all + rh;
+      ml[b] = *(const float2*)(a.part_ml + at * 2);
+      v[b][0] = *(const f32x4*)(a.part_o + at * HD + d0);
+      v[b][1] = *(const f32x4*)(a.part_o + at * HD + d0 + 4);
+    }
+    float top = M;
+#pragma unroll
+    for (int b = 0; b < B; ++b) top = fmaxf(top, ml[b].x);  // (the last split's, once more)
+    const float c = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    M = top;
+    ls *= c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      os[i] *= c;
+      oh[i] *= c;
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      // (without keys, the place holds anything)
+      if (s0 + b >= a.S || ml[b].x == -INFINITY) continue;
+      const float w = __builtin_amdgcn_exp2f(ml[b].x - ref);
+      ls += w * ml[b].y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) os[i] += w * v[b][i / 4][i % 4];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) carry(oh[i], os[i]);
+  }
+  const bool none = ls == 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) os[i] = none ? 0.f : (oh[i] + os[i]) / ls;
+  const int64_t at = (int64_t)row * a.ldo + (int64_t)head * HD + d0;
+#pragma unroll
+  for (int i = 0; i < 8; i += 4)
+    store_out4(a, F32, at + i, f32x4{os[i], os[i + 1], os[i + 2], os[i + 3]});
+  if (d0 == 0 && a.lse) a.lse[rh] = none ? -INFINITY : M * kLn2 + logf(ls);
+}
+
 template <int HD, int NT, Keys KEYS, bool SHARED, int W>
 hipError_t launch_rows_w(const ArgsOf<KEYS == kPaged8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
   constexpr int lds = RowsLds<HD>::BYTES(NT, W);
@@ -1857,8 +1926,14 @@ hipError_t launch(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t st
   }
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t rh = (int64_t)a.n_rows * a.H;
-  hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
-                     dim3(kBlock), 0, stream, a);
+  if constexpr (Q8 || SHARED) {
+    constexpr int per = kBlock / (HD / 8);
+    hipLaunchKernelGGL((k_attn_join8<HD, NT == 3>), dim3((unsigned)((rh + per - 1) / per)),
+                       dim3(kBlock), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
+                       dim3(kBlock), 0, stream, a);
+  }
   return hipGetLastError();
 }
 
