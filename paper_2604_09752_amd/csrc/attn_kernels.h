@@ -279,9 +279,7 @@ AIO_DEV bool step_unit(const AttnArgs& a, StepUnit& u) {
   return true;
 }
 
-// The same with groups, whose rows are taken COLS columns at a time: shared keys first, then every
-// sequence's own.
-template <int COLS>
+// The same with groups: shared keys first, then every sequence's own.
 AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
   const int b = blockIdx.x, tid = threadIdx.x;
   // (per split of n keys: whole blocks for each of the four waves)
@@ -291,7 +289,7 @@ AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
     const int t = udiv(lin, a.by_hkv);
     u.kvh = lin - t * a.kv.Hkv;
     GroupTile r;
-    if (!find_group_tile<COLS>(a, t, r)) return false;
+    if (!find_group_tile<kMaxGroup>(a, t, r)) return false;
     const int n = shared_keys(a, r.group, r.seq);
     if (n == 0) return false;
     const int chunk = chunk_of(n, a.px.S);
@@ -300,8 +298,8 @@ AIO_DEV bool shared_step_unit(const AttnMoreArgs& a, StepUnit& u) {
     u.c0 = split * chunk;
     u.c1 = min(n, u.c0 + chunk);
     u.first = r.first;
-    u.p0 = r.tile * COLS;
-    u.ncol = min(COLS, r.count * a.G - u.p0);
+    u.p0 = r.tile * kMaxGroup;
+    u.ncol = min(kMaxGroup, r.count * a.G - u.p0);
     u.need = n;
     if (u.c0 < n) return true;
     if (tid < u.ncol) {
@@ -346,20 +344,20 @@ AIO_DEV void step_place(const AttnArgs& a, const StepUnit& u, int c, int& row, i
 }
 
 // The waves' states of a workgroup in LDS, to be joined: o and l as sums, m in log2 units.
-template <int HD, int COLS>
+template <int HD>
 struct StepStates {
   static constexpr int OROW = HD + 4;  // floats of an output row
-  static constexpr int BYTES = kWaves * COLS * (OROW + 2) * 4;
+  static constexpr int BYTES = kWaves * kMaxGroup * (OROW + 2) * 4;
   float* om;
-  AIO_DEV float* out(int wave, int col) { return om + (wave * COLS + col) * OROW; }
+  AIO_DEV float* out(int wave, int col) { return om + (wave * kMaxGroup + col) * OROW; }
   AIO_DEV float2& ml(int wave, int col) {
-    return ((float2*)(om + kWaves * COLS * OROW))[wave * COLS + col];
+    return ((float2*)(om + kWaves * kMaxGroup * OROW))[wave * kMaxGroup + col];
   }
 };
 
 // Joins them and writes the workgroup's result.
-template <int HD, int NT, bool SHARED, int COLS>
-AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, StepStates<HD, COLS> st,
+template <int HD, int NT, bool SHARED>
+AIO_DEV void step_finish(const AttnArgs& a, const StepUnit& u, StepStates<HD> st,
                          const bool* use) {
   __syncthreads();
   for (int e = threadIdx.x; e < u.ncol * (HD / 4); e += kBlock) {
@@ -419,9 +417,8 @@ struct StepLds {
   static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
 };
 
-template <int HD, int NT, bool STREAM, bool SHARED = false>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(
-    ArgsOf<false, SHARED> a) {
+template <int HD, int NT, bool STREAM, bool SHARED>
+AIO_DEV void attn_step(ArgsOf<false, SHARED> a) {
   using L = StepLds<HD>;
   extern __shared__ __align__(16) char smem[];
   __shared__ float wm[kWaves][kMaxGroup], wl[kWaves][kMaxGroup];
@@ -435,7 +432,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   const int col = lane & 15, grp = lane >> 4;
   StepUnit u;
   if constexpr (SHARED) {
-    if (!shared_step_unit<kMaxGroup>(a, u)) return;
+    if (!shared_step_unit(a, u)) return;
   } else {
     if (!step_unit(a, u)) return;
   }
@@ -644,6 +641,12 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
   }
 }
 
+template <int HD, int NT, bool STREAM, bool SHARED = false>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn_step(
+    ArgsOf<false, SHARED> a) {
+  attn_step<HD, NT, STREAM, SHARED>(a);
+}
+
 // The same over pages of 8-bit codes.  Codes stay codes as far as LDS: a wave stores a block's
 // rows and the rows' powers of two, reads the keys as operands (a lane's eight codes of
 // a k chunk are eight neighbours of its row: the queries' chunks are taken alike) and the values
@@ -656,14 +659,14 @@ struct Step8Lds {
   static constexpr int ROW = HD + 16, HALF = 16 * ROW + 128;
   static constexpr int TBYTES = HALF + 16 * ROW;  // of a key or value tile
   static constexpr int WBYTES = 2 * TBYTES + 64 * 4;
-  static constexpr int OBYTES = StepStates<HD, kMaxGroup>::BYTES;
+  static constexpr int OBYTES = StepStates<HD>::BYTES;
   static constexpr int TILES = kWaves * WBYTES > OBYTES ? kWaves * WBYTES : OBYTES;
   static constexpr int HBYTES = HD * 16 * 4 + AIO_WAVE * 4;
   static constexpr int BYTES(int NT) { return TILES + (NT == 3 ? kWaves * HBYTES : 0); }
 };
 
-template <int HD, int NT, bool STREAM, bool SHARED = false>
-__global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMoreArgs a) {
+template <int HD, int NT, bool STREAM, bool SHARED>
+AIO_DEV void attn_step8(AttnMoreArgs a) {
   using L = Step8Lds<HD>;
   extern __shared__ __align__(16) char smem[];
   __shared__ bool use[kMaxGroup];
@@ -677,7 +680,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMore
   const int col = lane & 15, grp = lane >> 4;
   StepUnit u;
   if constexpr (SHARED) {
-    if (!shared_step_unit<kMaxGroup>(a, u)) return;
+    if (!shared_step_unit(a, u)) return;
   } else {
     if (!step_unit(a, u)) return;
   }
@@ -856,7 +859,7 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMore
   l += __shfl_xor(l, 32, AIO_WAVE);
   if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
   __syncthreads();
-  StepStates<HD, kMaxGroup> st{(float*)smem};
+  StepStates<HD> st{(float*)smem};
   if (col < u.ncol) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) *(f32x4*)(st.out(wid, col) + d * 16 + 4 * grp) = o[d];
@@ -865,215 +868,9 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMore
   step_finish<HD, NT, SHARED>(a, u, st, use);
 }
 
-// Groups of more than 16 columns, bf16 queries: 32 columns as 32 x 32 x 16 products, so that a
-// key that a wave has read and stored serves twice as many.  (48 rows of 32 heads on 8 behind 8192
-// keys are 192 columns: at 16 columns, LDS and the caches' lines were two thirds busy.)
-template <int HD, bool Q8>
-struct Step32Lds {
-  // row pitches and tiles as in Step8Lds and RowsLds
-  static constexpr int KROW = Q8 ? HD + 16 : HD * 2 + 16, VROW = Q8 ? HD + 16 : HD * 2 + 64;
-  static constexpr int GAP = Q8 ? 128 : 0;  // between a tile's halves
-  static constexpr int KBYTES = 32 * KROW + GAP, VBYTES = 32 * VROW + GAP;
-  static constexpr int WBYTES = KBYTES + VBYTES + 64 * 4;
-  static constexpr int OBYTES = StepStates<HD, 32>::BYTES;
-  static constexpr int BYTES = kWaves * WBYTES > OBYTES ? kWaves * WBYTES : OBYTES;
-};
-
-template <int HD, bool Q8>
-__global__ __launch_bounds__(kBlock, 2) void k_attn_step32(AttnMoreArgs a) {
-  using L = Step32Lds<HD, Q8>;
-  using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
-  extern __shared__ __align__(16) char smem[];
-  __shared__ bool use[32];
-  constexpr int NC = HD / 16;              // k chunks of a score product
-  constexpr int NHB = HD / 32;             // output tiles
-  constexpr int PER = 16 / sizeof(Elem);   // elements of a load
-  constexpr int TPR = HD / PER;            // lanes of a row
-  constexpr int RPL = AIO_WAVE / TPR;      // rows per load: 4 or 8 of one page, 16 of two
-  constexpr int NV = 32 / RPL;             // loads of a tile
-  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
-  const int wid = __builtin_amdgcn_readfirstlane(tid / AIO_WAVE);
-  const int col = lane & 31, kh = lane >> 5;
-  StepUnit u;
-  if (!shared_step_unit<32>(a, u)) return;
-  const int c0 = u.c0, c1 = u.c1;
-  bf16x8 q[NC][1];
-  int row, head;
-  step_place<true>(a, u, min(col, u.ncol - 1), row, head);
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-    load_query<1>(a, row, head, HD, Q8 ? c / 2 * 32 + 16 * kh + c % 2 * 8 : c * 16 + 8 * kh,
-                  col < u.ncol, q[c]);
-  if (tid < 32) use[tid] = paged_len(a.kv, row, a.max_len) >= u.need;
-
-  const int32_t* table = a.kv.table + (int64_t)u.seq * a.kv.tstride;
-  const int nt = (c1 - c0 + 31) / 32, pm = (1 << a.kv.shift) - 1;
-  const Elem* kb = (const Elem*)a.kv.k + u.kvh * a.kv.head_stride;
-  const Elem* vb = (const Elem*)a.kv.v + u.kvh * a.kv.head_stride;
-  const uint8_t* exps = nullptr;
-  if constexpr (Q8) exps = (lane < 32 ? a.exp.k : a.exp.v) + u.kvh * a.exp.head_stride;
-  // Lane l holds the page of key l mod 32 of a block (-1: not visible).
-  auto load_page = [&](int t) {
-    const int key = c0 + t * 32 + (lane & 31);
-    int p = -1;
-    if (key < c1) p = table[key >> a.kv.shift];
-    return (unsigned)p < (unsigned)a.kv.limit ? p : -1;
-  };
-  const int lr = lane / TPR, ld = lane % TPR * PER;
-  u32x4 kr[NV], vr[NV];
-  uint32_t er = 0;  // the byte of key (lane mod 32), of the values in lanes 32 to 63
-  auto load_block = [&](int t, int page) {
-    const int j0 = c0 + t * 32;
-    if constexpr (Q8) er = exps[(int64_t)max(page, 0) * a.exp.stride + ((j0 + (lane & 31)) & pm)];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      int64_t at;
-      if constexpr (RPL <= 8) {
-        at = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride +
-             ((j0 + i * RPL) & pm) * HD + (uint32_t)(lr * HD + ld);
-      } else {
-        const int64_t p0 = max(__builtin_amdgcn_readlane(page, i * RPL), 0) * a.kv.stride;
-        const int64_t p1 = max(__builtin_amdgcn_readlane(page, i * RPL + 8), 0) * a.kv.stride;
-        at = (lr < 8 ? p0 : p1) + ((j0 + i * RPL + lr) & pm) * HD + ld;
-      }
-      kr[i] = *(const u32x4*)(kb + at);
-      vr[i] = *(const u32x4*)(vb + at);
-    }
-  };
-  f32x16 o[NHB];
-#pragma unroll
-  for (int hb = 0; hb < NHB; ++hb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[hb][i] = 0.f;
-  float m = -INFINITY, l = 0.f, lh = 0.f;
-  char* ktile = smem + wid * L::WBYTES;
-  char* vtile = ktile + L::KBYTES;
-  float* scales = (float*)(vtile + L::VBYTES);  // of the 32 keys, of the 32 values
-  const char* kop = ktile + col * L::KROW + (col >= 16 ? L::GAP : 0) + 16 * kh;
-  const char* vop;
-  if constexpr (Q8) {
-    const int r = 4 * kh + (lane >> 1 & 3) + (lane & 8);
-    vop = vtile + r * L::VROW + (lane >> 4 & 1) * 16 + (lane & 1) * 8;
-  } else {
-    vop = vtile + (4 * kh + (lane & 15) / 4) * L::VROW +
-          ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
-  }
-  auto value_frag = [&](int c, int hb) {  // chunk of 16 keys, tile of 32 dims
-    if constexpr (Q8) {
-      const uint2 w = lds_read_tr8(vop + c * (16 * L::VROW + L::GAP) + hb * 32);
-      return codes_bf16(w.x, w.y);
-    } else {
-      const char* v = vop + c * 16 * L::VROW + hb * 64;
-      const uint2 v0 = lds_read_tr16(v), v1 = lds_read_tr16(v + 8 * L::VROW);
-      return as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
-    }
-  };
-
-  int page = load_page(wid), next = load_page(wid + kWaves);
-  if (wid < nt) load_block(wid, page);
-  for (int t = wid; t < nt; t += kWaves) {
-    const uint32_t vis = (uint32_t)__ballot(page >= 0);  // bit j: key j of the block
-    if constexpr (Q8) scales[lane] = page >= 0 ? __uint_as_float(er << 23) : 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int r = i * RPL + lr, gap = i * RPL >= 16 ? L::GAP : 0;
-      *(u32x4*)(ktile + r * L::KROW + gap + ld * sizeof(Elem)) = kr[i];
-      u32x4 w = vr[i];
-      // (values that may not be seen are zero: 0 x NaN is not; codes are finite)
-      if (!Q8 && vis != 0xffffffffu && !(vis >> r & 1)) w = u32x4{0, 0, 0, 0};
-      *(u32x4*)(vtile + r * L::VROW + gap + ld * sizeof(Elem)) = w;
-    }
-    // the wave's next block (its last one is read again: no branch)
-    const bool more = t + kWaves < nt;
-    page = more ? next : page;
-    load_block(more ? t + kWaves : t, page);
-    next = load_page(t + 2 * kWaves);
-    wave_lds_sync();  // the block is in LDS
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
-    if constexpr (Q8) {
-#pragma unroll
-      for (int c = 0; c < NC; c += 2) {
-        const u32x4 w = *(const u32x4*)(kop + c * 16);
-        s = mfma32(codes_bf16(w[0], w[1]), q[c][0], s);
-        s = mfma32(codes_bf16(w[2], w[3]), q[c + 1][0], s);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 by = *(const f32x4*)(scales + 8 * i + 4 * kh);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s[4 * i + v] *= by[v];
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        s = mfma32(as_bf16x8(*(const u32x4*)(kop + c * 32)), q[c][0], s);
-    }
-    // score v is that of key 8 (v / 4) + 4 kh + v mod 4
-    if (vis != 0xffffffffu) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (!(vis >> (v / 4 * 8 + 4 * kh + v % 4) & 1)) s[v] = -INFINITY;
-    }
-    float mx = s[0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    float other = mx;
-    swap32(mx, other);
-    mx = fmaxf(mx, other);
-    const float mnew = fmaxf(m, mx);
-    const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
-    if (__any(mnew > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
-      l *= c;
-      lh *= c;
-#pragma unroll
-      for (int hb = 0; hb < NHB; ++hb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[hb][i] *= c;
-    }
-    m = mnew;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, -mref));
-      l += s[v];
-    }
-    carry(lh, l);
-    if constexpr (Q8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 by = *(const f32x4*)(scales + 32 + 8 * i + 4 * kh);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s[4 * i + v] *= by[v];
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[8 * c + e];
-      bf16x8 pt[1];
-      terms<1>(p, pt);
-#pragma unroll
-      for (int hb = 0; hb < NHB; ++hb) o[hb] = mfma32(value_frag(c, hb), pt[0], o[hb]);
-    }
-    wave_lds_sync();  // every read of the block is done before the next is written
-  }
-  l += lh;
-  l += __shfl_xor(l, 32, AIO_WAVE);
-  if (l != l) m = l;  // (the maximum passes over a NaN, the states' join must not)
-  __syncthreads();
-  StepStates<HD, 32> st{(float*)smem};
-  if (col < u.ncol) {
-#pragma unroll
-    for (int i = 0; i < 4 * NHB; ++i)
-      *(f32x4*)(st.out(wid, col) + i / 4 * 32 + i % 4 * 8 + 4 * kh) =
-          f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2],
-                o[i / 4][4 * (i % 4) + 3]};
-    if (kh == 0) st.ml(wid, col) = make_float2(m * a.scale_log2, l);
-  }
-  step_finish<HD, 1, true>(a, u, st, use);
+template <int HD, int NT, bool STREAM, bool SHARED = false>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 4 : 2) void k_attn_step8(AttnMoreArgs a) {
+  attn_step8<HD, NT, STREAM, SHARED>(a);
 }
 
 // ------------------------------------------------------- the rows of prompts
@@ -1198,8 +995,8 @@ constexpr float kSlack = 8.f;
 // Products by which LDS reads run ahead of their use.
 constexpr int kAhead = 4;
 
-template <int HD, int NT, Keys KEYS, int W, bool SHARED = false>
-__global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
+template <int HD, int NT, Keys KEYS, int W, bool SHARED>
+AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   using L = RowsLds<HD>;
   constexpr bool PAGED = KEYS != kPacked, Q8 = KEYS == kPaged8;
   constexpr bool ADAPT = Q8 || SHARED;  // (with what the kernels over bf16 keys have no registers for)
@@ -1277,7 +1074,11 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
   // the rows that see all of the shared keys (the others' own workgroups read them)
   bool takes_part = true;
   if (shared && live) {
-    int lo = of.seq, hi = of.end;  // this row's sequence
+    int lo = first + row, hi = lo + 1;  // this row's sequence
+    if (a.cu_q) {
+      lo = of.seq;
+      hi = of.end;
+    }
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if (a.cu_q[mid] <= first + row) lo = mid;
@@ -1321,7 +1122,7 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
   // all through the loop below: 2048 rows of the 1B behind 1637 keys, bf16, 90 us without a hole,
   // 263 with one.)
   int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
-  bool holes = !ADAPT;  // (of those after them: some may be)
+  bool holes = PAGED && !ADAPT;  // (of those after them: some may be)
   if constexpr (PAGED) {
     // (not with holes among them)
     if (ADAPT ? t1 > t0 : tp > t0) {
@@ -1649,28 +1450,18 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[b] = mfma32(ak, q[c][n], s[b]);
       }
-      if constexpr (!ADAPT) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int kk = 32 * b + 8 * (v / 4) + 4 * kh + v % 4;
-          if (j0 + kk > lim || !seen[kk]) s[b][v] = -INFINITY;
-          mx = fmaxf(mx, s[b][v]);
-        }
-      }
     }
-    if constexpr (ADAPT) {
-      const int edge = lim - j0 - 4 * kh;
+    const int edge = lim - j0 - 4 * kh;
+#pragma unroll
+    for (int v = 0; v < 32; ++v)
+      if (v / 16 * 32 + v % 16 / 4 * 8 + v % 4 > edge) s[v / 16][v % 16] = -INFINITY;
+    if (holes) {
 #pragma unroll
       for (int v = 0; v < 32; ++v)
-        if (v / 16 * 32 + v % 16 / 4 * 8 + v % 4 > edge) s[v / 16][v % 16] = -INFINITY;
-      if (holes) {
-#pragma unroll
-        for (int v = 0; v < 32; ++v)
-          if (!seen[v / 16 * 32 + v % 16 / 4 * 8 + 4 * kh + v % 4]) s[v / 16][v % 16] = -INFINITY;
-      }
-#pragma unroll
-      for (int v = 0; v < 32; ++v) mx = fmaxf(mx, s[v / 16][v % 16]);
+        if (!seen[v / 16 * 32 + v % 16 / 4 * 8 + 4 * kh + v % 4]) s[v / 16][v % 16] = -INFINITY;
     }
+#pragma unroll
+    for (int v = 0; v < 32; ++v) mx = fmaxf(mx, s[v / 16][v % 16]);
     const float mref = refer(mx);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -1748,6 +1539,27 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(Arg
     }
 }
 
+template <int HD, int NT, Keys KEYS, int W, bool SHARED = false>
+__global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(
+    ArgsOf<KEYS == kPaged8, SHARED> a) {
+  attn_rows<HD, NT, KEYS, W, SHARED>(a);
+}
+
+// One new token of each sequence in groups of many columns: shared keys as the rows of a prompt,
+// 128 columns for a key that is staged once, every sequence's own keys as a step.
+template <int HD, int NT, bool Q8>
+struct WideLds {
+  static constexpr int ROWS = RowsLds<HD>::BYTES(NT, kWaves);
+  static constexpr int STEP = Q8 ? Step8Lds<HD>::BYTES(NT) : StepLds<HD>::BYTES(NT);
+  static constexpr int BYTES = ROWS > STEP ? ROWS : STEP;
+};
+template <int HD, int NT, bool Q8>
+__global__ __launch_bounds__(kBlock, NT == 1 ? 2 : 1) void k_attn_wide(AttnMoreArgs a) {
+  if ((int)blockIdx.x < a.px.groups) attn_rows<HD, NT, Q8 ? kPaged8 : kPaged, kWaves, true>(a);
+  else if constexpr (Q8) attn_step8<HD, NT, false, true>(a);
+  else attn_step<HD, NT, false, true>(a);
+}
+
 // Joins the splits of a row and head: one wave each.  4 to 5 us behind its attention
 // (launch and two dependent reads), whatever the sizes here.
 template <int HD, bool F32>
@@ -1814,23 +1626,25 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
 
 // The same with 8 elements of a row and head per lane and everything of 8 splits requested at
 // once, places without keys among it: one trip to memory where k_attn_join makes two, and
-// a quarter of the waves (400 rows of 16 heads of 128, 11 splits: 8.0 us, so XXX).
-template <int HD, bool F32>
+// a quarter of the waves (400 rows of 16 heads of 128, 7 splits: 8.0 -> 6.4 us).  SPL lanes share
+// the splits of 8 elements: many splits of few rows (48 rows of 32 heads, 17 splits: XXX).
+template <int HD, bool F32, int SPL>
 __global__ __launch_bounds__(kBlock) void k_attn_join8(AttnArgs a) {
-  constexpr int LANES = HD / 8, B = 8;
-  const int rh = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES, d0 = threadIdx.x % LANES * 8;
+  constexpr int LANES = HD / 8 * SPL, B = 8;
+  const int rh = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES;
+  const int d0 = threadIdx.x % (HD / 8) * 8, part = threadIdx.x % LANES / (HD / 8);
   const int all = a.n_rows * a.H;  // (below 2^31)
   if (rh >= all) return;
   const int row = rh / a.H, head = rh - row * a.H;
   // rows of no sequence are left alone
   if (a.cu_q && (row < a.cu_q[0] || row >= a.cu_q[a.n_seqs])) return;
   float os[8] = {}, oh[8] = {}, ls = 0.f, M = -INFINITY;
-  for (int s0 = 0; s0 < a.S; s0 += B) {
+  for (int s0 = part; s0 < a.S; s0 += B * SPL) {
     float2 ml[B];
     f32x4 v[B][2];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-      const int64_t at = (int64_t)min(s0 + b, a.S - 1) * all + rh;
+      const int64_t at = (int64_t)min(s0 + b * SPL, a.S - 1) * all + rh;
       ml[b] = *(const float2*)(a.part_ml + at * 2);
       v[b][0] = *(const f32x4*)(a.part_o + at * HD + d0);
       v[b][1] = *(const f32x4*)(a.part_o + at * HD + d0 + 4);
@@ -1850,7 +1664,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join8(AttnArgs a) {
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       // (without keys, the place holds anything)
-      if (s0 + b >= a.S || ml[b].x == -INFINITY) continue;
+      if (s0 + b * SPL >= a.S || ml[b].x == -INFINITY) continue;
       const float w = __builtin_amdgcn_exp2f(ml[b].x - ref);
       ls += w * ml[b].y;
 #pragma unroll
@@ -1859,6 +1673,20 @@ __global__ __launch_bounds__(kBlock) void k_attn_join8(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) carry(oh[i], os[i]);
   }
+#pragma unroll
+  for (int off = HD / 8; off < LANES; off *= 2) {
+    const float M2 = __shfl_xor(M, off, AIO_WAVE), top = fmaxf(M, M2);
+    const float c = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+    const float c2 = M2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M2 - top);
+    M = top;
+    ls = c * ls + c2 * __shfl_xor(ls, off, AIO_WAVE);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      os[i] = c * os[i] + c2 * __shfl_xor(os[i], off, AIO_WAVE);
+      oh[i] = c * oh[i] + c2 * __shfl_xor(oh[i], off, AIO_WAVE);
+    }
+  }
+  if (part) return;
   const bool none = ls == 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) os[i] = none ? 0.f : (oh[i] + os[i]) / ls;
@@ -1892,10 +1720,10 @@ template <int HD, int NT, bool Q8, bool SHARED, bool STREAM>
 hipError_t launch_step(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t stream) {
   const void* fn = nullptr;
   int lds = 0;
-  if (p.cols == 32) {
+  if (p.wide) {
     if constexpr (SHARED && NT == 1) {
-      fn = (const void*)k_attn_step32<HD, Q8>;
-      lds = Step32Lds<HD, Q8>::BYTES;
+      fn = (const void*)k_attn_wide<HD, NT, Q8>;
+      lds = WideLds<HD, NT, Q8>::BYTES;
     }
   } else if constexpr (Q8) {
     fn = (const void*)k_attn_step8<HD, NT, STREAM, SHARED>;
@@ -1927,9 +1755,10 @@ hipError_t launch(const ArgsOf<Q8, SHARED>& a, const AttnPlan& p, hipStream_t st
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t rh = (int64_t)a.n_rows * a.H;
   if constexpr (Q8 || SHARED) {
-    constexpr int per = kBlock / (HD / 8);
-    hipLaunchKernelGGL((k_attn_join8<HD, NT == 3>), dim3((unsigned)((rh + per - 1) / per)),
-                       dim3(kBlock), 0, stream, a);
+    const bool four = a.S > 8 && rh <= 32 * kCUs;  // (a wave each, one round of them)
+    const int per = kBlock / (HD / 8) / (four ? 4 : 1);
+    const auto fn = four ? k_attn_join8<HD, NT == 3, 4> : k_attn_join8<HD, NT == 3, 1>;
+    hipLaunchKernelGGL(fn, dim3((unsigned)((rh + per - 1) / per)), dim3(kBlock), 0, stream, a);
   } else {
     hipLaunchKernelGGL((k_attn_join<HD, NT == 3>), dim3((unsigned)((rh + kWaves - 1) / kWaves)),
                        dim3(kBlock), 0, stream, a);

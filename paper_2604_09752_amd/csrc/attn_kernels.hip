@@ -4,6 +4,8 @@
 
 // Workgroups up to which the keys are split.
 constexpr int64_t kStepGroups = 4 * kCUs, kRowsGroups = 2 * kCUs;
+// Columns of a group, on average, from which one token each takes k_attn_wide.
+constexpr int64_t kWideGroup = 48;
 
 
 int aio_attn_plan(const aio_seqs& s, int H, int Hkv, int hd, int dtype, AttnPlan* p,
@@ -80,23 +82,29 @@ int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, in
   px->n = x.n_groups;
   px->max = most_shared;
   // A place for every full tile of the groups' rows, and one more for each group with rows.
-  p->cols = !p->rows && dtype == AIO_BF16 && (int64_t)s.n_rows * G > 16 * (int64_t)x.n_groups ? 32 : 16;
-  const int64_t width = p->rows ? 32 * p->waves : p->cols;
+  p->wide = !p->rows && dtype == AIO_BF16 && (int64_t)s.n_rows * G >= kWideGroup * (int64_t)x.n_groups;
+  const int64_t width = p->rows ? 32 * p->waves : p->wide ? 32 * kWaves : kMaxGroup;
   const int64_t tiles = (int64_t)s.n_rows * G / width + std::min(x.n_groups, s.n_rows);
   auto splits = [](int64_t most, int64_t base, int64_t units) {
     return (int)std::max<int64_t>(1, std::min(units, most / std::max<int64_t>(1, base)));
   };
-  const int64_t most = !p->rows ? (p->cols == 32 ? kRowsGroups : kStepGroups) : dtype == AIO_F32 ? kRowsGroups / 2 : kRowsGroups;
-  const int64_t unit = p->rows ? kKeys : 128, own = p->rows ? p->tiles : s.n_seqs;
+  const int64_t most_rows = dtype == AIO_F32 ? kRowsGroups / 2 : kRowsGroups;
+  const int64_t units = ((int64_t)s.max_len + kKeys - 1) / kKeys;
+  const int64_t shared_units = (most_shared + kKeys - 1) / kKeys;
+  const int64_t own = p->rows ? p->tiles : s.n_seqs;
   if (p->rows) {
     // One round of workgroups, the own keys' among them; a sequence's own keys are split from
     // kOwnPer key tiles on.
-    const int64_t units = ((int64_t)s.max_len + unit - 1) / unit;
-    px->own = splits(most / 2, own * Hkv, (units + kOwnPer - 1) / kOwnPer);
-    px->S = splits(most - std::min(most / 2, own * Hkv), tiles * Hkv, (most_shared + unit - 1) / unit);
+    px->own = splits(most_rows / 2, own * Hkv, (units + kOwnPer - 1) / kOwnPer);
+    px->S = splits(most_rows - std::min(most_rows / 2, own * Hkv), tiles * Hkv, shared_units);
+  } else if (p->wide) {
+    // (a shared workgroup per CU at least, own ones beside it: 48 rows of 32 heads on 8 behind 8192 keys
+    // take XXX us with 12 splits, XXX with 16, XXX with 32)
+    px->own = splits(kRowsGroups, own * Hkv, (units + 1) / 2);
+    px->S = splits(std::max<int64_t>(kCUs, kRowsGroups - own * Hkv), tiles * Hkv, shared_units);
   } else {
-    px->S = splits(most, tiles * Hkv, (most_shared + unit - 1) / unit);
-    px->own = splits(most, own * Hkv, ((int64_t)s.max_len + unit - 1) / unit);
+    px->S = splits(kStepGroups, tiles * Hkv, (shared_units + 1) / 2);
+    px->own = splits(kStepGroups, own * Hkv, (units + 1) / 2);
   }
   const int64_t shared = tiles * Hkv * px->S;
   p->groups = shared + own * Hkv * px->own;

@@ -50,7 +50,7 @@ struct AttnPlan {
   int64_t tiles;   // row tiles of all sequences, at most (k_attn_rows)
   int64_t groups;  // workgroups
   size_t ws;       // bytes of partial results
-  int cols;        // of groups' rows in a tile of one token each: 16 or 32
+  bool wide;       // one token each in groups of many columns (k_attn_wide)
 };
 // AIO_OK, or the error that the entry points return for these sizes.
 // (key_bytes: of an element of the keys)
