@@ -92,6 +92,11 @@ int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, in
   const int64_t units = ((int64_t)s.max_len + kKeys - 1) / kKeys;
   const int64_t shared_units = (most_shared + kKeys - 1) / kKeys;
   const int64_t own = p->rows ? p->tiles : s.n_seqs;
+  // (128 keys each of what the longest may have beyond the longest prefix, where both are given
+  // closely; four at least, for sequences that share less.  Splits without keys are not free: about
+  // 220 workgroups start in a microsecond)
+  const int64_t own_units = std::max<int64_t>(
+      std::min<int64_t>(4, (units + 1) / 2), ((int64_t)s.max_len - most_shared) / 128 + 1);
   if (p->rows) {
     // One round of workgroups, the own keys' among them; a sequence's own keys are split from
     // kOwnPer key tiles on.
@@ -100,11 +105,11 @@ int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, in
   } else if (p->wide) {
     // (a shared workgroup per CU at least, own ones beside it: 48 rows of 32 heads on 8 behind 8192 keys
     // take XXX us with 12 splits, XXX with 16, XXX with 32)
-    px->own = splits(kRowsGroups, own * Hkv, (units + 1) / 2);
+    px->own = splits(kRowsGroups, own * Hkv, own_units);
     px->S = splits(std::max<int64_t>(kCUs, kRowsGroups - own * Hkv), tiles * Hkv, shared_units);
   } else {
     px->S = splits(kStepGroups, tiles * Hkv, (shared_units + 1) / 2);
-    px->own = splits(kStepGroups, own * Hkv, (units + 1) / 2);
+    px->own = splits(kStepGroups, own * Hkv, own_units);
   }
   const int64_t shared = tiles * Hkv * px->S;
   p->groups = shared + own * Hkv * px->own;
