@@ -133,6 +133,21 @@ int aio_attention_plan(const aio_seqs* s, int H, int Hkv, int hd, int dtype, int
   return AIO_OK;
 }
 
+int aio_groups_attention_plan(const aio_seqs* s, const aio_prefixes* x, int H, int Hkv, int hd,
+                              int dtype, int key_bytes, int32_t* out) {
+  if (!s || !x || !out) return AIO_EINVAL;
+  AttnPlan p;
+  PrefixArgs px;
+  const int rc = aio_groups_plan(*s, *x, H, Hkv, hd, dtype, &p, &px, key_bytes);
+  if (rc) return rc;
+  out[0] = p.waves;
+  out[1] = p.wide;
+  out[2] = px.S;
+  out[3] = px.S ? px.own : p.splits;
+  out[4] = px.groups;
+  return AIO_OK;
+}
+
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd) {
   // step: splits n Hkv <= kStepGroups, so splits n H <= kStepGroups G; rows: splits tiles
   // Hkv <= kRowsGroups and n_rows G <= 256 tiles, so splits n_rows H <= 256 kRowsGroups

@@ -66,6 +66,11 @@ int aio_groups_plan(const aio_seqs& s, const aio_prefixes& x, int H, int Hkv, in
 // whether the keys pass the caches by.
 extern "C" int aio_attention_plan(const aio_seqs* s, int H, int Hkv, int hd, int dtype,
                                   int32_t* out);
+// The same with groups (over 8-bit keys: key_bytes 1): out[5] = waves of a workgroup of prompt
+// rows (0: one new token per sequence), whether shared keys are taken as those, splits of the
+// shared and of the own keys (0, 1: nothing is shared), workgroups of the shared part.
+extern "C" int aio_groups_attention_plan(const aio_seqs* s, const aio_prefixes* x, int H, int Hkv,
+                                         int hd, int dtype, int key_bytes, int32_t* out);
 // No attention of these heads takes more workspace, whatever its sequences.
 size_t aio_attn_workspace_bound(int H, int Hkv, int hd);
 

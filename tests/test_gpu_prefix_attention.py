@@ -77,12 +77,15 @@ STEPS = {
     "many": ([500 + 7 * (i % 11) for i in range(70)], [(0, 69, 490), (69, 70, 64)]),
     "groups": ([150 + i for i in range(140)], [(2 * i, 2 * i + 2, 140 + i) for i in range(70)]),
     "none": ([30, 600], []),
+    # (48 columns per group and more with 4 or 8 heads of queries per kv head)
+    "wide": ([700 + 3 * i for i in range(40)] + [0, 690, 20], [(0, 43, 688)]),
+    "wide groups": ([300 + i % 9 for i in range(26)], [(0, 13, 299), (13, 26, 270)]),
 }
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("q8", [False, True])
-@pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 64), (8, 2, 128), (6, 2, 64), (16, 1, 128)])
+@pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 64), (8, 2, 128), (6, 2, 64), (16, 1, 128), (8, 2, 64)])
 @pytest.mark.parametrize("name", list(STEPS))
 def test_step(name, H, Hkv, hd, q8, dtype):
     k_len, groups = STEPS[name]
@@ -93,6 +96,31 @@ def test_step(name, H, Hkv, hd, q8, dtype):
                dict(max_len=30000, max_prefix=20000), dict(max_prefix=100)):
         out, l = p.run(q, **kw)
         check_attention(out, l, want, "%s %s" % (name, kw))
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_wide_values_that_are_not_finite(hd, q8):
+    """In the prefix they reach every row of the group, in a sequence's own keys that one."""
+    k_len = [400 + i for i in range(14)]
+    p = Grouped(k_len, [(0, 14, 384)], 1, hd, q8=q8)
+    q = rows(14, 4, hd, BF16)
+    want = p.ref(q)
+    page = int(p.case.table[3, 25])  # own keys of sequence 3 (24 full pages are shared)
+    for at, who in (((int(p.case.table[0, 7]), 5), range(14)), ((page, 2), [3])):
+        kv = [t.clone() for t in p.kv]
+        if q8:
+            p.kv[1][at[0], 0, at[1]] = 0
+            p.kv[3][at[0], 0, at[1]] = 255
+        else:
+            p.kv[1][at[0], 0, at[1]] = float("nan")
+        out, l = p.run(q, max_len=420, max_prefix=384)
+        out = out.cpu()
+        assert torch.isnan(out[list(who)]).all()
+        out[list(who)] = want[0][list(who)].to(BF16)
+        check_attention(out, l.cpu(), want)
+        for t, old in zip(p.kv, kv):
+            t.copy_(old)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -154,10 +182,10 @@ def test_prompts(name, H, Hkv, hd, q8, dtype):
 @pytest.mark.parametrize("q8", [False, True])
 def test_wide_tiles(q8):
     """Enough rows and heads for 256-row tiles of bf16 queries: as without groups."""
-    ql, k_len = [600, 500, 401], [1100, 1001, 960]
+    ql, k_len = [900, 700, 560], [1400, 1201, 1119]
     p = Grouped(k_len, [(0, 3, 490)], 16, 64, q8=q8)
     q = rows(sum(ql), 128, 64, BF16)
-    out, l = p.run(q, ql, max_len=1100, max_prefix=490)
+    out, l = p.run(q, ql, max_len=1400, max_prefix=490)
     plain, pl = torch.empty_like(out), torch.empty_like(l)
     f = B.aio_q8_attention if q8 else B.aio_paged_attention
     f(q.cuda(), *p.kv, p.lens, p.table, plain, cu_q=cu(ql).cuda(), lse=pl)
