@@ -1,5 +1,6 @@
-// Attention over the keys of several sequences, in pages or packed: one new
-// token per sequence (k_attn_step) and the rows of prompts (k_attn_rows).
+// Attention over the keys of several sequences, in pages or packed, bf16 or 8-bit codes: one
+// new token per sequence (k_attn_step, k_attn_step8) and the rows of prompts (k_attn_rows), by
+// themselves or in groups that share their first keys (SHARED, k_attn_wide).
 //
 // For a row with scores s_j = scale q.k_j over its visible keys j, with the
 // running maximum m and sum l over the key blocks seen so far:
@@ -651,7 +652,12 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 // rows and the rows' powers of two, reads the keys as operands (a lane's eight codes of
 // a k chunk are eight neighbours of its row: the queries' chunks are taken alike) and the values
 // transposed, and makes bf16 of both in registers, where codes are exact.  A power of two goes
-// to the key's score and to the value's weight, 16 products instead of 128.
+// to the key's score and to the value's weight, 16 products instead of 128.  What bounds it is the
+// reading of the codes (two requests of 32768 keys, 32 heads of 128, fp32: 92 us, 5.9 TB/s; with
+// bf16 made before LDS, 126), or with few keys the launch and three dependent reads (one request
+// of 201 keys: 7.2 us); of 24 ragged requests of up to 4096 keys, 31 us, 2.8 TB/s, half is
+// the start of 960 workgroups and the longest of them.  Two blocks in flight instead of one: no
+// faster (34 us, 94 us).
 template <int HD>
 struct Step8Lds {
   // bytes of a row, and of the second 16 rows from the first: the 16 rows of an operand, and
@@ -1546,7 +1552,11 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(
 }
 
 // One new token of each sequence in groups of many columns: shared keys as the rows of a prompt,
-// 128 columns for a key that is staged once, every sequence's own keys as a step.
+// 128 columns for a key that is staged once, every sequence's own keys as a step (48 rows of 32
+// heads on 8 behind 8192 keys, bf16: 34 us; all as steps of 16 columns, 42, where LDS and the
+// caches' lines are two thirds busy; of 32 columns, 37).  What bounds it is one tile after the other
+// in each workgroup (2.3 us per 64 keys, whether one or two are on a CU), and the start and
+// the join, 10 us.
 template <int HD, int NT, bool Q8>
 struct WideLds {
   static constexpr int ROWS = RowsLds<HD>::BYTES(NT, kWaves);
@@ -1626,8 +1636,9 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
 
 // The same with 8 elements of a row and head per lane and everything of 8 splits requested at
 // once, places without keys among it: one trip to memory where k_attn_join makes two, and
-// a quarter of the waves (400 rows of 16 heads of 128, 7 splits: 8.0 -> 6.4 us).  SPL lanes share
-// the splits of 8 elements: many splits of few rows (48 rows of 32 heads, 17 splits: XXX).
+// a quarter of the waves (343 rows of 16 heads of 128: 8.0 us, so 6.4).  SPL lanes share the
+// splits of 8 elements where there are many of few rows (48 rows of 32 heads, 17 splits: 6.0 us;
+// 33 splits one after the other took 10.1).
 template <int HD, bool F32, int SPL>
 __global__ __launch_bounds__(kBlock) void k_attn_join8(AttnArgs a) {
   constexpr int LANES = HD / 8 * SPL, B = 8;

@@ -31,7 +31,6 @@ AIO_DEV float group_sum(float v) {
 }
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 // 16-byte streaming load of weights (read once per token: no reuse to keep).
 AIO_DEV uint4 ld_stream(const uint4* p) {
@@ -68,11 +67,6 @@ AIO_DEV float dot4_i8(uint32_t w, const float4 a, float acc) {
 template <int CTRL>
 AIO_DEV float dpp_mov(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
-}
-
-template <int CTRL>
-AIO_DEV uint32_t dpp_bits(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
 }
 
 // Sum over aligned groups of 8 or 16 lanes; every lane of a group receives

