@@ -561,7 +561,8 @@ int aio_page_append(const aio_paged_kv* kv, const aio_seqs* s, const void* k_row
  * s head_dim and one unsigned byte b at p exp_page_stride + h exp_head_stride +
  * s of k_exp_dev or v_exp_dev; its elements are code 2^(b - 127), half the bytes
  * of a bf16 page.  b lies from 8 to 248; b = 255 with codes of 0 stands for a
- * row that held something not finite, and reads as NaN. */
+ * row that held something not finite, and reads as NaN.  (Codes and bytes of a
+ * page that lie behind one another are one copy for aio_page_copy.) */
 typedef struct aio_q8_kv {
   void* k_dev;
   void* v_dev;
@@ -583,7 +584,8 @@ typedef struct aio_q8_kv {
  * and the codes are the elements over 2^(b - 127), rounded alike and held to 127: an
  * element is off by at most A / 127, or by 2^-120 where that is more.  A row with an infinity
  * or NaN gets b = 255 and codes of 0.  Which rows are written, and the errors, as
- * aio_page_append; pages, heads, K and V, codes and bytes must not overlap. */
+ * aio_page_append; pages, heads, K and V, codes and bytes must not overlap
+ * (AIO_EINVAL where strides or the first page's rows show it). */
 int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev,
                   const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                   int64_t head_stride, void* hip_stream);

@@ -521,9 +521,10 @@ def _paged8(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.
     page_stride, head_stride, slot, one = stride
     if v.stride() != stride or one != 1 or slot != hd:
         raise ValueError("pages: K and V of the same strides, slots and dimensions contiguous")
-    exp_stride = k_exp.stride()
-    if (k_exp.shape != shape[:3] or v_exp.shape != shape[:3] or k_exp.dtype is not torch.uint8 or
-            v_exp.dtype is not torch.uint8 or v_exp.stride() != exp_stride or exp_stride[2] != 1):
+    exp_shape, exp_stride = k_exp.shape, k_exp.stride()
+    if (exp_shape != (pages, heads, size) or v_exp.shape != exp_shape or
+            k_exp.dtype is not torch.uint8 or v_exp.dtype is not torch.uint8 or
+            v_exp.stride() != exp_stride or exp_stride[2] != 1):
         raise ValueError("k_exp, v_exp: two uint8 [n_pages, kv_heads, page_size] of the same "
                          "strides, slots contiguous")
     return _pack_q8(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
@@ -789,6 +790,12 @@ def _append(call, at, kv, kv_heads, page_size, hd, k_rows, v_rows, lens, table, 
         raise AioError(rc, call.__name__)
 
 
+def _head_weight(w: torch.Tensor, hd: int) -> int:
+    if w.dtype is not torch.bfloat16 or w.shape != (hd,) or (w.stride(0) != 1 and hd > 1):
+        raise ValueError("q_weight, k_weight: contiguous bf16 [head_dim]")
+    return w.data_ptr()
+
+
 def aio_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
                      q_out: torch.Tensor, k_out: torch.Tensor,
                      q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
@@ -806,15 +813,15 @@ def aio_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
     rows, heads, hd = shape
     _i32(positions, 1, "positions")
     _need(positions.shape[0] == rows, "one position per row")
-    for w in (q_weight, k_weight):
-        if w is not None and (w.dtype is not torch.bfloat16 or w.shape != (hd,) or
-                              not w.is_contiguous()):
-            raise ValueError("q_weight, k_weight: contiguous bf16 [head_dim]")
+    qw = kw = None
+    if q_weight is not None:
+        qw = _head_weight(q_weight, hd)
+    if k_weight is not None:
+        kw = _head_weight(k_weight, hd)
     r = _pack_qk(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
                  _rows3(q, shape, "q"), _rows3(k, k_shape, "k"), _rows3(q_out, shape, "q_out"),
                  _rows3(k_out, k_shape, "k_out"), _DTYPES[dtype], rows, heads, k_shape[1], hd)
-    rc = _launch(at, lib().aio_qk_norm_rope, r, positions.data_ptr(), _ptr(q_weight),
-                 _ptr(k_weight), eps, base)
+    rc = _launch(at, lib().aio_qk_norm_rope, r, positions.data_ptr(), qw, kw, eps, base)
     if rc:
         raise AioError(rc, "aio_qk_norm_rope")
 

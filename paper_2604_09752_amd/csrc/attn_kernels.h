@@ -69,6 +69,18 @@ AIO_DEV void terms(const float (&x)[8], bf16x8 (&t)[NT]) {
   }
 }
 
+// Eight elements of a query row, times a power of two.
+template <int NT>
+AIO_DEV void load_scaled_query(const AttnArgs& a, int row, int head, int hd, int d0, float by,
+                               bf16x8 (&t)[NT]) {
+  const int64_t at = (int64_t)row * a.ldq + (int64_t)head * hd + d0;
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    x[j] = by * (NT == 1 ? bf16_to_f32(((const uint16_t*)a.q)[at + j]) : ((const float*)a.q)[at + j]);
+  terms<NT>(x, t);
+}
+
 // Eight elements of a query row.
 template <int NT>
 AIO_DEV void load_query(const AttnArgs& a, int row, int head, int hd, int d0, bool live,
@@ -276,6 +288,45 @@ AIO_DEV bool step_unit(const AttnArgs& a, StepUnit& u) {
     if (tid < a.G)
       a.part_ml[(((int64_t)split * a.n_rows + u.seq) * a.H + u.kvh * a.G + tid) * 2] = -INFINITY;
     return false;
+  }
+  return true;
+}
+
+// The same for up to 64 sequences, whose splits that have keys come first, the others last: empty
+// workgroups among them would take places, and not evenly (24 requests of 118 to 4096 keys, 8 kv
+// heads, in splits of 896 keys: 31.4 us with the empty ones between, 26.9 so; of 512 keys: 39, 28).
+// A sequence's first split marks the places of those without keys.
+AIO_DEV bool packed_step_unit(const AttnArgs& a, StepUnit& u) {
+  const int tid = threadIdx.x, lane = tid & (AIO_WAVE - 1);
+  int len = 0, pieces = 0;
+  if (lane < a.n_seqs) {
+    len = paged_len(a.kv, lane, a.max_len);
+    pieces = max(1, (int)(((int64_t)len + a.chunk - 1) / a.chunk));
+  }
+  int end = pieces;  // of the splits up to this sequence's
+#pragma unroll
+  for (int off = 1; off < AIO_WAVE; off *= 2) {
+    const int before = __shfl_up(end, off, AIO_WAVE);
+    if (lane >= off) end += before;
+  }
+  // (sequences, their kv heads, their splits; lanes past the last sequence repeat its end)
+  const int seq = __popcll(__ballot(end * a.kv.Hkv <= (int)blockIdx.x));
+  if (seq >= a.n_seqs) return false;
+  u.seq = seq;
+  len = __builtin_amdgcn_readlane(len, seq);
+  pieces = __builtin_amdgcn_readlane(pieces, seq);
+  const int at = blockIdx.x - (__builtin_amdgcn_readlane(end, seq) - pieces) * a.kv.Hkv;
+  u.kvh = (int)((unsigned)at / (unsigned)pieces);
+  u.slot = at - u.kvh * pieces;
+  u.c0 = u.slot * a.chunk;
+  u.c1 = min(len, u.c0 + a.chunk);
+  u.first = seq;
+  u.p0 = 0;
+  u.ncol = a.G;
+  u.need = 0;
+  if (u.slot == 0 && tid < a.G) {
+    const int64_t rh = (int64_t)seq * a.H + u.kvh * a.G + tid;
+    for (int i = pieces; i < a.S; ++i) a.part_ml[((int64_t)i * a.n_rows * a.H + rh) * 2] = -INFINITY;
   }
   return true;
 }
@@ -655,9 +706,9 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 // to the key's score and to the value's weight, 16 products instead of 128.  What bounds it is the
 // reading of the codes (two requests of 32768 keys, 32 heads of 128, fp32: 92 us, 5.9 TB/s; with
 // bf16 made before LDS, 126), or with few keys the launch and three dependent reads (one request
-// of 201 keys: 7.2 us); of 24 ragged requests of up to 4096 keys, 31 us, 2.8 TB/s, half is
-// the start of 960 workgroups and the longest of them.  Two blocks in flight instead of one: no
-// faster (34 us, 94 us).
+// of 201 keys: 7.2 us).  24 ragged requests of up to 4096 keys: 27 us, 3.3 TB/s, of which the
+// join, the start and seven blocks one after the other in the longest workgroups are half.  Two
+// blocks in flight instead of one: no faster (7 % and 2 % slower).
 template <int HD>
 struct Step8Lds {
   // bytes of a row, and of the second 16 rows from the first: the 16 rows of an operand, and
@@ -688,7 +739,7 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
   if constexpr (SHARED) {
     if (!shared_step_unit(a, u)) return;
   } else {
-    if (!step_unit(a, u)) return;
+    if (!(a.n_seqs <= AIO_WAVE ? packed_step_unit(a, u) : step_unit(a, u))) return;
   }
   const int seq = u.seq, kvh = u.kvh, c0 = u.c0, c1 = u.c1;
   bf16x8 q[NC][NT];
@@ -697,6 +748,30 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
 #pragma unroll
   for (int c = 0; c < NC; ++c)
     load_query<NT>(a, row, head, HD, c / 2 * 64 + 16 * grp + c % 2 * 8, col < u.ncol, q[c]);
+  // Products with codes would pass the largest float, before the key's power of two brings them
+  // down, from queries of 2^114 on: columns with an element of 2^99 are taken 2^-14 times as large.
+  float scale_log2 = a.scale_log2;
+  {
+    bool large = false;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const u32x4 w = __builtin_bit_cast(u32x4, q[c][0]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        large |= (w[k] & 0x7f80u) >= 0x7100u || (w[k] & 0x7f800000u) >= 0x71000000u;
+    }
+    if (__any(large)) {
+      large |= __shfl_xor((int)large, 16, AIO_WAVE) != 0;
+      large |= __shfl_xor((int)large, 32, AIO_WAVE) != 0;
+      large &= scale_log2 < 0x1p100f && col < u.ncol;
+      if (large) {
+        scale_log2 *= 0x1p14f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          load_scaled_query<NT>(a, row, head, HD, c / 2 * 64 + 16 * grp + c % 2 * 8, 0x1p-14f, q[c]);
+      }
+    }
+  }
   if constexpr (SHARED) {
     if (tid < kMaxGroup) use[tid] = paged_len(a.kv, row, a.max_len) >= u.need;
   }
@@ -747,7 +822,7 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
   float* park_m = (float*)(smem + L::TILES + wid * L::HBYTES + HD * 16 * 4) + lane;
   auto parked_scale = [&] {
     const float mh = *park_m;
-    return mh == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mh - m) * a.scale_log2);
+    return mh == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mh - m) * scale_log2);
   };
   char* ktile = smem + wid * L::WBYTES;
   char* vtile = ktile + L::TBYTES;
@@ -810,9 +885,9 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
       swap16(mx, other);
       mx = fmaxf(mx, other);
       const float mnew = fmaxf(m, mx);
-      const float mref = mnew == -INFINITY ? 0.f : mnew * a.scale_log2;
+      const float mref = mnew == -INFINITY ? 0.f : mnew * scale_log2;
       if (__any(mnew > m)) {
-        const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.scale_log2 - mref);
+        const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * scale_log2 - mref);
         l *= c;
         lh *= c;
 #pragma unroll
@@ -821,7 +896,7 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
       m = mnew;
 #pragma unroll
       for (int v = 0; v < 8; ++v) {
-        p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], a.scale_log2, -mref));
+        p[v] = __builtin_amdgcn_exp2f(fmaf(p[v], scale_log2, -mref));
         l += p[v];
       }
       carry(lh, l);
@@ -869,7 +944,7 @@ AIO_DEV void attn_step8(AttnMoreArgs a) {
   if (col < u.ncol) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) *(f32x4*)(st.out(wid, col) + d * 16 + 4 * grp) = o[d];
-    if (grp == 0) st.ml(wid, col) = make_float2(m * a.scale_log2, l);
+    if (grp == 0) st.ml(wid, col) = make_float2(m * scale_log2, l);
   }
   step_finish<HD, NT, SHARED>(a, u, st, use);
 }

@@ -467,18 +467,19 @@ int aio_qk_norm_rope(const aio_qk_rows* r, const int32_t* positions_dev,
   if (r->dtype != AIO_F32 && r->dtype != AIO_BF16) return AIO_EINVAL;
   if (!(eps > 0.f) || !isfinite(eps) || !(base > 1.f) || !isfinite(base)) return AIO_EINVAL;
   const int64_t size = r->dtype == AIO_F32 ? 4 : 2;
-  struct Rows {
+  const int64_t strides[4] = {r->q_stride, r->k_stride, r->q_out_stride, r->k_out_stride};
+  for (const int64_t n : strides)
+    if (n < 0 || n > ((int64_t)1 << 56) || n * size % 16) return AIO_EINVAL;
+  const int64_t q_width = r->n_heads * r->head_dim * size, k_width = r->n_kv_heads * r->head_dim * size;
+  const struct Rows {
     const void* p;
     int64_t stride, width;  // bytes
-  } rows[4] = {{r->q_dev, r->q_stride * size, r->n_heads * r->head_dim * size},
-               {r->k_dev, r->k_stride * size, r->n_kv_heads * r->head_dim * size},
-               {r->q_out_dev, r->q_out_stride * size, r->n_heads * r->head_dim * size},
-               {r->k_out_dev, r->k_out_stride * size, r->n_kv_heads * r->head_dim * size}};
-  const int64_t strides[4] = {r->q_stride, r->k_stride, r->q_out_stride, r->k_out_stride};
-  for (int i = 0; i < 4; ++i) {
-    if (strides[i] < 0 || strides[i] > ((int64_t)1 << 56) || rows[i].stride % 16) return AIO_EINVAL;
-    if (i >= 2 && r->n_rows > 1 && rows[i].stride < rows[i].width) return AIO_EINVAL;
-  }
+  } rows[4] = {{r->q_dev, strides[0] * size, q_width},
+               {r->k_dev, strides[1] * size, k_width},
+               {r->q_out_dev, strides[2] * size, q_width},
+               {r->k_out_dev, strides[3] * size, k_width}};
+  for (int i = 2; i < 4; ++i)
+    if (r->n_rows > 1 && rows[i].stride < rows[i].width) return AIO_EINVAL;
   if (r->n_rows == 0) return AIO_OK;
   for (const Rows& x : rows)
     if (!good(x.p, 16)) return AIO_EINVAL;

@@ -68,6 +68,25 @@ def test_step_split_over_the_keys(n, length, hd, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 90])
+def test_step_ragged_batches(n, dtype):
+    """Splits with keys come first for up to 64 sequences, and one after the other beyond;
+    idle places among them, whatever the workspace holds."""
+    lens = [(37 * i * i + 1) % 700 if i % 7 else 0 for i in range(n)]
+    lens[n // 2] = 1500
+    pool = Q8Pool(PoolCase(lens, 2, 64, 16, seed=n))
+    q = rows(n, 4, 64, dtype)
+    want = ref(pool.case, q, [1] * n)
+    for max_len in (1500, 9000):
+        need = B.aio_q8_workspace_bytes(n, n, max_len, 4, 2, 64)
+        assert need > 0
+        for fill in (0, 255):
+            ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+            out, l = run(pool, q, max_len=max_len, ws=ws)
+            check_attention(out, l, want, (max_len, fill))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("page,hd", [(16, 64), (8, 128), (8, 64)])
 def test_step_holes(page, hd, dtype):
     lens = [100, 40, 16, 700]
@@ -167,6 +186,27 @@ def test_magnitudes(ql, scale_k, scale_v, dtype):
     q = (rows(sum(n), 4, 64, F32) / scale_k / 64).to(dtype)
     out, l = run(pool, q, ql)
     check_attention(out, l, ref(case, q, n))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("big", [2.0 ** 120, 2.0 ** 104, 2.0 ** -104])
+@pytest.mark.parametrize("ql", [None, [40]])
+def test_queries_at_the_ends_of_the_range(ql, big, dtype):
+    """Queries next to the largest (smallest) numbers, keys that bring their scores back; one
+    query among them is of ordinary size and sees scores next to 0, or the largest keys."""
+    n, hd = 150, 64
+    case = PoolCase([n], 1, hd, 16)
+    case.keys[0] = (case.keys[0].float() / big).to(BF16)
+    for j in range(-(-n // 16)):
+        m = min(16, n - j * 16)
+        case.k[int(case.table[0, j]), :, :m] = case.keys[0][j * 16: j * 16 + m].transpose(0, 1)
+    pool = Q8Pool(case)
+    nq = ql or [1]
+    q = (rows(sum(nq), 4, hd, F32).clamp(-3, 3) * big).to(dtype)
+    if big > 1:
+        q[:, 2] = rows(sum(nq), 1, hd, F32)[:, 0].to(dtype)
+    out, l = run(pool, q, ql)
+    check_attention(out, l, ref(case, q, nq))
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
