@@ -187,7 +187,7 @@ constexpr int kStepCarry = 32, kRowsCarry = 32;
 // rows all see all of them: its rows and heads are packed into tiles that read each key
 // once, and every sequence's own workgroups begin behind them.  Both write partial
 // results, the shared part into the first px.S places of a row and its own into the others,
-// and k_attn_join joins them.  A sequence whose rows do not all see the whole prefix (an idle
+// and k_attn_join8 joins them.  A sequence whose rows do not all see the whole prefix (an idle
 // place, say) takes no part: its own workgroups read all of its keys and mark the first
 // places as empty.
 //
@@ -1080,7 +1080,8 @@ template <int HD, int NT, Keys KEYS, int W, bool SHARED>
 AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   using L = RowsLds<HD>;
   constexpr bool PAGED = KEYS != kPacked, Q8 = KEYS == kPaged8;
-  constexpr bool ADAPT = Q8 || SHARED;  // (with what the kernels over bf16 keys have no registers for)
+  // edge tiles requested ahead, waves without rows that only move tiles
+  constexpr bool AHEAD = Q8 || SHARED;
   constexpr int kThreads = W * AIO_WAVE, kRows = W * 32;
   extern __shared__ __align__(16) char smem[];
   __shared__ uint8_t seen[kKeys];
@@ -1177,7 +1178,7 @@ AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
     return;
   }
   // (a wave without rows only moves tiles)
-  const bool idle = ADAPT && p0 + wid * 32 >= packed;
+  const bool idle = AHEAD && p0 + wid * 32 >= packed;
 
   bf16x8 q[NC][NT];
 #pragma unroll
@@ -1203,12 +1204,12 @@ AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   // all through the loop below: 2048 rows of the 1B behind 1637 keys, bf16, 90 us without a hole,
   // 263 with one.)
   int tp = min(t1, max(t0, all_lim < 0 ? 0 : (all_lim + 1) / kKeys));
-  bool holes = PAGED && !ADAPT;  // (of those after them: some may be)
+  bool holes = PAGED && !AHEAD;  // (of those after them: some may be)
   if constexpr (PAGED) {
     // (not with holes among them)
-    if (ADAPT ? t1 > t0 : tp > t0) {
+    if (AHEAD ? t1 > t0 : tp > t0) {
       bool hole = false;
-      const int e1 = ((ADAPT ? min(t1 * kKeys, len) : tp * kKeys) - 1) >> a.kv.shift;
+      const int e1 = ((AHEAD ? min(t1 * kKeys, len) : tp * kKeys) - 1) >> a.kv.shift;
       for (int e = (t0 * kKeys >> a.kv.shift) + tid; e <= e1; e += kThreads)
         hole |= (unsigned)table[e] >= (unsigned)a.kv.limit;
       if (__syncthreads_or(hole)) {
@@ -1483,7 +1484,7 @@ AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
   };
   for (int t = tp; t < t1; ++t) {
     const int j0 = t * kKeys;
-    if (!ADAPT || t == tp) fetch(t);
+    if (!AHEAD || t == tp) fetch(t);
     __syncthreads();  // every wave is done with the tile before
     bool odd = false;
 #pragma unroll
@@ -1517,7 +1518,7 @@ AIO_DEV void attn_rows(ArgsOf<KEYS == kPaged8, SHARED> a) {
       }
       __syncthreads();
     }
-    if (ADAPT && t + 1 < t1) fetch(t + 1);  // (in flight meanwhile)
+    if (AHEAD && t + 1 < t1) fetch(t + 1);  // (in flight meanwhile)
     if (j0 > wave_lim || idle) continue;
     f32x16 s[2];
     float mx = -INFINITY;
