@@ -585,7 +585,7 @@ typedef struct aio_q8_kv {
  * element is off by at most A / 127, or by 2^-120 where that is more.  A row with an infinity
  * or NaN gets b = 255 and codes of 0.  Which rows are written, and the errors, as
  * aio_page_append; pages, heads, K and V, codes and bytes must not overlap
- * (AIO_EINVAL where strides or the first page's rows show it). */
+ * (AIO_EINVAL). */
 int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev,
                   const void* v_rows_dev, int32_t dtype, int64_t row_stride,
                   int64_t head_stride, void* hip_stream);

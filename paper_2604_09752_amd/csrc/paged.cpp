@@ -61,25 +61,72 @@ int check_q8(const aio_q8_kv& kv) {
   return AIO_OK;
 }
 
-// Codes, bytes, K or V that would take each other's place: pages and heads by their strides,
-// K against V and codes against bytes by their first rows too.
+typedef __int128 wide;  // (addresses and strides are any 64-bit numbers)
+wide floor_div(wide a, wide b) { return a / b - (a % b < 0); }  // b > 0
+
+// Blocks of `size` bytes in a grid of pages and heads.
+struct Blocks {
+  const void* at;
+  int64_t page, head, size;
+};
+
+// Rows of n blocks, of na and nb bytes, sa and sb apart, the second row d behind the first: whether a
+// block of one and one of the other share a byte.
+bool lines_overlap(wide d, int64_t n, int64_t sa, wide na, int64_t sb, wide nb) {
+  if (d >= (n - 1) * (wide)sa + na || -d >= (n - 1) * (wide)sb + nb) return false;
+  if (n == 1) return true;
+  if (sa == sb) {
+    if (sa == 0) return true;  // (d lies between -nb and na)
+    // the first of the differences d + t s, |t| < n, above -nb
+    const wide t = std::max<wide>(floor_div(-nb - d, sa) + 1, -(n - 1));
+    return t < n && d + t * sa < na;
+  }
+  for (int64_t i = 0; i < n; ++i) {
+    const wide at = d - i * (wide)sa;  // from block i of the first row
+    const wide j = sb ? std::max<wide>(floor_div(-nb - at, sb) + 1, 0) : 0;
+    if (j < n && at + j * sb < na && at + j * sb > -nb) return true;
+  }
+  return false;
+}
+
+// Whether a block of one grid and one of the other share a byte.
+bool grids_overlap(const Blocks& a, const Blocks& b, int64_t pages, int64_t heads) {
+  const wide d = (wide)(uintptr_t)b.at - (wide)(uintptr_t)a.at;
+  // all heads of a page, all pages of a head, as one block each: what pools look like
+  const wide a_heads = (heads - 1) * (wide)a.head + a.size, b_heads = (heads - 1) * (wide)b.head + b.size;
+  if (a.page == b.page && !lines_overlap(d, pages, a.page, a_heads, b.page, b_heads)) return false;
+  const wide a_pages = (pages - 1) * (wide)a.page + a.size, b_pages = (pages - 1) * (wide)b.page + b.size;
+  if (!lines_overlap(d, heads, a.head, a_pages, b.head, b_pages)) return false;
+  auto at = [&](wide from) { return lines_overlap(from, pages, a.page, a.size, b.page, b.size); };
+  if (a.head == b.head) {
+    for (int64_t h = 1 - heads; h < heads; ++h)
+      if (at(d + h * (wide)a.head)) return true;
+    return false;
+  }
+  for (int64_t i = 0; i < heads; ++i) {
+    // the heads of b that begin before the last page of a's head i ends, from the first that
+    // ends behind its start
+    const wide from = d - i * (wide)a.head;
+    wide j = b.head ? std::max<wide>(floor_div(-b_pages - from, b.head) + 1, 0) : 0;
+    for (; j < heads && from + j * b.head < a_pages; ++j)
+      if (at(from + j * b.head)) return true;
+  }
+  return false;
+}
+
+// Codes, bytes, K or V that would take each other's place.
 bool q8_overlaps(const aio_q8_kv& kv) {
   const int64_t codes = (int64_t)kv.page_size * kv.head_dim, exps = kv.page_size;
-  auto apart = [](const void* a, const void* b) {
-    const intptr_t x = (intptr_t)a, y = (intptr_t)b;
-    return (int64_t)(x < y ? y - x : x - y);
-  };
-  auto overlaps = [&](int64_t between, int64_t page, int64_t head, int64_t size) {
-    return aio_grid_overlaps(2, between, kv.n_pages, page, size) ||
-           aio_grid_overlaps(2, between, kv.n_kv_heads, head, size) ||
-           aio_grid_overlaps(kv.n_pages, page, kv.n_kv_heads, head, size);
-  };
-  if (overlaps(apart(kv.k_dev, kv.v_dev), kv.page_stride, kv.head_stride, codes) ||
-      overlaps(apart(kv.k_exp_dev, kv.v_exp_dev), kv.exp_page_stride, kv.exp_head_stride, exps))
+  if (aio_grid_overlaps(kv.n_pages, kv.page_stride, kv.n_kv_heads, kv.head_stride, codes) ||
+      aio_grid_overlaps(kv.n_pages, kv.exp_page_stride, kv.n_kv_heads, kv.exp_head_stride, exps))
     return true;
-  for (const void* c : {kv.k_dev, kv.v_dev})
-    for (const void* e : {kv.k_exp_dev, kv.v_exp_dev})
-      if (apart(c, e) < ((uintptr_t)c < (uintptr_t)e ? codes : exps)) return true;
+  const Blocks all[] = {{kv.k_dev, kv.page_stride, kv.head_stride, codes},
+                        {kv.v_dev, kv.page_stride, kv.head_stride, codes},
+                        {kv.k_exp_dev, kv.exp_page_stride, kv.exp_head_stride, exps},
+                        {kv.v_exp_dev, kv.exp_page_stride, kv.exp_head_stride, exps}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 4; ++j)
+      if (grids_overlap(all[i], all[j], kv.n_pages, kv.n_kv_heads)) return true;
   return false;
 }
 
@@ -197,7 +244,6 @@ int aio_check_paged(const aio_paged_kv& kv) {
 }
 
 bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t size) {
-  typedef __int128 wide;  // (strides are any 63-bit numbers)
   if ((n1 > 1 && s1 < size) || (n2 > 1 && s2 < size)) return true;
   if (n1 == 1 || n2 == 1) return false;
   // one dimension within a step of the other
@@ -218,7 +264,6 @@ bool aio_grid_overlaps(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t s
 
 bool aio_rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb,
                       int64_t n) {
-  typedef __int128 wide;
   const wide x = (uintptr_t)a, y = (uintptr_t)b;
   if (x + (wide)(n - 1) * sa + wa <= y || y + (wide)(n - 1) * sb + wb <= x) return false;
   if (sa != sb || n == 1 || sa == 0) return true;
