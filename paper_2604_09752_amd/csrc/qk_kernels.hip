@@ -83,18 +83,20 @@ __global__ __launch_bounds__(kBlock) void k_qk_norm_rope(QkArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += x[i] * x[i] + y[i] * y[i];
     sum = head_sum<LANES>(sum);
-    float inv = rsqrtf(sum * (1.f / HD) + a.eps);
-    if (!(sum < INFINITY)) {
-      // squares past the largest float: of elements 2^-70 times as large (eps is nothing then)
-      constexpr float kDown = 0x1p-70f;
+    const float mean = sum * (1.f / HD) + a.eps;
+    float inv = rsqrtf(mean);
+    if (!(mean >= 0x1p-90f && mean < INFINITY)) {
+      // the squares, eps or their sum past the largest float, or next to the smallest, where floats
+      // have few bits: of elements 2^-70 or 2^60 times as large, and eps by the square of that
+      const float by = mean < 0x1p-90f ? 0x1p60f : 0x1p-70f;
       sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] *= kDown;
-        y[i] *= kDown;
+        x[i] *= by;
+        y[i] *= by;
         sum += x[i] * x[i] + y[i] * y[i];
       }
-      inv = rsqrtf(head_sum<LANES>(sum) * (1.f / HD));
+      inv = rsqrtf(head_sum<LANES>(sum) * (1.f / HD) + a.eps * by * by);
     }
     float wx[8], wy[8];
 #pragma unroll
