@@ -591,7 +591,10 @@ int aio_q8_append(const aio_q8_kv* kv, const aio_seqs* s, const void* k_rows_dev
                   int64_t head_stride, void* hip_stream);
 
 /* aio_paged_attention over pages of 8-bit codes (an element is exactly a bf16,
- * so nothing is rounded on the way to the products).  Its workspace is
+ * so nothing is rounded on the way to the products; but for one new token per
+ * sequence the powers of two go to the weights, which bf16 terms hold to 2^-133:
+ * outputs are off by another 2^-126 n / l, of n keys and the sum l of their weights
+ * over the largest, which values below 2^-100 show).  Its workspace is
  * aio_q8_workspace_bytes's.  Errors as aio_paged_attention. */
 int aio_q8_attention(const aio_q8_kv* kv, const aio_seqs* s, const aio_attn* a, void* ws_dev,
                      size_t ws_bytes, void* hip_stream);
@@ -607,6 +610,7 @@ size_t aio_q8_workspace_bytes(const aio_seqs* s, int32_t n_heads, int32_t n_kv_h
 typedef struct aio_prefixes {
   int32_t n_groups;                /* at most 2^30                           */
   int32_t max_prefix;              /* more keys than that are not shared     */
+                                   /* (see aio_prefix_attention)             */
   const int32_t* cu_seqs_dev;      /* [n_groups + 1], ascending              */
   const int32_t* prefix_lens_dev;  /* [n_groups]                             */
 } aio_prefixes;
@@ -617,7 +621,11 @@ typedef struct aio_prefixes {
  * own length, in whole multiples of 64; the others' tables have to list pages of the
  * same contents (a fork's are the same pages).  A sequence that is not
  * to share (an idle place with lens 0, new rows that begin within the prefix)
- * computes all of its keys by itself.  Its workspace is
+ * computes all of its keys by itself.  max_len - max_prefix is taken for the number of
+ * keys that a sequence has beyond its prefix, which are split by that: state max_prefix
+ * closely where they are many (one sequence of 32768 keys on 8 kv heads behind 1024: 38
+ * us with 1024, 107 with max_len, 35 without groups).  Sharing does not pay where the rows of
+ * prompts fill whole tiles by themselves, nor for few shared keys.  Its workspace is
  * aio_prefix_workspace_bytes's.  Errors as aio_paged_attention; AIO_EINVAL: a null
  * or misaligned array of the groups; AIO_ERANGE: negative counts, or more groups than 2^30. */
 int aio_prefix_attention(const aio_paged_kv* kv, const aio_seqs* s, const aio_prefixes* x,

@@ -699,7 +699,8 @@ def aio_prefix_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens
                          ws: torch.Tensor | None = None) -> None:
     """aio_paged_attention of sequences in groups: those from cu_seqs[g] up to
     cu_seqs[g + 1] begin with the same prefix_lens[g] keys, which are read once for all
-    of them.  max_prefix: no prefix is longer (default: max_len)."""
+    of them.  max_prefix: no prefix is longer (default: max_len; state it closely where
+    sequences have many keys beyond their prefixes, which are split by the difference)."""
     at = _device_of(q, k, v, lens, table, cu_seqs, prefix_lens, out, cu_q, lse, ws)
     kv, kv_heads, page_size, hd = _paged(k, v)
     a = _attn(q, out, lse, scale)
