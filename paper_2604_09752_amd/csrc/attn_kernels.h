@@ -44,7 +44,9 @@ AIO_DEV f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 }
 
 // Eight fp32 values as NT bf16 operands: one, rounded to nearest even, or
-// three that add up to the value exactly.
+// three that add up to the value exactly.  Weights of bf16 queries take one: off by 2^-8 of
+// themselves at most, of either sign, they leave outputs 2.1e-3 to 2.3e-3 from 64 bits, of which the
+// outputs' own rounding to bf16 is 1.7e-3; three would take three times the products.
 template <int NT>
 AIO_DEV void terms(const float (&x)[8], bf16x8 (&t)[NT]) {
   if constexpr (NT == 1) {
@@ -177,7 +179,7 @@ AIO_DEV void carry(T& hi, T& lo) {
 // k_attn_step and of 64 in k_attn_rows: 96 and 384 matrix instructions on one sum in
 // between.  Equal values under 131072 equal keys: 1e-3 off in one sum of the prompt rows,
 // 4e-6 carried every 32 blocks, 2e-6 every 16; 8192 rows of 32 heads take 1406, 1432 and
-// 1457 us.  (bf16 outputs round to 2^-9, which no such chain comes near.)
+// 1457 us.  (bf16 outputs round to 2^-8 of themselves, which no such chain comes near.)
 constexpr int kStepCarry = 32, kRowsCarry = 32;
 
 // --------------------------------------------------------- shared prefixes
@@ -706,9 +708,10 @@ __global__ __launch_bounds__(kBlock, NT == 1 ? 3 : HD == 64 ? 4 : 2) void k_attn
 // to the key's score and to the value's weight, 16 products instead of 128.  What bounds it is the
 // reading of the codes (two requests of 32768 keys, 32 heads of 128, fp32: 92 us, 5.9 TB/s; with
 // bf16 made before LDS, 126), or with few keys the launch and three dependent reads (one request
-// of 201 keys: 7.2 us).  24 ragged requests of up to 4096 keys: 27 us, 3.3 TB/s, of which the
-// join, the start and seven blocks one after the other in the longest workgroups are half.  Two
-// blocks in flight instead of one: no faster (7 % and 2 % slower).
+// of 201 keys: 7.2 us).  24 ragged requests of up to 4096 keys, 89 MB: 25 us and 4 for the join; 24 of
+// 1792 keys each, as many, take 26, so it is not the longest that count, and of 3584 keys 43: 5.3 TB/s,
+// behind a start and an end of 9 us.  Two blocks in flight instead of one: no faster (7 % and 2 %
+// slower).
 template <int HD>
 struct Step8Lds {
   // bytes of a row, and of the second 16 rows from the first: the 16 rows of an operand, and
@@ -1630,9 +1633,10 @@ __global__ __launch_bounds__(W * AIO_WAVE, NT == 1 ? 2 : 1) void k_attn_rows(
 // One new token of each sequence in groups of many columns: shared keys as the rows of a prompt,
 // 128 columns for a key that is staged once, every sequence's own keys as a step (48 rows of 32
 // heads on 8 behind 8192 keys, bf16: 34 us; all as steps of 16 columns, 42, where LDS and the
-// caches' lines are two thirds busy; of 32 columns, 37).  What bounds it is one tile after the other
-// in each workgroup (2.3 us per 64 keys, whether one or two are on a CU), and the start and
-// the join, 10 us.
+// caches' lines are two thirds busy; of 32 columns, 37).  The kernel takes 30.7 us behind 8192 keys (8
+// tiles per workgroup), 25.0 behind 4096, 22.8 behind 2048 and 21.3 behind 1024: 1.3 us per
+// tile, and 20 that no shared key takes, of which the own keys are 4 (26.6 behind 8192 with one own key
+// each); the rest is the start, the chain of reads before the first key, and the end.
 template <int HD, int NT, bool Q8>
 struct WideLds {
   static constexpr int ROWS = RowsLds<HD>::BYTES(NT, kWaves);
