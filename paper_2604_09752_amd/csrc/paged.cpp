@@ -97,6 +97,7 @@ bool grids_overlap(const Blocks& a, const Blocks& b, int64_t pages, int64_t head
   if (a.page == b.page && !lines_overlap(d, pages, a.page, a_heads, b.page, b_heads)) return false;
   const wide a_pages = (pages - 1) * (wide)a.page + a.size, b_pages = (pages - 1) * (wide)b.page + b.size;
   if (!lines_overlap(d, heads, a.head, a_pages, b.head, b_pages)) return false;
+  if (pages == 1) return true;  // (one block each indeed)
   auto at = [&](wide from) { return lines_overlap(from, pages, a.page, a.size, b.page, b.size); };
   if (a.head == b.head) {
     for (int64_t h = 1 - heads; h < heads; ++h)

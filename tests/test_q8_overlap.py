@@ -119,3 +119,13 @@ def test_numbers_near_the_largest_do_not_wrap(L):
     assert not refused(L, kv)
     kv.k_exp_dev = BASE + CODES
     assert refused(L, kv)
+
+
+def test_one_page_of_many_heads_is_compared_at_once(L):
+    heads = 1 << 30
+    kv = pool(BASE, BASE + CODES // 2, 1 << 61, 1 << 62, 0, 2 * CODES, 0, SIZE, 1, heads)
+    assert refused(L, kv)
+    kv.v_dev = BASE + CODES
+    assert not refused(L, kv)
+    kv.v_dev = BASE + 2 * CODES * (heads - 1) + 16
+    assert refused(L, kv)
